@@ -1,0 +1,58 @@
+// Internal launchers of the paged key-value cache (host side).  kv_capi.hip
+// validates arguments and calls these; every launcher only enqueues work.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/rift_kv.h"
+
+namespace rift {
+
+constexpr int kMaxRotary = 256;
+
+// One of the two row sets that a rotation takes: n heads a row.
+struct RopeRows {
+    const void* x;
+    void* y;
+    int64_t ld_x, ld_y;
+    int n;
+};
+struct RopeFreqs {
+    double f[kMaxRotary / 2];   // turns (not radians) a position of each pair
+};
+hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, int rows, int head_dim,
+                          int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st);
+
+// Where rows go, or come from: the page table and each row's sequence and position.
+struct KvPlaces {
+    const int* table;
+    int n_seq, max_pages;
+    const int* seq_ids;     // null: row i is of sequence i
+    const int* positions;
+    int rows;
+    int* status;
+};
+hipError_t launch_kv_write(const riftkv_cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v, bool bf16,
+                           const KvPlaces& at, hipStream_t st);
+hipError_t launch_kv_read(const riftkv_cache& c, void* k, int64_t ld_k, void* v, int64_t ld_v, bool bf16,
+                          const KvPlaces& at, hipStream_t st);
+
+struct KvAttention {
+    const void* q;
+    void* out;
+    int64_t ld_q, ld_out;
+    int n_heads;
+    bool bf16;              // type of q and out
+    const int* table;
+    int n_seq, max_pages;
+    const int* lens;
+    float scale;
+    int* status;
+    void* workspace;
+};
+size_t kv_attention_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages);
+hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipStream_t st);
+
+}  // namespace rift

@@ -1,0 +1,261 @@
+"""The paged key-value cache (include/rift_kv.h): rotary positions, rows into
+pages and out of them, attention of one new token a sequence.
+
+Argument marshalling only, as in _lib: tensors are checked, raw pointers and the
+stream go to the C ABI, and a non-OK status raises RiftError.  Rows are
+[rows][heads][head_dim] tensors whose heads and elements are contiguous; the
+rows themselves may be any stride apart (slices of a projection).  All tensors
+of a call are on one device, which need not be the current one."""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+from typing import Optional
+
+from ._lib import RIFT_BF16, RIFT_F32, _check, load
+
+RIFTKV_F32, RIFTKV_BF16, RIFTKV_FP8, RIFTKV_INT8 = 0, 1, 2, 3
+# Every symbol include/rift_kv.h declares, in declaration order.
+KV_EXPORTS = ("riftkv_abi_version", "riftkv_rope_freqs", "riftkv_rope", "riftkv_write", "riftkv_read",
+              "riftkv_attention_workspace_size", "riftkv_attention")
+ROPE_SCALINGS = ("none", "linear", "base", "ramp", "bands")
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + \
+        [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dt")]
+
+
+class _RopeStruct(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32)] + \
+        [(n, ctypes.c_double) for n in ("base", "factor", "original_len", "low", "high")]
+
+
+_lib: Optional[ctypes.CDLL] = None
+torch = _ROWS = _STORES = None   # set by the first call: importing the package does not import torch
+
+
+def _load() -> ctypes.CDLL:
+    global _lib, torch, _ROWS, _STORES
+    if _lib is None:
+        import torch as t
+        torch = t
+        _ROWS = {t.bfloat16: RIFT_BF16, t.float32: RIFT_F32}
+        _STORES = {t.float32: RIFTKV_F32, t.bfloat16: RIFTKV_BF16, t.float8_e4m3fn: RIFTKV_FP8, t.int8: RIFTKV_INT8}
+        L = load()
+        P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        F32, F64 = ctypes.c_float, ctypes.c_double
+        L.riftkv_abi_version.restype = I32
+        L.riftkv_abi_version.argtypes = []
+        L.riftkv_rope_freqs.restype = I32
+        L.riftkv_rope_freqs.argtypes = [P, P, P]
+        L.riftkv_rope.restype = I32
+        L.riftkv_rope.argtypes = [P, I64, I32, P, I64, P, I64, I32, P, I64, I32, P, I32, I32, I32, I32, P, F64, P]
+        for name in ("riftkv_write", "riftkv_read"):
+            getattr(L, name).restype = I32
+            getattr(L, name).argtypes = [P, P, I64, P, I64, I32, P, I32, I32, P, P, I32, P, P]
+        L.riftkv_attention_workspace_size.restype = SZ
+        L.riftkv_attention_workspace_size.argtypes = [P, I32, I32, I32]
+        L.riftkv_attention.restype = I32
+        L.riftkv_attention.argtypes = [P, P, I64, I32, I32, P, I32, I32, P, F32, P, I64, P, P, SZ, P]
+        _lib = L
+    return _lib
+
+
+# ----------------------------------------------------------------------------- checks
+def _dense(t, dtype, shape, device, name):
+    """A contiguous device tensor; shape None: any."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    if t.device != device:
+        raise ValueError(f"{name}: must be on {device}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, shape, device, name):
+    """[rows][heads][head_dim], the last two contiguous: (pointer, elements between rows)."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name}: must be on {device}")
+    n, heads, hd = shape
+    st = t.stride()
+    if (hd > 1 and st[2] != 1) or (heads > 1 and st[1] != hd):
+        raise ValueError(f"{name}: heads and elements must be contiguous")
+    return t.data_ptr(), (st[0] if n > 1 else heads * hd)
+
+
+def _device_of(t, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a device tensor")
+    return t.device
+
+
+def _row_type(t, name):
+    dt = _ROWS.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    return dt
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _on(device):
+    """The device as the current one for a call."""
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _stream(stream, device):
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if s.device != device:
+        raise ValueError(f"stream: must be on {device}")
+    return s.cuda_stream or None
+
+
+# ----------------------------------------------------------------------------- the pages
+class KvCache:
+    """One layer's pages, as riftkv_cache made them: what the calls take."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        _load()
+        dev = _device_of(k, "k")
+        dt = _STORES.get(k.dtype)
+        if dt is None:
+            raise TypeError(f"k: unsupported storage dtype {k.dtype}")
+        if k.dim() != 4:
+            raise ValueError("k: expected [n_pages][n_kv_heads][page_size][head_dim]")
+        shape = tuple(k.shape)
+        scaled = dt in (RIFTKV_FP8, RIFTKV_INT8)
+        if scaled != (k_scale is not None) or scaled != (v_scale is not None):
+            raise ValueError("k_scale and v_scale go with 8-bit pages, and only with them")
+        p = [_dense(k, k.dtype, shape, dev, "k"), _dense(v, k.dtype, shape, dev, "v"), None, None]
+        if scaled:
+            p[2] = _dense(k_scale, torch.uint8, shape[:3], dev, "k_scale")
+            p[3] = _dense(v_scale, torch.uint8, shape[:3], dev, "v_scale")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device, self.dt = dev, dt
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
+        self.struct = _CacheStruct(*p, shape[0], shape[2], shape[1], shape[3], dt)
+        self.ref = ctypes.byref(self.struct)
+
+
+def riftkv_cache(k, v, k_scale=None, v_scale=None) -> KvCache:
+    """A handle on pages k, v [n_pages][n_kv_heads][page_size][head_dim] (bf16, f32,
+    float8_e4m3fn or int8; 8-bit ones with scale bytes [n_pages][n_kv_heads][page_size],
+    uint8).  It keeps the tensors; make it once."""
+    return KvCache(k, v, k_scale, v_scale)
+
+
+# ----------------------------------------------------------------------------- positions
+def riftkv_rope_freqs(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                      original_len: float = 0.0, low: float = 0.0, high: float = 0.0):
+    """Host-only call: (float64 numpy array of rotary_dim / 2 angles a position,
+    magnitude) for riftkv_rope."""
+    import numpy as np
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling: one of {ROPE_SCALINGS}")
+    cfg = _RopeStruct(int(rotary_dim), ROPE_SCALINGS.index(scaling), float(base), float(factor), float(original_len),
+                      float(low), float(high))
+    out = np.zeros(max(1, int(rotary_dim) // 2), dtype=np.float64)
+    mag = ctypes.c_double(0.0)
+    _check(_load().riftkv_rope_freqs(ctypes.byref(cfg), out.ctypes.data, ctypes.byref(mag)), "riftkv_rope_freqs")
+    return out, float(mag.value)
+
+
+def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "half", magnitude: float = 1.0,
+                stream=None) -> None:
+    """Rotates the rows q and k (either may be None) into q_out and k_out (None: in
+    place) by positions [rows] i32.  freqs: float64 numpy array of rotary_dim / 2
+    angles a position (riftkv_rope_freqs)."""
+    L = _load()
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("q or k is needed")
+    dev, dt, rows, hd = _device_of(x, "rows"), _row_type(x, "rows"), x.shape[0], x.shape[-1]
+    args = []
+    for t, o, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if t is None:
+            if o is not None:
+                raise ValueError(f"{name}_out without {name}")
+            args += [None, 0, 0, None, 0]
+            continue
+        if t.dim() != 3:
+            raise ValueError(f"{name}: expected [rows][heads][head_dim]")
+        shape = (rows, t.shape[1], hd)
+        p, ld = _rows(t, x.dtype, shape, dev, name)
+        po, ldo = (p, ld) if o is None else _rows(o, x.dtype, shape, dev, name + "_out")
+        args += [p, ld, shape[1], po, ldo]
+    if freqs.dtype != "float64" or not freqs.flags.c_contiguous:
+        raise TypeError("freqs: expected a contiguous float64 array")
+    pos = _dense(positions, torch.int32, (rows,), dev, "positions")
+    with _on(dev):
+        st = L.riftkv_rope(*args, dt, pos, rows, hd, 2 * freqs.size, ROPE_LAYOUTS[layout], freqs.ctypes.data,
+                           magnitude, _stream(stream, dev))
+    if st:
+        _check(st, "riftkv_rope")
+
+
+# ----------------------------------------------------------------------------- rows
+def _move(name, cache, k, v, page_table, positions, status, seq_ids, stream):
+    dev, rows = cache.device, k.shape[0]
+    dt = _row_type(k, "k")
+    shape = (rows, cache.n_kv_heads, cache.head_dim)
+    pk, ldk = _rows(k, k.dtype, shape, dev, "k")
+    pv, ldv = _rows(v, k.dtype, shape, dev, "v")
+    n_seq, max_pages = page_table.shape
+    table = _dense(page_table, torch.int32, None, dev, "page_table")
+    pos = _dense(positions, torch.int32, (rows,), dev, "positions")
+    ids = None if seq_ids is None else _dense(seq_ids, torch.int32, (rows,), dev, "seq_ids")
+    word = _dense(status, torch.int32, (1,), dev, "status")
+    with _on(dev):
+        st = getattr(_load(), name)(cache.ref, pk, ldk, pv, ldv, dt, table, n_seq, max_pages, ids, pos, rows, word,
+                                    _stream(stream, dev))
+    if st:
+        _check(st, name)
+
+
+def riftkv_write(cache: KvCache, k, v, page_table, positions, status, seq_ids=None, stream=None) -> None:
+    """Rows k, v [rows][n_kv_heads][head_dim] into the pages of their sequences:
+    row i is at positions[i] of sequence seq_ids[i] (None: i); page_table
+    [n_seq][max_pages], all i32.  Negative ones are skipped."""
+    _move("riftkv_write", cache, k, v, page_table, positions, status, seq_ids, stream)
+
+
+def riftkv_read(cache: KvCache, page_table, positions, k_out, v_out, status, seq_ids=None, stream=None) -> None:
+    """The same rows out of the pages, into k_out and v_out."""
+    _move("riftkv_read", cache, k_out, v_out, page_table, positions, status, seq_ids, stream)
+
+
+# ----------------------------------------------------------------------------- attention
+def riftkv_attention_workspace_size(cache: KvCache, n_seq: int, n_heads: int, max_pages: int) -> int:
+    return int(_load().riftkv_attention_workspace_size(cache.ref, int(n_heads), int(n_seq), int(max_pages)))
+
+
+def riftkv_attention(cache: KvCache, q, page_table, lens, out, workspace, status, scale: Optional[float] = None,
+                     stream=None) -> None:
+    """out[i] := attention of q[i] [n_heads][head_dim] over the first lens[i] tokens of
+    sequence i's pages; scale None: 1 / sqrt(head_dim)."""
+    dev = cache.device
+    dt = _row_type(q, "q")
+    n_seq, max_pages = page_table.shape
+    shape = (n_seq, q.shape[1], cache.head_dim)
+    pq, ldq = _rows(q, q.dtype, shape, dev, "q")
+    po, ldo = _rows(out, q.dtype, shape, dev, "out")
+    table = _dense(page_table, torch.int32, None, dev, "page_table")
+    n = _dense(lens, torch.int32, (n_seq,), dev, "lens")
+    word = _dense(status, torch.int32, (1,), dev, "status")
+    ws = _dense(workspace, torch.uint8, None, dev, "workspace")
+    with _on(dev):
+        st = _load().riftkv_attention(cache.ref, pq, ldq, shape[1], dt, table, n_seq, max_pages, n,
+                                      cache.head_dim ** -0.5 if scale is None else scale, po, ldo, word, ws,
+                                      workspace.numel(), _stream(stream, dev))
+    if st:
+        _check(st, "riftkv_attention")
