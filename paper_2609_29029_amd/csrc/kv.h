@@ -53,6 +53,8 @@ struct KvAttention {
     void* workspace;
 };
 size_t kv_attention_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages);
+// whether 64-bit counts hold the call's tiles
+bool kv_attention_counts(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages);
 hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipStream_t st);
 
 }  // namespace rift

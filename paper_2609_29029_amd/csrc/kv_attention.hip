@@ -1,81 +1,696 @@
-// One query token of every sequence over its paged keys and values: a wave takes
-// one query head of one sequence and walks the tokens with a running maximum and sum.
+// One query token of every sequence over its paged keys and values, split over the
+// length and joined.
+//
+//   attention_kernel   The tiles (32 tokens of one sequence and head group) of all
+//                      sequences, one after the other, are dealt out evenly to the
+//                      waves, in runs: however uneven the lengths, waves finish
+//                      together, and a wave writes at most two results of parts.
+//                      Heads a wave finishes go straight to the output, the parts at
+//                      its ends meet in LDS, and what a workgroup holds only a part
+//                      of goes to its two slots of the workspace.
+//   join_kernel        the parts of heads that several workgroups share; sequences
+//                      without tokens.
+//
+// A head group is up to 16 query heads of one key head.  With the tile's tokens as rows,
+// S^T = K Q^T leaves a lane the scores of one query and 8 tokens; they are the lane's
+// own share of the second product's right operand, O^T = V^T P^T, if its token
+// order is the lanes' (a sum's order is free), and a lane's own rows of V are, with two
+// bytes or halfwords exchanged in registers, its share of the left one.  So nothing
+// passes through LDS, and the softmax is a lane's own but for two swaps.  Unused
+// query columns cost nothing: the bytes of keys and values bound this kernel.
+//
+// Scores, weights and sums are float32; each weight goes into the matrix product as
+// bf16 terms that add up to it (two: 2^-17 of it, three: 2^-25, for float32 rows),
+// each float32 query as three.
+#include <type_traits>
+
 #include "kv_device.h"
 
 namespace rift {
 
 namespace {
 
-template <riftkv_dtype DT>
-__device__ __forceinline__ float cached(const void* pages, const uint8_t* scales, size_t row, int hd, int e) {
-    const size_t i = row * hd + e;
-    if constexpr (DT == RIFTKV_F32) return static_cast<const float*>(pages)[i];
-    else if constexpr (DT == RIFTKV_BF16) return bf16_to_f32(static_cast<const bf16_t*>(pages)[i]);
+constexpr int kTile = 32;                 // tokens of a tile
+constexpr int kWaves = 4;                 // of a workgroup
+constexpr int kThreads = 64 * kWaves;
+constexpr int kMinTiles = 2;              // a wave's share, where there are fewer than waves to share them
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+struct AttnParams {
+    const void* q;
+    void* out;
+    int64_t ld_q, ld_out;
+    const unsigned char *k, *v;
+    const uint8_t *ks, *vs;
+    const int* table;
+    const int* lens;
+    int* status;
+    float* slots;          // [wgs][2][rows][HD + 4]: weighted values, max, sum
+    int4* joins;           // [wgs]: sequence, head group and last workgroup of a head begun here
+    int n_seq, max_pages, n_pages, n_kv, shift, group, q_tiles, rows;
+    float scale_log2;
+};
+
+// A place in the sequence of tiles.
+struct Place {
+    int seq, hq, tile, len;
+};
+
+__device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
+
+// 0 for a length out of range.
+__device__ __forceinline__ int length_of(int len, int max_pages, int shift) {
+    return len < 0 || (int64_t)len > ((int64_t)max_pages << shift) ? 0 : len;
+}
+
+__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// Maximum and sum over the four lanes that hold a query's tokens (16 lanes apart).
+__device__ __forceinline__ float quad_max(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Two 8-bit codes (half `hi` of w) as two bf16 values, exact.
+template <riftkv_dtype DT, bool HI>
+__device__ __forceinline__ uint32_t widen(uint32_t w) {
+    if constexpr (DT == RIFTKV_FP8)
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
     else {
-        const uint32_t code = static_cast<const uint8_t*>(pages)[i];
-        const float f = DT == RIFTKV_FP8 ? __builtin_amdgcn_cvt_f32_fp8((int)code, 0) : (float)(int8_t)code;
-        return f * scale_of(scales[row]);
+        const float a = (float)(int8_t)(w >> (HI ? 16 : 0)), b = (float)(int8_t)(w >> (HI ? 24 : 8));
+        return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
     }
 }
 
-template <typename T, riftkv_dtype DT>
-__global__ void __launch_bounds__(64)
-attention_kernel(riftkv_cache c, KvAttention a) {
-    const int seq = blockIdx.x / a.n_heads, h = blockIdx.x - seq * a.n_heads, lane = threadIdx.x;
-    const int kvh = h / (a.n_heads / c.n_kv_heads), hd = c.head_dim, shift = 31 - __clz(c.page_size);
-    const int len = a.lens[seq];
-    const size_t q0 = (size_t)seq * a.ld_q + (size_t)h * hd, o0 = (size_t)seq * a.ld_out + (size_t)h * hd;
-    auto load_q = [&](int e) {
-        if constexpr (sizeof(T) == 2) return bf16_to_f32(static_cast<const bf16_t*>(a.q)[q0 + e]);
-        else return static_cast<const float*>(a.q)[q0 + e];
-    };
-    const float q1 = load_q(lane), q2 = hd == 128 ? load_q(lane + 64) : 0.f;
-    bool bad = len < 0 || (int64_t)len > ((int64_t)a.max_pages << shift);
-    float m = -INFINITY, l = 0.f, o1 = 0.f, o2 = 0.f;
-    for (int j = 0; j < len && !bad; ++j) {
-        const int page = a.table[(size_t)seq * a.max_pages + (j >> shift)];
-        if (page < 0 || page >= c.n_pages) {
-            bad = true;
-            break;
+// Terms of bf16 that add up to x.
+template <int N>
+__device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        t[i] = static_cast<__bf16>(x);
+        x -= static_cast<float>(t[i]);
+    }
+}
+
+template <int N>
+struct Words {
+    typedef uint32_t type __attribute__((ext_vector_type(N)));
+};
+template <>
+struct Words<1> {
+    typedef uint32_t type;
+};
+
+// N words from p.
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char* p) {
+    constexpr int C = N < 4 ? N : 4;
+    typedef typename Words<C>::type vec;
+#pragma unroll
+    for (int i = 0; i < N / C; ++i) {
+        const vec x = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p) + i);
+        if constexpr (C == 1) w[0] = x;
+        else
+#pragma unroll
+            for (int j = 0; j < C; ++j) w[C * i + j] = x[j];
+    }
+}
+
+// T: type of queries and outputs.
+template <typename T, riftkv_dtype DT, int HD>
+__global__ void __launch_bounds__(kThreads, 2)
+attention_kernel(AttnParams p) {
+    constexpr int B = DT == RIFTKV_F32 ? 4 : DT == RIFTKV_BF16 ? 2 : 1;   // bytes a value
+    constexpr bool SCALED = B == 1, F32 = DT == RIFTKV_F32;
+    constexpr int KL = HD * B / 64;          // 16-byte loads of a lane for 16 keys
+    constexpr int VW = HD * B / 64;          // words of a lane of one value row
+    constexpr int C = HD / 16;               // columns of a lane of one value row
+    constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
+    constexpr int RS = HD + 4;               // floats of a part's row: values, max, sum (and odd to the banks)
+    extern __shared__ __align__(16) float records[];   // [2 kWaves][rows][RS]
+    __shared__ int4 meta[2 * kWaves];        // sequence (-1: no record), head group, whether it begins and ends the head
+    __shared__ long long head_end[2 * kWaves];   // the tile after the head's last
+    __shared__ long long sums[kWaves];
+    __shared__ int found_seq[kWaves];
+    __shared__ long long found_at[kWaves];   // tiles before that sequence
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, g = lane >> 4;
+    const int HQ = p.n_kv * p.q_tiles;
+    const int slot_floats = p.rows * RS;
+
+    // This wave's share of the tiles: a thread sums a run of sequences, the workgroup
+    // scans the sums, and whoever holds a wave's first tile looks it up.
+    const int per = (p.n_seq + kThreads - 1) / kThreads;
+    const int s0 = min(tid * per, p.n_seq), s1 = min(s0 + per, p.n_seq);
+    long long mine = 0;
+    for (int s = s0; s < s1; ++s) mine += tiles_of(length_of(p.lens[s], p.max_pages, p.shift));
+    long long incl = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const long long o = __shfl_up(incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 63) sums[wave] = incl;
+    if (tid < 2 * kWaves) meta[tid] = make_int4(-1, 0, 0, 0);
+    __syncthreads();
+    long long before = incl - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) before += sums[w];
+        total += sums[w];
+    }
+    const unsigned long long N = (unsigned long long)total * HQ;
+    const unsigned long long all = (unsigned long long)gridDim.x * kWaves, most = (N + kMinTiles - 1) / kMinTiles;
+    const unsigned W = (unsigned)(most < all ? most : all);      // waves with tiles
+    auto first_of = [&](unsigned w) { return (long long)(N * w / W); };   // N W < 2^64: W <= 2^12, N <= 2^16 2^12 2^26
+    if (mine > 0) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const unsigned gw = blockIdx.x * kWaves + w;
+            if (gw >= W) continue;
+            const long long a = first_of(gw);
+            if (a >= before * HQ && a < (before + mine) * HQ) {
+                long long at = before;
+                int s = s0;
+                for (;; ++s) {
+                    const int t = tiles_of(length_of(p.lens[s], p.max_pages, p.shift));
+                    if (a < (at + t) * HQ) break;
+                    at += t;
+                }
+                found_seq[w] = s;
+                found_at[w] = at;
+            }
         }
-        const size_t row = ((((size_t)page * c.n_kv_heads) + kvh) << shift) + (j & (c.page_size - 1));
-        float s = q1 * cached<DT>(c.k, c.k_scale, row, hd, lane);
-        if (hd == 128) s = fmaf(q2, cached<DT>(c.k, c.k_scale, row, hd, lane + 64), s);
-        s = wave_sum(s) * a.scale;
-        const float mn = fmaxf(m, s), ref = mn == -INFINITY ? 0.f : mn;
-        const float f = expf(m - ref), p = expf(s - ref);
-        l = fmaf(l, f, p);
-        o1 = fmaf(o1, f, p * cached<DT>(c.v, c.v_scale, row, hd, lane));
-        if (hd == 128) o2 = fmaf(o2, f, p * cached<DT>(c.v, c.v_scale, row, hd, lane + 64));
-        m = mn;
     }
-    if (bad) {
-        *a.status = RIFT_ERR_SHAPE;
-        l = NAN;
+    __syncthreads();
+
+    const unsigned gw = blockIdx.x * kWaves + wave;
+    if (gw < W) {
+        const long long a = first_of(gw);
+        int left = __builtin_amdgcn_readfirstlane((int)(first_of(gw + 1) - a));
+        Place cur;
+        cur.seq = __builtin_amdgcn_readfirstlane(found_seq[wave]);
+        cur.len = __builtin_amdgcn_readfirstlane(p.lens[cur.seq]);
+        {
+            const long long in = a - found_at[wave] * HQ;      // tiles of the sequence before
+            const int t = tiles_of(cur.len);
+            cur.hq = __builtin_amdgcn_readfirstlane((int)(in / t));
+            cur.tile = __builtin_amdgcn_readfirstlane((int)(in - (long long)cur.hq * t));
+        }
+        auto after = [&](Place c) __attribute__((always_inline)) {
+            if ((c.tile + 1) * kTile < c.len) {
+                ++c.tile;
+                return c;
+            }
+            c.tile = 0;
+            if (++c.hq == HQ) {
+                c.hq = 0;
+                do {
+                    ++c.seq;
+                    c.len = length_of(p.lens[c.seq], p.max_pages, p.shift);
+                } while (c.len == 0);
+            }
+            return c;
+        };
+        // pages of the two halves of a tile (the second's may be past the end: the first's)
+        struct Pages {
+            int a, b;
+        };
+        auto pages_at = [&](const Place& c) __attribute__((always_inline)) {
+            const int* row = p.table + (size_t)c.seq * p.max_pages;
+            const int t0 = c.tile * kTile, t1 = t0 + 16 < c.len ? t0 + 16 : t0;
+            return Pages{row[t0 >> p.shift], row[t1 >> p.shift]};
+        };
+        uint32_t kr[2][KL][4], vr[2][4][VW], ksc[2], vsc[2];
+        const unsigned k_lane = n * HD * B + g * 16, v_lane = g * 4 * HD * B + n * VW * 4;
+        // first row of a half's keys and values among the pages' rows
+        auto row_of = [&](const Place& c, int page, int h) __attribute__((always_inline)) {
+            page = (unsigned)page < (unsigned)p.n_pages ? page : 0;
+            return ((((size_t)page * p.n_kv) + c.hq / p.q_tiles) << p.shift) + ((c.tile * kTile + 16 * h) & ((1 << p.shift) - 1));
+        };
+        auto load_k = [&](const Place& c, const Pages& pg, bool live) __attribute__((always_inline)) {
+            const unsigned off = live ? k_lane : 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const size_t r = row_of(c, h ? pg.b : pg.a, h);
+#pragma unroll
+                for (int i = 0; i < KL; ++i) load_words<4>(kr[h][i], p.k + r * (HD * B) + off + 64 * i);
+                if constexpr (SCALED) ksc[h] = *reinterpret_cast<const uint32_t*>(p.ks + r + 4 * g);
+            }
+        };
+        auto load_v = [&](const Place& c, const Pages& pg, bool live) __attribute__((always_inline)) {
+            const unsigned off = live ? v_lane : 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const size_t r = row_of(c, h ? pg.b : pg.a, h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) load_words<VW>(vr[h][i], p.v + r * (HD * B) + off + i * (HD * B));
+                if constexpr (SCALED) vsc[h] = *reinterpret_cast<const uint32_t*>(p.vs + r + 4 * g);
+            }
+        };
+
+        Pages cur_pages = pages_at(cur);
+        load_k(cur, cur_pages, true);
+        load_v(cur, cur_pages, true);
+        Place nxt = left > 1 ? after(cur) : cur;
+        Pages nxt_pages = pages_at(nxt);
+
+        bf16x8_t qf[F32 ? 1 : NQ][F32 ? 1 : HD / 32];
+        float qs[F32 ? HD / 4 : 1];
+        f32x4_t o[C];
+        float m = -INFINITY, l = 0.f;
+        bool bad = false;          // a page of the head is out of range
+        int begin = cur.tile;      // this wave's first tile of the head
+        int n_records = 0;
+        auto start_head = [&](const Place& c) __attribute__((always_inline)) {
+            const int kvh = c.hq / p.q_tiles, r = (c.hq - kvh * p.q_tiles) * 16 + n;   // this lane's query
+            const bool there = r < p.group;
+            const size_t q0 = (size_t)c.seq * p.ld_q + (size_t)(kvh * p.group + (there ? r : 0)) * HD;
+            if constexpr (F32) {
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i) {
+                    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p.q) + q0 + 16 * i + 4 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) qs[4 * i + e] = there ? x[e] : 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int f = 0; f < HD / 32; ++f) {
+                    const size_t at = q0 + (SCALED ? (f >> 1) * 64 + g * 16 + (f & 1) * 8 : f * 32 + g * 8);
+                    if constexpr (NQ == 1) {
+                        u32x4_t x = *reinterpret_cast<const u32x4_t*>(static_cast<const bf16_t*>(p.q) + at);
+                        if (!there) x = u32x4_t{0, 0, 0, 0};
+                        qf[0][f] = __builtin_bit_cast(bf16x8_t, x);
+                    } else {
+                        const float* src = static_cast<const float*>(p.q) + at;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            __bf16 t[NQ];
+                            split_bf16<NQ>(there ? src[e] : 0.f, t);
+#pragma unroll
+                            for (int i = 0; i < NQ; ++i) qf[i][f][e] = t[i];
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            m = -INFINITY;
+            l = 0.f;
+            bad = false;
+        };
+        start_head(cur);
+
+        for (;;) {
+            const bool live = left > 1;
+            bad |= (unsigned)cur_pages.a >= (unsigned)p.n_pages || (unsigned)cur_pages.b >= (unsigned)p.n_pages;
+            // scores: s[4 h + i] of this lane's query and token 16 h + 4 g + i of the tile
+            float s[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (F32) {
+#pragma unroll
+                    for (int i = 0; i < KL; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][i][e]), qs[4 * i + e], acc, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int f = 0; f < HD / 32; ++f) {
+                        u32x4_t kw;
+                        if constexpr (SCALED) {
+                            const uint32_t w0 = kr[h][f >> 1][2 * (f & 1)], w1 = kr[h][f >> 1][2 * (f & 1) + 1];
+                            kw = u32x4_t{widen<DT, false>(w0), widen<DT, true>(w0), widen<DT, false>(w1), widen<DT, true>(w1)};
+                        } else {
+                            kw = u32x4_t{kr[h][f][0], kr[h][f][1], kr[h][f][2], kr[h][f][3]};
+                        }
+#pragma unroll
+                        for (int i = 0; i < NQ; ++i)
+                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kw), qf[i][f], acc, 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = acc[i];
+                    if constexpr (SCALED) x *= scale_of((ksc[h] >> (8 * i)) & 0xFFu);
+                    s[4 * h + i] = x * p.scale_log2;
+                }
+            }
+            load_k(nxt, nxt_pages, live);
+            const int there = cur.len - cur.tile * kTile - 4 * g;   // tokens from this lane's first on
+            const bool tail = cur.len - cur.tile * kTile < kTile;
+            if (tail) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (16 * (j >> 2) + (j & 3) >= there) s[j] = -INFINITY;
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[j]);
+            mx = quad_max(mx);
+            if (__any(mx > m)) {
+                const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - ref_of(mn));
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[c] *= f;
+            }
+            const float ref = ref_of(m);
+            float pr[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                pr[j] = __builtin_amdgcn_exp2f(s[j] - ref);
+                l += pr[j];
+                if constexpr (SCALED) pr[j] *= scale_of((vsc[j >> 2] >> (8 * (j & 3))) & 0xFFu);
+            }
+            if (tail) {   // whatever lies behind the last token: no part of the sum, NaN or not
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (16 * (j >> 2) + (j & 3) >= there) {
+                        pr[j] = 0.f;
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) vr[j >> 2][j & 3][w] = 0;
+                    }
+            }
+            if constexpr (F32) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j >> 2][j & 3][c]), pr[j], o[c], 0, 0, 0);
+            } else {
+                bf16x8_t pf[NP];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    __bf16 t[NP];
+                    split_bf16<NP>(pr[j], t);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) pf[i][j] = t[i];
+                }
+                auto add = [&](int c, const u32x4_t& vw) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int i = 0; i < NP; ++i)
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vw), pf[i], o[c], 0, 0, 0);
+                };
+#pragma unroll
+                for (int c = 0; c < C; c += 2) {   // columns c and c + 1 of the lane's rows, tokens in pairs
+                    u32x4_t v0, v1;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const uint32_t(&x)[VW] = vr[d >> 1][2 * (d & 1)], (&y)[VW] = vr[d >> 1][2 * (d & 1) + 1];
+                        if constexpr (SCALED) {
+                            const uint32_t w = __builtin_amdgcn_perm(y[c >> 2], x[c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+                            v0[d] = widen<DT, false>(w);
+                            v1[d] = widen<DT, true>(w);
+                        } else {
+                            v0[d] = __builtin_amdgcn_perm(y[c >> 1], x[c >> 1], 0x05040100u);
+                            v1[d] = __builtin_amdgcn_perm(y[c >> 1], x[c >> 1], 0x07060302u);
+                        }
+                    }
+                    add(c, v0);
+                    add(c + 1, v1);
+                }
+            }
+            load_v(nxt, nxt_pages, live);
+            const Place nn = left > 2 ? after(nxt) : nxt;
+            const Pages nn_pages = pages_at(nn);
+
+            const bool ends = (cur.tile + 1) * kTile >= cur.len;
+            if (ends || !live) {   // the wave's last tile of this head: o[c][i] is column (4 g + i) C + c of query n
+                float sum = quad_sum(l);
+                if (bad) {
+                    sum = NAN;
+                    if (lane == 0) *p.status = RIFT_ERR_SHAPE;
+                }
+                const int kvh = cur.hq / p.q_tiles, r0 = (cur.hq - kvh * p.q_tiles) * 16;
+                const bool valid = r0 + n < p.group;
+                if (begin == 0 && ends) {
+                    if (valid) {
+                        const float inv = 1.f / sum;
+                        const size_t o0 = (size_t)cur.seq * p.ld_out + (size_t)(kvh * p.group + r0 + n) * HD;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int c = 0; c < C; c += 4) {
+                                const size_t at = o0 + (4 * g + i) * C + c;
+                                if constexpr (sizeof(T) == 2) {
+                                    uint32_t w[2];
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e)
+                                        w[e] = (uint32_t)round_bf16(o[c + 2 * e][i] * inv) | (uint32_t)round_bf16(o[c + 2 * e + 1][i] * inv) << 16;
+                                    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + at) = make_uint2(w[0], w[1]);
+                                } else {
+                                    *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + at) =
+                                        f32x4_t{o[c][i] * inv, o[c + 1][i] * inv, o[c + 2][i] * inv, o[c + 3][i] * inv};
+                                }
+                            }
+                    }
+                } else {
+                    const int rec = 2 * wave + n_records++;
+                    if (lane == 0) {
+                        meta[rec] = make_int4(cur.seq, cur.hq, begin == 0, ends);
+                        head_end[rec] = first_of(gw + 1) - left - cur.tile + tiles_of(cur.len);
+                    }
+                    if (valid) {
+                        float* dst = records + (size_t)rec * slot_floats + n * RS;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int c = 0; c < C; c += 4)
+                                *reinterpret_cast<f32x4_t*>(dst + (4 * g + i) * C + c) = f32x4_t{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+                        if (g == 0) {
+                            dst[HD] = m;
+                            dst[HD + 1] = sum;
+                        }
+                    }
+                }
+                if (!live) break;
+                start_head(nxt);
+                begin = 0;
+            }
+            cur = nxt;
+            cur_pages = nxt_pages;
+            nxt = nn;
+            nxt_pages = nn_pages;
+            --left;
+        }
     }
-    const float inv = len == 0 ? 0.f : 1.f / l;
-    auto store = [&](int e, float x) {
-        if constexpr (sizeof(T) == 2) static_cast<bf16_t*>(a.out)[o0 + e] = round_bf16(x);
-        else static_cast<float*>(a.out)[o0 + e] = x;
-    };
-    store(lane, o1 * inv);
-    if (hd == 128) store(lane + 64, o2 * inv);
+    __syncthreads();
+
+    // Neighbouring records of one head are joined: a whole head goes to the output, the
+    // end of one begun in an earlier workgroup to slot 0, the start of one that goes
+    // on in the next to slot 1.
+    int4 join = make_int4(-1, 0, 0, 0);
+    for (int r = 0; r < 2 * kWaves;) {
+        const int4 a = meta[r];
+        if (a.x < 0) {
+            ++r;
+            continue;
+        }
+        int e = r + 1, ends = a.w;      // records r .. e - 1, absent ones among them
+        for (; e < 2 * kWaves; ++e) {
+            const int4 b = meta[e];
+            if (b.x < 0) continue;
+            if (b.x != a.x || b.y != a.y) break;
+            ends = b.w;
+        }
+        const int kvh = a.y / p.q_tiles, r0 = (a.y - kvh * p.q_tiles) * 16, rows = min(16, p.group - r0);
+        float* slot = p.slots + ((size_t)blockIdx.x * 2 + (a.z ? 1 : 0)) * slot_floats;
+        if (a.z && !ends)   // the wave with the head's last tile u: the largest w with N w / W < u + 1
+            join = make_int4(a.x, a.y, (int)(((unsigned long long)head_end[r] * W - 1) / N) / kWaves, 0);
+        for (int item = tid; item < rows * (HD / 4); item += kThreads) {
+            const int row = item / (HD / 4), col = 4 * (item % (HD / 4));
+            float mx = -INFINITY, L = 0.f;
+            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+            for (int i = r; i < e; ++i)
+                if (meta[i].x >= 0) mx = fmaxf(mx, records[(size_t)i * slot_floats + row * RS + HD]);
+            for (int i = r; i < e; ++i) {
+                if (meta[i].x < 0) continue;
+                const float* src = records + (size_t)i * slot_floats + row * RS;
+                const float f = __builtin_amdgcn_exp2f(src[HD] - ref_of(mx));
+                L = fmaf(f, src[HD + 1], L);
+                acc += f * *reinterpret_cast<const f32x4_t*>(src + col);
+            }
+            if (a.z && ends) {
+                const size_t at = (size_t)a.x * p.ld_out + (size_t)(kvh * p.group + r0 + row) * HD + col;
+                acc *= 1.f / L;
+                if constexpr (sizeof(T) == 2)
+                    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + at) =
+                        make_uint2((uint32_t)round_bf16(acc[0]) | (uint32_t)round_bf16(acc[1]) << 16,
+                                   (uint32_t)round_bf16(acc[2]) | (uint32_t)round_bf16(acc[3]) << 16);
+                else
+                    *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + at) = acc;
+            } else {
+                *reinterpret_cast<f32x4_t*>(slot + row * RS + col) = acc;
+                if (col == 0) {
+                    slot[row * RS + HD] = mx;
+                    slot[row * RS + HD + 1] = L;
+                }
+            }
+        }
+        r = e;
+    }
+    if (tid == 0) p.joins[blockIdx.x] = join;
+}
+
+// One workgroup for each of the first kernel's: the head that it begins and others go
+// on with, from its slot 1 and their slots 0.  Threads take four columns of a row and
+// every PG-th part, then join over LDS.
+constexpr int kJoinThreads = 1024;
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kJoinThreads)
+join_kernel(AttnParams p) {
+    constexpr int RS = HD + 4, CV = HD / 4;
+    __shared__ __align__(16) f32x4_t accs[kJoinThreads];
+    __shared__ float2 mls[kJoinThreads];
+    const int tid = threadIdx.x;
+    // sequences without tokens, or of a length out of range
+    for (int s = blockIdx.x; s < p.n_seq; s += gridDim.x) {
+        const int len = p.lens[s];
+        const bool bad = len != 0 && length_of(len, p.max_pages, p.shift) == 0;
+        if (len != 0 && !bad) continue;
+        if (bad && tid == 0) *p.status = RIFT_ERR_SHAPE;
+        for (int i = tid; i < p.n_kv * p.group * HD; i += kJoinThreads) {
+            if constexpr (sizeof(T) == 2) static_cast<bf16_t*>(p.out)[(size_t)s * p.ld_out + i] = bad ? 0x7FC0 : 0;
+            else static_cast<float*>(p.out)[(size_t)s * p.ld_out + i] = bad ? NAN : 0.f;
+        }
+    }
+    const int4 join = p.joins[blockIdx.x];
+    if (join.x < 0) return;
+    const int kvh = join.y / p.q_tiles, r0 = (join.y - kvh * p.q_tiles) * 16, rows = min(16, p.group - r0);
+    const int items = rows * CV, PG = kJoinThreads / items;       // at least 2 (16 rows of 32 vectors)
+    const int parts = join.z - (int)blockIdx.x + 1, slot_floats = p.rows * RS;
+    const int pg = tid / items, item = tid - pg * items, row = item / CV, col = 4 * (item - row * CV);
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    if (pg < PG) {
+        for (int i = pg; i < parts; i += PG) {
+            const float* src = p.slots + ((size_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * slot_floats + row * RS;
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(src + col);
+            const float mi = src[HD], li = src[HD + 1], mn = fmaxf(m, mi);
+            const float f = __builtin_amdgcn_exp2f(m - ref_of(mn)), fi = __builtin_amdgcn_exp2f(mi - ref_of(mn));
+            acc = acc * f + x * fi;
+            l = l * f + li * fi;
+            m = mn;
+        }
+    }
+    accs[tid] = acc;
+    mls[tid] = make_float2(m, l);
+    __syncthreads();
+    if (tid >= items) return;
+    float mx = m;
+    const int used = min(PG, parts);
+    for (int i = 1; i < used; ++i) mx = fmaxf(mx, mls[i * items + tid].x);
+    float f = __builtin_amdgcn_exp2f(m - ref_of(mx));
+    acc *= f;
+    l *= f;
+    for (int i = 1; i < used; ++i) {
+        const float2 ml = mls[i * items + tid];
+        f = __builtin_amdgcn_exp2f(ml.x - ref_of(mx));
+        acc += f * accs[i * items + tid];
+        l += f * ml.y;
+    }
+    acc *= 1.f / l;
+    const size_t at = (size_t)join.x * p.ld_out + (size_t)(kvh * p.group + r0 + row) * HD + col;
+    if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + at) =
+            make_uint2((uint32_t)round_bf16(acc[0]) | (uint32_t)round_bf16(acc[1]) << 16,
+                       (uint32_t)round_bf16(acc[2]) | (uint32_t)round_bf16(acc[3]) << 16);
+    else
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + at) = acc;
+}
+
+constexpr int kMaxWgs = 512;   // two workgroups a CU
+
+int q_tiles_of(const riftkv_cache& c, int n_heads) { return (n_heads / c.n_kv_heads + 15) / 16; }
+int rows_of(const riftkv_cache& c, int n_heads) {
+    const int group = n_heads / c.n_kv_heads;
+    return group < 16 ? group : 16;
+}
+int64_t most_tiles(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages) {
+    return n_seq * c.n_kv_heads * q_tiles_of(c, n_heads) * ((max_pages * c.page_size + kTile - 1) / kTile);
+}
+int workgroups(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages) {
+    const int64_t wgs = (most_tiles(c, n_heads, n_seq, max_pages) + kWaves * kMinTiles - 1) / (kWaves * kMinTiles);
+    return (int)(wgs < 1 ? 1 : wgs > kMaxWgs ? kMaxWgs : wgs);
 }
 
 }  // namespace
 
-size_t kv_attention_workspace(const riftkv_cache&, int, int64_t, int64_t) { return 256; }
+size_t kv_attention_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages) {
+    const size_t wgs = workgroups(c, n_heads, n_seq, max_pages);
+    const size_t joins = (wgs * sizeof(int4) + 255) / 256 * 256;
+    return joins + wgs * 2 * rows_of(c, n_heads) * (c.head_dim + 4) * sizeof(float);
+}
+
+bool kv_attention_counts(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages) {
+    return most_tiles(c, n_heads, n_seq, max_pages) < (1ll << 41);   // times 2,048 waves in 64 bits, a wave's share in 31
+}
 
 hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipStream_t st) {
-    const dim3 grid((unsigned)a.n_seq * (unsigned)a.n_heads);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64), 0, st, c, a); };
+    AttnParams p{};
+    p.q = a.q;
+    p.out = a.out;
+    p.ld_q = a.ld_q;
+    p.ld_out = a.ld_out;
+    p.k = static_cast<const unsigned char*>(c.k);
+    p.v = static_cast<const unsigned char*>(c.v);
+    p.ks = c.k_scale;
+    p.vs = c.v_scale;
+    p.table = a.table;
+    p.lens = a.lens;
+    p.status = a.status;
+    const int wgs = workgroups(c, a.n_heads, a.n_seq, a.max_pages);
+    p.joins = static_cast<int4*>(a.workspace);
+    p.slots = reinterpret_cast<float*>(static_cast<unsigned char*>(a.workspace) + (wgs * sizeof(int4) + 255) / 256 * 256);
+    p.n_seq = a.n_seq;
+    p.max_pages = a.max_pages;
+    p.n_pages = c.n_pages;
+    p.n_kv = c.n_kv_heads;
+    p.shift = 31 - __builtin_clz(c.page_size);
+    p.group = a.n_heads / c.n_kv_heads;
+    p.q_tiles = q_tiles_of(c, a.n_heads);
+    p.rows = rows_of(c, a.n_heads);
+    p.scale_log2 = a.scale * 1.4426950408889634f;
+    const size_t lds = 2 * kWaves * (size_t)p.rows * (c.head_dim + 4) * sizeof(float);
+    auto launch = [&](auto kernel, auto join) {
+        if (lds > 64 * 1024) {   // 16 query rows of 128 dimensions; the attribute is the current device's
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kThreads), lds, st, p);
+        hipLaunchKernelGGL(join, dim3(wgs), dim3(kJoinThreads), 0, st, p);
+        return hipGetLastError();
+    };
+    auto heads = [&](auto t, auto dt) {
+        using T = decltype(t);
+        if (c.head_dim == 128) return launch(attention_kernel<T, dt.value, 128>, join_kernel<T, 128>);
+        return launch(attention_kernel<T, dt.value, 64>, join_kernel<T, 64>);
+    };
+    auto types = [&](auto dt) {
+        if constexpr (dt.value != RIFTKV_F32)
+            if (a.bf16) return heads(bf16_t{}, dt);
+        return heads(float{}, dt);
+    };
     switch (c.dt) {
-        case RIFTKV_F32: launch(attention_kernel<float, RIFTKV_F32>); break;
-        case RIFTKV_BF16: a.bf16 ? launch(attention_kernel<bf16_t, RIFTKV_BF16>) : launch(attention_kernel<float, RIFTKV_BF16>); break;
-        case RIFTKV_FP8: a.bf16 ? launch(attention_kernel<bf16_t, RIFTKV_FP8>) : launch(attention_kernel<float, RIFTKV_FP8>); break;
-        case RIFTKV_INT8: a.bf16 ? launch(attention_kernel<bf16_t, RIFTKV_INT8>) : launch(attention_kernel<float, RIFTKV_INT8>); break;
+        case RIFTKV_F32: return types(std::integral_constant<riftkv_dtype, RIFTKV_F32>{});
+        case RIFTKV_BF16: return types(std::integral_constant<riftkv_dtype, RIFTKV_BF16>{});
+        case RIFTKV_FP8: return types(std::integral_constant<riftkv_dtype, RIFTKV_FP8>{});
+        case RIFTKV_INT8: return types(std::integral_constant<riftkv_dtype, RIFTKV_INT8>{});
     }
-    return hipGetLastError();
+    return hipErrorInvalidValue;
 }
 
 }  // namespace rift
