@@ -1,5 +1,7 @@
-// Rows of the paged key-value cache: rotary positions, rows into pages, rows out
-// of them.  A wave takes one head of one row.
+// Rows of the paged key-value cache: rotary positions, rows into pages, rows out of
+// them.  All three are bound by the bytes they move, so a lane moves 16 bytes of a row
+// at a time, several of them in flight, and what belongs to a whole row (its sines,
+// its place in the pages) is worked out once by the workgroup and passed in LDS.
 #include <type_traits>
 
 #include "kv_device.h"
@@ -7,6 +9,8 @@
 namespace rift {
 
 namespace {
+
+constexpr int kThreads = 256;
 
 template <typename T>
 __device__ __forceinline__ float load_f32(const void* p, size_t i) {
@@ -19,6 +23,47 @@ __device__ __forceinline__ void store_f32(void* p, size_t i, float x) {
     else static_cast<float*>(p)[i] = x;
 }
 
+// 8 elements of a row, 16-byte aligned.
+template <typename T>
+struct Eight {
+    u32x4_t w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Eight<T> load_eight(const void* p, size_t i) {
+    Eight<T> x;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) x.w[j] = reinterpret_cast<const u32x4_t*>(static_cast<const T*>(p) + i)[j];
+    return x;
+}
+template <typename T>
+__device__ __forceinline__ void widen_eight(const Eight<T>& x, float (&f)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 2) {
+            f[2 * j] = bf16_lo(x.w[0][j]);
+            f[2 * j + 1] = bf16_hi(x.w[0][j]);
+        } else {
+            f[j] = __uint_as_float(x.w[0][j]);
+            f[4 + j] = __uint_as_float(x.w[1][j]);
+        }
+    }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return (uint32_t)round_bf16(a) | (uint32_t)round_bf16(b) << 16;
+}
+template <typename T>
+__device__ __forceinline__ void store_eight(void* p, size_t i, const float (&f)[8]) {
+    u32x4_t* q = reinterpret_cast<u32x4_t*>(static_cast<T*>(p) + i);
+    if constexpr (sizeof(T) == 2) {
+        *q = u32x4_t{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+    } else {
+        q[0] = u32x4_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+        q[1] = u32x4_t{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])};
+    }
+}
+
+// ---------------------------------------------------------------- positions
+
 // The angle in turns, reduced to [-1/2, 1/2] in float64: float32 holds it and its
 // sine and cosine to their last bits however far the position is.
 __device__ __forceinline__ float2 rope_turn(int position, double turns, float magnitude) {
@@ -28,10 +73,11 @@ __device__ __forceinline__ float2 rope_turn(int position, double turns, float ma
     return make_float2(c * magnitude, s * magnitude);
 }
 
+// Any sizes, strides and alignment: a wave takes one head of one row.
 template <typename T>
 __global__ void __launch_bounds__(64)
-rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int head_dim, int rotary_dim, int interleaved,
-            RopeFreqs freqs, float magnitude) {
+rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int head_dim, int rotary_dim, int interleaved,
+                RopeFreqs freqs, float magnitude) {
     const int heads = q.n + k.n;
     const int row = blockIdx.x / heads, h = blockIdx.x - row * heads;
     const RopeRows& r = h < q.n ? q : k;
@@ -48,97 +94,285 @@ rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int head_
     for (int j = rotary_dim + threadIdx.x; j < head_dim; j += 64) store_f32<T>(r.y, y0 + j, load_f32<T>(r.x, x0 + j));
 }
 
-// Index of (page, head, row in page) among the pages' rows; -1 where the row is
+// Eights of elements: a workgroup takes `per` heads of `tile` rows.  A head's items are,
+// in the half layout, rotary_dim / 16 pairs of eights, then the eights that are
+// copied; interleaved, head_dim / 8 eights of four pairs each or copied.
+template <typename T, bool INTERLEAVED>
+__global__ void __launch_bounds__(kThreads)
+rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int rows, int tile, int per, int head_dim,
+            int rotary_dim, RopeFreqs freqs, float magnitude) {
+    extern __shared__ __align__(16) float2 turns[];   // [tile][rotary_dim / 2]
+    const int row0 = blockIdx.x * tile, n_rows = min(tile, rows - row0);
+    const int heads = q.n + k.n, h0 = blockIdx.y * per, n_heads = min(per, heads - h0);
+    const int half = rotary_dim / 2;
+    const int turned = INTERLEAVED ? rotary_dim / 8 : rotary_dim / 16, items = turned + (head_dim - rotary_dim) / 8;
+    for (int i = threadIdx.x; i < n_rows * half; i += kThreads) {
+        const int r = i / half, j = i - r * half;
+        turns[i] = rope_turn(positions[row0 + r], freqs.f[j], magnitude);
+    }
+    __syncthreads();
+    // item v of head h of row r
+    int v = threadIdx.x % items, h = threadIdx.x / items;
+    int r = h / n_heads;
+    h -= r * n_heads;
+    const int dv = kThreads % items, dh = kThreads / items;
+    while (r < n_rows) {
+        const int head = h0 + h;
+        const bool is_q = head < q.n;
+        const void* x = is_q ? q.x : k.x;
+        void* y = is_q ? q.y : k.y;
+        const size_t hoff = (size_t)(is_q ? head : head - q.n) * head_dim;
+        const size_t x0 = (size_t)(row0 + r) * (is_q ? q.ld_x : k.ld_x) + hoff;
+        const size_t y0 = (size_t)(row0 + r) * (is_q ? q.ld_y : k.ld_y) + hoff;
+        const float2* cs = turns + r * half;
+        if (v >= turned) {
+            const int e = rotary_dim + 8 * (v - turned);
+            float f[8];
+            widen_eight<T>(load_eight<T>(x, x0 + e), f);
+            store_eight<T>(y, y0 + e, f);
+        } else if constexpr (INTERLEAVED) {
+            float f[8];
+            widen_eight<T>(load_eight<T>(x, x0 + 8 * v), f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 o = rotate_pair(f[2 * j], f[2 * j + 1], cs[4 * v + j]);
+                f[2 * j] = o.x;
+                f[2 * j + 1] = o.y;
+            }
+            store_eight<T>(y, y0 + 8 * v, f);
+        } else {
+            float a[8], b[8];
+            const Eight<T> xa = load_eight<T>(x, x0 + 8 * v), xb = load_eight<T>(x, x0 + half + 8 * v);
+            widen_eight<T>(xa, a);
+            widen_eight<T>(xb, b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 o = rotate_pair(a[j], b[j], cs[8 * v + j]);
+                a[j] = o.x;
+                b[j] = o.y;
+            }
+            store_eight<T>(y, y0 + 8 * v, a);
+            store_eight<T>(y, y0 + half + 8 * v, b);
+        }
+        v += dv;
+        h += dh;
+        if (v >= items) {
+            v -= items;
+            ++h;
+        }
+        while (h >= n_heads) {
+            h -= n_heads;
+            ++r;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- pages
+
+// Index of (page, head 0, row in page) among the pages' rows; -1 where the row is
 // skipped, or is out of range and the status set.
-__device__ __forceinline__ int64_t page_row(const KvPlaces& at, int row, int head, int n_pages, int page_size, int n_kv) {
+__device__ __forceinline__ int64_t page_row(const KvPlaces& at, int row, int n_pages, int shift, int n_kv) {
     const int seq = at.seq_ids ? at.seq_ids[row] : row, pos = at.positions[row];
     if (seq < 0 || pos < 0) return -1;
-    const int shift = 31 - __clz(page_size);
     int page = -1;
     if (seq < at.n_seq && (pos >> shift) < at.max_pages) page = at.table[(size_t)seq * at.max_pages + (pos >> shift)];
     if (page < 0 || page >= n_pages) {
         *at.status = RIFT_ERR_SHAPE;
         return -1;
     }
-    return (((int64_t)page * n_kv + head) << shift) + (pos & (page_size - 1));
+    return (((int64_t)page * n_kv) << shift) + (pos & ((1 << shift) - 1));
 }
 
-template <typename T, riftkv_dtype DT, int HD>
-__device__ void write_row(const void* x, size_t x0, void* pages, uint8_t* scales, int64_t to, int lane) {
-    constexpr int E = HD / 64;
-    float f[E];
-    for (int e = 0; e < E; ++e) f[e] = load_f32<T>(x, x0 + lane + 64 * e);
-    const size_t y0 = (size_t)to * HD;
-    if constexpr (DT == RIFTKV_F32 || DT == RIFTKV_BF16) {
-        for (int e = 0; e < E; ++e) {
-            if constexpr (DT == RIFTKV_F32) static_cast<float*>(pages)[y0 + lane + 64 * e] = f[e];
-            else static_cast<bf16_t*>(pages)[y0 + lane + 64 * e] = round_bf16(f[e]);
+// Maximum over the G (8 or 16) lanes of a row.
+template <int G>
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, false));    // quad_perm 1, 0, 3, 2
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, false));    // quad_perm 2, 3, 0, 1
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xf, 0xf, false));   // row_half_mirror
+    if constexpr (G == 16) x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xf, 0xf, false));   // row_mirror
+    return x;
+}
+
+// 8 values as codes: y = x up is exact, so that one addition rounds it to nearest even.
+template <riftkv_dtype DT>
+__device__ __forceinline__ uint2 codes_of(const float (&f)[8], float up) {
+    uint32_t w[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float* x = f + 4 * j;
+        if constexpr (DT == RIFTKV_FP8) {
+            int c = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * up, x[1] * up, 0, false);
+            c = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * up, x[3] * up, c, true);
+            w[j] = (uint32_t)c;
+        } else {
+            constexpr float kOne = 12582912.f;   // 1.5 2^23: its last bit is worth 1
+            uint32_t b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(fmaf(x[e], up, kOne));   // the low byte is the code
+            const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000C0Cu);
+            w[j] = lo | hi;
         }
-    } else {
-        uint32_t most = 0;
-        for (int e = 0; e < E; ++e) most = max(most, __float_as_uint(f[e]) & 0x7FFFFFFFu);
-        for (int s = 32; s >= 1; s >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, s));
-        const bool bad = most >= kNotFinite;
-        const uint32_t b = bad ? 255u : scale_byte<DT>(most);
-        const float up = bad ? 0.f : __uint_as_float((254u - b) << 23);
-        for (int e = 0; e < E; ++e) {
-            const float y = bad ? 0.f : f[e] * up;
-            uint8_t code;
-            if constexpr (DT == RIFTKV_FP8) code = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
-            else code = (uint8_t)(int)rintf(y);
-            static_cast<uint8_t*>(pages)[y0 + lane + 64 * e] = code;
+    }
+    return make_uint2(w[0], w[1]);
+}
+template <riftkv_dtype DT>
+__device__ __forceinline__ void values_of(uint2 c, float scale, float (&f)[8]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t w = j ? c.y : c.x;
+        float* x = f + 4 * j;
+        if constexpr (DT == RIFTKV_FP8) {
+            const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+            x[0] = a[0] * scale;
+            x[1] = a[1] * scale;
+            x[2] = b[0] * scale;
+            x[3] = b[1] * scale;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)(w >> (8 * e)) * scale;
         }
-        if (lane == 0) scales[to] = (uint8_t)b;
     }
 }
 
-template <typename T, riftkv_dtype DT, int HD>
-__device__ void read_row(void* y, size_t y0, const void* pages, const uint8_t* scales, int64_t from, int lane) {
-    const size_t x0 = (size_t)from * HD;
-    for (int e = lane; e < HD; e += 64) {
-        float f;
-        if constexpr (DT == RIFTKV_F32) f = static_cast<const float*>(pages)[x0 + e];
-        else if constexpr (DT == RIFTKV_BF16) f = bf16_to_f32(static_cast<const bf16_t*>(pages)[x0 + e]);
-        else {
-            const uint32_t code = static_cast<const uint8_t*>(pages)[x0 + e];
-            if constexpr (DT == RIFTKV_FP8) f = __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
-            else f = (float)(int8_t)code;
-            f *= scale_of(scales[from]);
+// Rows move as eights: HD / 8 lanes a row of a head, the rows of a tile under each other
+// in a wave, which then writes (reads) several rows of a page in sequence.
+struct MoveParams {
+    unsigned char* pages[2];     // keys, values
+    uint8_t* scales[2];
+    void* rows_of[2];
+    int64_t ld[2];
+    int n_pages, shift, n_kv;
+    int tile_log2, per;          // rows and heads of a workgroup
+    KvPlaces at;
+};
+constexpr int kTileRows = 16, kUnroll = 4;
+
+template <typename T, riftkv_dtype DT, int HD, bool WRITE>
+__global__ void __launch_bounds__(kThreads)
+move_kernel(MoveParams p) {
+    constexpr int G = HD / 8, E = DT == RIFTKV_F32 ? 4 : DT == RIFTKV_BF16 ? 2 : 1;
+    constexpr bool SCALED = E == 1;
+    __shared__ int64_t places[kTileRows];
+    const int which = blockIdx.z, row0 = blockIdx.x << p.tile_log2, h0 = blockIdx.y * p.per;
+    const int n_heads = min(p.per, p.n_kv - h0);
+    unsigned char* pages = p.pages[which];
+    uint8_t* scales = p.scales[which];
+    void* rows = p.rows_of[which];
+    const int64_t ld = p.ld[which];
+    const int items = n_heads << p.tile_log2;            // (head, row) pairs, the row running fastest
+    const int lane = threadIdx.x % G, first = threadIdx.x / G;
+    constexpr int STEP = kThreads / G;
+    const int tile_mask = (1 << p.tile_log2) - 1;
+    auto row_at = [&](int i) { return row0 + (i & tile_mask); };
+    auto rows_index = [&](int i) { return (size_t)row_at(i) * ld + (size_t)(h0 + (i >> p.tile_log2)) * HD + 8 * lane; };
+    Eight<T> x[kUnroll];
+    auto load_rows = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int i = i0 + u * STEP;
+            if (i < items && row_at(i) < p.at.rows) x[u] = load_eight<T>(rows, rows_index(i));
         }
-        store_f32<T>(y, y0 + e, f);
+    };
+    if constexpr (WRITE) load_rows(first);
+    if (threadIdx.x <= tile_mask) {
+        const int row = row0 + threadIdx.x;
+        places[threadIdx.x] = row < p.at.rows ? page_row(p.at, row, p.n_pages, p.shift, p.n_kv) : -1;
+    }
+    __syncthreads();
+    for (int i0 = first; i0 < items; i0 += kUnroll * STEP) {
+        if constexpr (WRITE) {
+            if (i0 != first) load_rows(i0);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = i0 + u * STEP;
+                const int64_t place = i < items ? places[i & tile_mask] : -1;
+                if (place < 0) continue;      // all lanes of a row alike
+                const size_t to = (size_t)place + ((size_t)(h0 + (i >> p.tile_log2)) << p.shift);
+                float f[8];
+                widen_eight<T>(x[u], f);
+                if constexpr (DT == RIFTKV_F32) store_eight<float>(pages, to * HD + 8 * lane, f);
+                else if constexpr (DT == RIFTKV_BF16) {
+                    if constexpr (sizeof(T) == 2) reinterpret_cast<u32x4_t*>(pages)[(to * HD >> 3) + lane] = x[u].w[0];
+                    else store_eight<bf16_t>(pages, to * HD + 8 * lane, f);
+                } else {
+                    uint32_t most = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+                    most = row_max<G>(most);
+                    const bool bad = most >= kNotFinite;
+                    const uint32_t b = bad ? 255u : scale_byte<DT>(most);
+                    const uint2 c = codes_of<DT>(f, __uint_as_float((254u - b) << 23));
+                    reinterpret_cast<uint2*>(pages)[(to * HD >> 3) + lane] = bad ? make_uint2(0, 0) : c;
+                    if (lane == 0) scales[to] = (uint8_t)b;
+                }
+            }
+        } else {
+            Eight<std::conditional_t<DT == RIFTKV_F32, float, bf16_t>> y[kUnroll];
+            uint2 c[kUnroll];
+            uint32_t b[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = i0 + u * STEP;
+                const int64_t place = i < items ? places[i & tile_mask] : -1;
+                if (place < 0) continue;
+                const size_t from = (size_t)place + ((size_t)(h0 + (i >> p.tile_log2)) << p.shift);
+                if constexpr (SCALED) {
+                    c[u] = reinterpret_cast<const uint2*>(pages)[(from * HD >> 3) + lane];
+                    b[u] = scales[from];
+                } else {
+                    y[u] = load_eight<std::conditional_t<DT == RIFTKV_F32, float, bf16_t>>(pages, from * HD + 8 * lane);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = i0 + u * STEP;
+                if (i >= items || places[i & tile_mask] < 0) continue;
+                float f[8];
+                if constexpr (SCALED) values_of<DT>(c[u], scale_of(b[u]), f);
+                else widen_eight(y[u], f);
+                if constexpr (DT == RIFTKV_BF16 && sizeof(T) == 2) reinterpret_cast<u32x4_t*>(rows)[rows_index(i) >> 3] = y[u].w[0];
+                else store_eight<T>(rows, rows_index(i), f);
+            }
+        }
     }
 }
 
-template <typename T, riftkv_dtype DT, int HD>
-__global__ void __launch_bounds__(64)
-write_kernel(riftkv_cache c, const void* k, int64_t ld_k, const void* v, int64_t ld_v, KvPlaces at) {
-    const int row = blockIdx.x / c.n_kv_heads, h = blockIdx.x - row * c.n_kv_heads;
-    const int64_t to = page_row(at, row, h, c.n_pages, c.page_size, c.n_kv_heads);
-    if (to < 0) return;
-    write_row<T, DT, HD>(k, (size_t)row * ld_k + h * HD, c.k, c.k_scale, to, threadIdx.x);
-    write_row<T, DT, HD>(v, (size_t)row * ld_v + h * HD, c.v, c.v_scale, to, threadIdx.x);
-}
-
-template <typename T, riftkv_dtype DT, int HD>
-__global__ void __launch_bounds__(64)
-read_kernel(riftkv_cache c, void* k, int64_t ld_k, void* v, int64_t ld_v, KvPlaces at) {
-    const int row = blockIdx.x / c.n_kv_heads, h = blockIdx.x - row * c.n_kv_heads;
-    const int64_t from = page_row(at, row, h, c.n_pages, c.page_size, c.n_kv_heads);
-    if (from < 0) return;
-    read_row<T, DT, HD>(k, (size_t)row * ld_k + h * HD, c.k, c.k_scale, from, threadIdx.x);
-    read_row<T, DT, HD>(v, (size_t)row * ld_v + h * HD, c.v, c.v_scale, from, threadIdx.x);
-}
-
-// f<T, DT, HD>() for the types of a call; the C ABI has refused the others.
-template <typename F>
-hipError_t with_types(bool bf16, riftkv_dtype dt, int hd, F f) {
-    auto heads = [&](auto t, auto d) {
-        if (hd == 128) f(t, d, std::integral_constant<int, 128>{});
-        else f(t, d, std::integral_constant<int, 64>{});
+template <bool WRITE>
+hipError_t launch_move(const riftkv_cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v, bool bf16,
+                       const KvPlaces& at, hipStream_t st) {
+    MoveParams p{};
+    p.pages[0] = static_cast<unsigned char*>(c.k);
+    p.pages[1] = static_cast<unsigned char*>(c.v);
+    p.scales[0] = c.k_scale;
+    p.scales[1] = c.v_scale;
+    p.rows_of[0] = const_cast<void*>(k);
+    p.rows_of[1] = const_cast<void*>(v);
+    p.ld[0] = ld_k;
+    p.ld[1] = ld_v;
+    p.n_pages = c.n_pages;
+    p.shift = 31 - __builtin_clz(c.page_size);
+    p.n_kv = c.n_kv_heads;
+    p.at = at;
+    // 16 rows of 8 heads a workgroup; fewer rows where that leaves CUs without work
+    p.per = c.n_kv_heads < 8 ? c.n_kv_heads : 8;
+    const unsigned splits = (c.n_kv_heads + p.per - 1) / p.per;
+    p.tile_log2 = 4;
+    while (p.tile_log2 > 0 && (int64_t)(at.rows >> p.tile_log2) * splits * 2 < 512) --p.tile_log2;
+    const dim3 grid((unsigned)((at.rows + (1 << p.tile_log2) - 1) >> p.tile_log2), splits, 2);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, p);
         return hipGetLastError();
     };
-    auto types = [&](auto d) { return bf16 ? heads(bf16_t{}, d) : heads(float{}, d); };
-    switch (dt) {
+    auto heads = [&](auto t, auto dt) {
+        using U = decltype(t);
+        return c.head_dim == 128 ? launch(move_kernel<U, dt.value, 128, WRITE>) : launch(move_kernel<U, dt.value, 64, WRITE>);
+    };
+    auto types = [&](auto dt) {
+        if constexpr (!(WRITE && dt.value == RIFTKV_F32))
+            if (bf16) return heads(bf16_t{}, dt);
+        return heads(float{}, dt);
+    };
+    switch (c.dt) {
         case RIFTKV_F32: return types(std::integral_constant<riftkv_dtype, RIFTKV_F32>{});
         case RIFTKV_BF16: return types(std::integral_constant<riftkv_dtype, RIFTKV_BF16>{});
         case RIFTKV_FP8: return types(std::integral_constant<riftkv_dtype, RIFTKV_FP8>{});
@@ -151,30 +385,45 @@ hipError_t with_types(bool bf16, riftkv_dtype dt, int hd, F f) {
 
 hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, int rows, int head_dim,
                           int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st) {
-    const dim3 grid((unsigned)rows * (unsigned)(q.n + k.n));
+    const int heads = q.n + k.n;
+    auto aligned = [&](const RopeRows& r) {   // 16-byte eights
+        const int64_t per = bf16 ? 8 : 4;
+        return r.n == 0 || (((reinterpret_cast<uintptr_t>(r.x) | reinterpret_cast<uintptr_t>(r.y)) & 15) == 0 &&
+                            r.ld_x % per == 0 && r.ld_y % per == 0);
+    };
+    if (head_dim % 8 != 0 || rotary_dim % 16 != 0 || !aligned(q) || !aligned(k)) {
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)rows * (unsigned)heads), dim3(64), 0, st, q, k, positions, head_dim,
+                               rotary_dim, interleaved ? 1 : 0, freqs, magnitude);
+        };
+        if (bf16) launch(rope_any_kernel<bf16_t>);
+        else launch(rope_any_kernel<float>);
+        return hipGetLastError();
+    }
+    // 4 rows of all heads a workgroup, so that the sines are worked out once a row; fewer
+    // rows, then heads, where that leaves CUs without work
+    int tile = 4, per = heads;
+    while (tile > 1 && rows / tile < 1024) tile /= 2;
+    while (per > 4 && (int64_t)rows * ((heads + per - 1) / per) < 512) per = (per + 1) / 2;
+    const dim3 grid((unsigned)((rows + tile - 1) / tile), (unsigned)((heads + per - 1) / per));
+    const size_t lds = (size_t)tile * (rotary_dim / 2) * sizeof(float2);
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(64), 0, st, q, k, positions, head_dim, rotary_dim, interleaved ? 1 : 0,
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, q, k, positions, rows, tile, per, head_dim, rotary_dim,
                            freqs, magnitude);
     };
-    if (bf16) launch(rope_kernel<bf16_t>);
-    else launch(rope_kernel<float>);
+    if (bf16) interleaved ? launch(rope_kernel<bf16_t, true>) : launch(rope_kernel<bf16_t, false>);
+    else interleaved ? launch(rope_kernel<float, true>) : launch(rope_kernel<float, false>);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_write(const riftkv_cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v, bool bf16,
                            const KvPlaces& at, hipStream_t st) {
-    const dim3 grid((unsigned)at.rows * (unsigned)c.n_kv_heads);
-    return with_types(bf16, c.dt, c.head_dim, [&](auto t, auto dt, auto hd) {
-        hipLaunchKernelGGL((write_kernel<decltype(t), dt.value, hd.value>), grid, dim3(64), 0, st, c, k, ld_k, v, ld_v, at);
-    });
+    return launch_move<true>(c, k, ld_k, v, ld_v, bf16, at, st);
 }
 
 hipError_t launch_kv_read(const riftkv_cache& c, void* k, int64_t ld_k, void* v, int64_t ld_v, bool bf16,
                           const KvPlaces& at, hipStream_t st) {
-    const dim3 grid((unsigned)at.rows * (unsigned)c.n_kv_heads);
-    return with_types(bf16, c.dt, c.head_dim, [&](auto t, auto dt, auto hd) {
-        hipLaunchKernelGGL((read_kernel<decltype(t), dt.value, hd.value>), grid, dim3(64), 0, st, c, k, ld_k, v, ld_v, at);
-    });
+    return launch_move<false>(c, k, ld_k, v, ld_v, bf16, at, st);
 }
 
 }  // namespace rift
