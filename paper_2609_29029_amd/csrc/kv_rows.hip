@@ -12,6 +12,8 @@ namespace {
 
 constexpr int kThreads = 256;
 
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
 template <typename T>
 __device__ __forceinline__ float load_f32(const void* p, size_t i) {
     if constexpr (sizeof(T) == 2) return bf16_to_f32(static_cast<const bf16_t*>(p)[i]);
@@ -23,7 +25,8 @@ __device__ __forceinline__ void store_f32(void* p, size_t i, float x) {
     else static_cast<float*>(p)[i] = x;
 }
 
-// 8 elements of a row, 16-byte aligned.
+// 8 elements of a row, 16-byte aligned; read once, so past the caches (2 to 4% of every
+// large call).
 template <typename T>
 struct Eight {
     u32x4_t w[sizeof(T) / 2];
@@ -32,7 +35,8 @@ template <typename T>
 __device__ __forceinline__ Eight<T> load_eight(const void* p, size_t i) {
     Eight<T> x;
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j) x.w[j] = reinterpret_cast<const u32x4_t*>(static_cast<const T*>(p) + i)[j];
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+        x.w[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(static_cast<const T*>(p) + i) + j);
     return x;
 }
 template <typename T>
@@ -216,10 +220,10 @@ __device__ __forceinline__ uint2 codes_of(const float (&f)[8], float up) {
     return make_uint2(w[0], w[1]);
 }
 template <riftkv_dtype DT>
-__device__ __forceinline__ void values_of(uint2 c, float scale, float (&f)[8]) {
+__device__ __forceinline__ void values_of(u32x2_t c, float scale, float (&f)[8]) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const uint32_t w = j ? c.y : c.x;
+        const uint32_t w = c[j];
         float* x = f + 4 * j;
         if constexpr (DT == RIFTKV_FP8) {
             const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
@@ -308,7 +312,7 @@ move_kernel(MoveParams p) {
             }
         } else {
             Eight<std::conditional_t<DT == RIFTKV_F32, float, bf16_t>> y[kUnroll];
-            uint2 c[kUnroll];
+            u32x2_t c[kUnroll];
             uint32_t b[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
@@ -317,7 +321,7 @@ move_kernel(MoveParams p) {
                 if (place < 0) continue;
                 const size_t from = (size_t)place + ((size_t)(h0 + (i >> p.tile_log2)) << p.shift);
                 if constexpr (SCALED) {
-                    c[u] = reinterpret_cast<const uint2*>(pages)[(from * HD >> 3) + lane];
+                    c[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(pages) + (from * HD >> 3) + lane);
                     b[u] = scales[from];
                 } else {
                     y[u] = load_eight<std::conditional_t<DT == RIFTKV_F32, float, bf16_t>>(pages, from * HD + 8 * lane);
@@ -353,10 +357,13 @@ hipError_t launch_move(const riftkv_cache& c, const void* k, int64_t ld_k, const
     p.shift = 31 - __builtin_clz(c.page_size);
     p.n_kv = c.n_kv_heads;
     p.at = at;
-    // 16 rows of 8 heads a workgroup; fewer rows where that leaves CUs without work
-    p.per = c.n_kv_heads < 8 ? c.n_kv_heads : 8;
+    // 8 rows of 16 heads a workgroup that writes, 16 of 8 one that reads (the scene's 32,987 rows of 32 heads
+    // into e4m3 pages: 187 us and with 16 of 8 218; 120,001 rows of 8 heads out of int8 ones: 149 us
+    // and with 8 of 8 160); fewer rows where that leaves CUs without work
+    const int most = WRITE ? 16 : 8;
+    p.per = c.n_kv_heads < most ? c.n_kv_heads : most;
     const unsigned splits = (c.n_kv_heads + p.per - 1) / p.per;
-    p.tile_log2 = 4;
+    p.tile_log2 = WRITE ? 3 : 4;
     while (p.tile_log2 > 0 && (int64_t)(at.rows >> p.tile_log2) * splits * 2 < 512) --p.tile_log2;
     const dim3 grid((unsigned)((at.rows + (1 << p.tile_log2) - 1) >> p.tile_log2), splits, 2);
     auto launch = [&](auto kernel) {
