@@ -131,7 +131,13 @@ __global__ void __launch_bounds__(kThreads, 2)
 attention_kernel(AttnParams p) {
     constexpr int B = DT == RIFTKV_F32 ? 4 : DT == RIFTKV_BF16 ? 2 : 1;   // bytes a value
     constexpr bool SCALED = B == 1, F32 = DT == RIFTKV_F32;
-    constexpr int KL = HD * B / 64;          // 16-byte loads of a lane for 16 keys
+    // A load of keys takes E 64-byte pieces of 16 / E rows (whole 128-byte lines), so that
+    // a row of the first product's left operand is one piece of one token: it meets each piece of
+    // the query, in an accumulator of its own, and a score is the sum of what belongs
+    // together.  Rows of 64 bytes, and float32 ones (whose products are not idle): E = 1.
+    constexpr int E = F32 || HD * B == 64 ? 1 : 2;
+    constexpr int KF = HD * B / (64 * E);    // loads of a lane for 16 / E keys
+    constexpr int I = 4 / E;                 // a lane's scores of those
     constexpr int VW = HD * B / 64;          // words of a lane of one value row
     constexpr int C = HD / 16;               // columns of a lane of one value row
     constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
@@ -231,8 +237,10 @@ attention_kernel(AttnParams p) {
             const int t0 = c.tile * kTile, t1 = t0 + 16 < c.len ? t0 + 16 : t0;
             return Pages{row[t0 >> p.shift], row[t1 >> p.shift]};
         };
-        uint32_t kr[2][KL][4], vr[2][4][VW], ksc[2], vsc[2];
-        const unsigned k_lane = n * HD * B + g * 16, v_lane = g * 4 * HD * B + n * VW * 4;
+        uint32_t kr[2][E][KF][4], vr[2][4][VW], ksc[2], vsc[2];
+        // load x of the E takes tokens 4 r + I x + i (r = 0..3, i < I): lane (n, g) the piece n mod E of row n / E
+        const unsigned k_lane = (E == 1 ? n : 4 * (n >> 2) + ((n >> 1) & 1)) * HD * B + (n % E) * 64 + g * 16;
+        const unsigned v_lane = g * 4 * HD * B + n * VW * 4;
         // first row of a half's keys and values among the pages' rows
         auto row_of = [&](const Place& c, int page, int h) __attribute__((always_inline)) {
             page = (unsigned)page < (unsigned)p.n_pages ? page : 0;
@@ -244,7 +252,10 @@ attention_kernel(AttnParams p) {
             for (int h = 0; h < 2; ++h) {
                 const size_t r = row_of(c, h ? pg.b : pg.a, h);
 #pragma unroll
-                for (int i = 0; i < KL; ++i) load_words<4>(kr[h][i], p.k + r * (HD * B) + off + 64 * i);
+                for (int x = 0; x < E; ++x)
+#pragma unroll
+                    for (int f = 0; f < KF; ++f)
+                        load_words<4>(kr[h][x][f], p.k + r * (HD * B) + off + x * I * HD * B + 64 * E * f);
                 if constexpr (SCALED) ksc[h] = *reinterpret_cast<const uint32_t*>(p.ks + r + 4 * g);
             }
         };
@@ -318,33 +329,44 @@ attention_kernel(AttnParams p) {
             float s[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-                if constexpr (F32) {
 #pragma unroll
-                    for (int i = 0; i < KL; ++i)
+                for (int x = 0; x < E; ++x) {
+                    f32x4_t acc[E];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[h][i][e]), qs[4 * i + e], acc, 0, 0, 0);
-                } else {
+                    for (int e = 0; e < E; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int f = 0; f < HD / 32; ++f) {
-                        u32x4_t kw;
-                        if constexpr (SCALED) {
-                            const uint32_t w0 = kr[h][f >> 1][2 * (f & 1)], w1 = kr[h][f >> 1][2 * (f & 1) + 1];
-                            kw = u32x4_t{widen<DT, false>(w0), widen<DT, true>(w0), widen<DT, false>(w1), widen<DT, true>(w1)};
+                    for (int f = 0; f < KF; ++f) {
+                        const uint32_t(&w)[4] = kr[h][x][f];
+                        if constexpr (F32) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                acc[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[j]), qs[4 * f + j], acc[0], 0, 0, 0);
                         } else {
-                            kw = u32x4_t{kr[h][f][0], kr[h][f][1], kr[h][f][2], kr[h][f][3]};
+#pragma unroll
+                            for (int y = 0; y < (SCALED ? 2 : 1); ++y) {   // 16 bytes: 8 or 16 values
+                                u32x4_t kw;
+                                if constexpr (SCALED)
+                                    kw = u32x4_t{widen<DT, false>(w[2 * y]), widen<DT, true>(w[2 * y]), widen<DT, false>(w[2 * y + 1]),
+                                                 widen<DT, true>(w[2 * y + 1])};
+                                else
+                                    kw = u32x4_t{w[0], w[1], w[2], w[3]};
+#pragma unroll
+                                for (int e = 0; e < E; ++e)
+#pragma unroll
+                                    for (int i = 0; i < NQ; ++i)
+                                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                            __builtin_bit_cast(bf16x8_t, kw), qf[i][SCALED ? 2 * (f * E + e) + y : f * E + e], acc[e], 0, 0, 0);
+                            }
                         }
-#pragma unroll
-                        for (int i = 0; i < NQ; ++i)
-                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kw), qf[i][f], acc, 0, 0, 0);
                     }
-                }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = acc[i];
-                    if constexpr (SCALED) x *= scale_of((ksc[h] >> (8 * i)) & 0xFFu);
-                    s[4 * h + i] = x * p.scale_log2;
+                    for (int i = 0; i < I; ++i) {
+                        float a = acc[0][i * E];
+                        if constexpr (E == 2) a += acc[1][i * E + 1];
+                        const int j = 4 * h + I * x + i;
+                        if constexpr (SCALED) a *= scale_of((ksc[h] >> (8 * (j & 3))) & 0xFFu);
+                        s[j] = a * p.scale_log2;
+                    }
                 }
             }
             load_k(nxt, nxt_pages, live);
