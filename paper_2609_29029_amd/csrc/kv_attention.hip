@@ -1,15 +1,16 @@
 // One query token of every sequence over its paged keys and values, split over the
 // length and joined.
 //
-//   attention_kernel   The tiles (32 tokens of one sequence and head group) of all
-//                      sequences, one after the other, are dealt out evenly to the
+//   attention_kernel   Short heads: a workgroup takes one whole, its waves a share each.
+//                      Otherwise the tiles (32 tokens of one sequence and head group) of
+//                      all sequences, one after the other, are dealt out evenly to the
 //                      waves, in runs: however uneven the lengths, waves finish
 //                      together, and a wave writes at most two results of parts.
 //                      Heads a wave finishes go straight to the output, the parts at
 //                      its ends meet in LDS, and what a workgroup holds only a part
 //                      of goes to its two slots of the workspace.
-//   join_kernel        the parts of heads that several workgroups share; sequences
-//                      without tokens.
+//   join_kernel        after a split: the parts of heads that several workgroups share;
+//                      sequences without tokens.
 //
 // A head group is up to 16 query heads of one key head.  With the tile's tokens as rows,
 // S^T = K Q^T leaves a lane the scores of one query and 8 tokens; they are the lane's
@@ -31,9 +32,8 @@ namespace rift {
 namespace {
 
 constexpr int kTile = 32;                 // tokens of a tile
-constexpr int kWaves = 4;                 // of a workgroup
-constexpr int kThreads = 64 * kWaves;
-constexpr int kMinTiles = 2;              // a wave's share, where there are fewer than waves to share them
+constexpr int kSplitWaves = 4;            // of a workgroup, where heads are split over workgroups
+constexpr int kFewSeqs = 256;             // sequences whose lengths a wave holds in registers
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
@@ -49,6 +49,7 @@ struct AttnParams {
     float* slots;          // [wgs][2][rows][HD + 4]: weighted values, max, sum
     int4* joins;           // [wgs]: sequence, head group and last workgroup of a head begun here
     int n_seq, max_pages, n_pages, n_kv, shift, group, q_tiles, rows;
+    int few;               // at most kFewSeqs sequences, and 31 bits hold their tiles
     float scale_log2;
 };
 
@@ -65,6 +66,33 @@ __device__ __forceinline__ int length_of(int len, int max_pages, int shift) {
 }
 
 __device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// a / b; most operands have 32 bits, and 64-bit division is long.
+__device__ __forceinline__ unsigned long long quotient(unsigned long long a, unsigned long long b) {
+    return ((a | b) >> 32) == 0 ? (unsigned)a / (unsigned)b : a / b;
+}
+
+// Inclusive sums over the wave.
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast 15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast 31 into rows 2 and 3
+    return x;
+}
+
+// How N tiles are dealt to W waves (W <= N): wave w's run begins at w q + min(w, r).
+struct Deal {
+    unsigned long long q, r;
+    __device__ __forceinline__ Deal(unsigned long long N, unsigned W) : q(quotient(N, W)), r(N - q * W) {}
+    __device__ __forceinline__ unsigned long long first(unsigned w) const { return w * q + (w < r ? w : r); }
+    __device__ __forceinline__ int owner(unsigned long long tile) const {
+        const unsigned long long longer = r * (q + 1);
+        return (int)(tile < longer ? quotient(tile, q + 1) : r + quotient(tile - longer, q));
+    }
+};
 
 // Maximum and sum over the four lanes that hold a query's tokens (16 lanes apart).
 __device__ __forceinline__ float quad_max(float x) {
@@ -125,10 +153,31 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char
     }
 }
 
-// T: type of queries and outputs.
-template <typename T, riftkv_dtype DT, int HD>
-__global__ void __launch_bounds__(kThreads, 2)
+// Output of a sequence without tokens, or of a length out of range: head group hq, or all (-1).
+template <typename T>
+__device__ void fill_heads(const AttnParams& p, int seq, int given, int hq, int hd, int tid, int threads) {
+    const bool bad = given != 0;
+    if (bad && tid == 0) *p.status = RIFT_ERR_SHAPE;
+    int h0 = 0, heads = p.n_kv * p.group;
+    if (hq >= 0) {
+        const int kvh = hq / p.q_tiles, r0 = (hq - kvh * p.q_tiles) * 16;
+        h0 = kvh * p.group + r0;
+        heads = min(16, p.group - r0);
+    }
+    const size_t at = (size_t)seq * p.ld_out + (size_t)h0 * hd;
+    for (int i = tid; i < heads * hd; i += threads) {
+        if constexpr (sizeof(T) == 2) static_cast<bf16_t*>(p.out)[at + i] = bad ? 0x7FC0 : 0;
+        else static_cast<float*>(p.out)[at + i] = bad ? NAN : 0.f;
+    }
+}
+
+// T: type of queries and outputs.  WHOLE: a workgroup takes a head group of a sequence;
+// otherwise a run of all tiles.
+template <typename T, riftkv_dtype DT, int HD, int WAVES, bool WHOLE>
+__global__ void __launch_bounds__(64 * WAVES, 2)
 attention_kernel(AttnParams p) {
+    constexpr int kThreads = 64 * WAVES;
+    constexpr int RECORDS = WHOLE ? WAVES : 2 * WAVES;   // a wave's parts of heads
     constexpr int B = DT == RIFTKV_F32 ? 4 : DT == RIFTKV_BF16 ? 2 : 1;   // bytes a value
     constexpr bool SCALED = B == 1, F32 = DT == RIFTKV_F32;
     // A load of keys takes E 64-byte pieces of 16 / E rows (whole 128-byte lines), so that
@@ -142,77 +191,139 @@ attention_kernel(AttnParams p) {
     constexpr int C = HD / 16;               // columns of a lane of one value row
     constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
     constexpr int RS = HD + 4;               // floats of a part's row: values, max, sum (and odd to the banks)
-    extern __shared__ __align__(16) float records[];   // [2 kWaves][rows][RS]
-    __shared__ int4 meta[2 * kWaves];        // sequence (-1: no record), head group, whether it begins and ends the head
-    __shared__ long long head_end[2 * kWaves];   // the tile after the head's last
-    __shared__ long long sums[kWaves];
-    __shared__ int found_seq[kWaves];
-    __shared__ long long found_at[kWaves];   // tiles before that sequence
+    extern __shared__ __align__(16) float records[];   // [RECORDS][rows][RS]
+    __shared__ int4 meta[RECORDS];           // sequence (-1: no record), head group, whether it begins and ends the head
+    __shared__ unsigned long long head_end[RECORDS];   // the tile after the head's last
+    __shared__ long long sums[WAVES];
+    __shared__ int found_seq[WAVES];
+    __shared__ long long found_at[WAVES];    // tiles before that sequence
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
     const int HQ = p.n_kv * p.q_tiles;
     const int slot_floats = p.rows * RS;
 
-    // This wave's share of the tiles: a thread sums a run of sequences, the workgroup
-    // scans the sums, and whoever holds a wave's first tile looks it up.
-    const int per = (p.n_seq + kThreads - 1) / kThreads;
-    const int s0 = min(tid * per, p.n_seq), s1 = min(s0 + per, p.n_seq);
-    long long mine = 0;
-    for (int s = s0; s < s1; ++s) mine += tiles_of(length_of(p.lens[s], p.max_pages, p.shift));
-    long long incl = mine;
+    if (lane < RECORDS / WAVES) meta[wave * (RECORDS / WAVES) + lane] = make_int4(-1, 0, 0, 0);
+    Place cur{};
+    int left = 0;                       // tiles of this wave from cur on
+    unsigned long long end = 0;         // and the tile after them, among all
+    unsigned waves = 0;                 // waves with tiles, and their shares
+    Deal deal(0, 1);
+    if constexpr (WHOLE) {
+        cur.seq = blockIdx.x / HQ;
+        cur.hq = blockIdx.x - cur.seq * HQ;
+        const int given = p.lens[cur.seq];
+        cur.len = length_of(given, p.max_pages, p.shift);
+        if (cur.len == 0) {
+            fill_heads<T>(p, cur.seq, given, cur.hq, HD, tid, kThreads);
+            return;
+        }
+        const int t = tiles_of(cur.len);
+        cur.tile = (int)((unsigned)(t * wave) / WAVES);
+        left = (int)((unsigned)(t * (wave + 1)) / WAVES) - cur.tile;
+    } else {
+        const unsigned all = gridDim.x * WAVES, gw = blockIdx.x * WAVES + wave;
+        if (p.few) {
+            // Every wave by itself: the lengths in registers, scanned.
+            constexpr int CH = kFewSeqs / 64;
+            int len[CH], incl[CH], total = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const long long o = __shfl_up(incl, d);
-        if (lane >= d) incl += o;
-    }
-    if (lane == 63) sums[wave] = incl;
-    if (tid < 2 * kWaves) meta[tid] = make_int4(-1, 0, 0, 0);
-    __syncthreads();
-    long long before = incl - mine, total = 0;
+            for (int c = 0; c < CH; ++c) {
+                const int s = 64 * c + lane;
+                len[c] = s < p.n_seq ? length_of(p.lens[s], p.max_pages, p.shift) : 0;
+            }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += sums[w];
-        total += sums[w];
-    }
-    const unsigned long long N = (unsigned long long)total * HQ;
-    const unsigned long long all = (unsigned long long)gridDim.x * kWaves, most = (N + kMinTiles - 1) / kMinTiles;
-    const unsigned W = (unsigned)(most < all ? most : all);      // waves with tiles
-    auto first_of = [&](unsigned w) { return (long long)(N * w / W); };   // N W < 2^64: W <= 2^12, N <= 2^16 2^12 2^26
-    if (mine > 0) {
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const unsigned gw = blockIdx.x * kWaves + w;
-            if (gw >= W) continue;
-            const long long a = first_of(gw);
-            if (a >= before * HQ && a < (before + mine) * HQ) {
-                long long at = before;
-                int s = s0;
-                for (;; ++s) {
-                    const int t = tiles_of(length_of(p.lens[s], p.max_pages, p.shift));
-                    if (a < (at + t) * HQ) break;
-                    at += t;
+            for (int c = 0; c < CH; ++c) {
+                incl[c] = 0;
+                if (64 * c < p.n_seq) {
+                    incl[c] = wave_scan(tiles_of(len[c])) + total;
+                    total = __builtin_amdgcn_readlane(incl[c], 63);
                 }
-                found_seq[w] = s;
-                found_at[w] = at;
+            }
+            const unsigned long long N = (unsigned long long)total * HQ;
+            waves = (unsigned)(N < all ? N : all);
+            if (gw < waves) {
+                deal = Deal(N, waves);
+                const unsigned long long first = deal.first(gw);
+                const int at = (int)quotient(first, HQ);      // tiles of sequences, one head group each
+                int c0 = 0, ch = 0;
+                unsigned long long mask = 0;
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    if (mask == 0 && 64 * c < p.n_seq) {
+                        mask = __ballot(incl[c] > at);
+                        if (mask != 0) {
+                            ch = c;
+                            const int l = __ffsll(mask) - 1;
+                            cur.len = __builtin_amdgcn_readlane(len[c], l);
+                            c0 = __builtin_amdgcn_readlane(incl[c], l) - tiles_of(cur.len);
+                        }
+                    }
+                cur.seq = 64 * ch + __ffsll(mask) - 1;
+                const unsigned long long in = first - (unsigned long long)c0 * HQ;
+                const int t = tiles_of(cur.len);
+                cur.hq = (int)quotient(in, t);
+                cur.tile = (int)(in - (unsigned long long)cur.hq * t);
+            }
+        } else {
+            // A thread sums a run of sequences, the workgroup scans the sums, and whoever
+            // holds a wave's first tile looks it up.
+            const int per = (p.n_seq + kThreads - 1) / kThreads;
+            const int s0 = min(tid * per, p.n_seq), s1 = min(s0 + per, p.n_seq);
+            long long mine = 0;
+            for (int s = s0; s < s1; ++s) mine += tiles_of(length_of(p.lens[s], p.max_pages, p.shift));
+            long long incl = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const long long o = __shfl_up(incl, d);
+                if (lane >= d) incl += o;
+            }
+            if (lane == 63) sums[wave] = incl;
+            __syncthreads();
+            long long before = incl - mine, total = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) before += sums[w];
+                total += sums[w];
+            }
+            const unsigned long long N = (unsigned long long)total * HQ;
+            waves = (unsigned)(N < all ? N : all);
+            if (waves > 0) deal = Deal(N, waves);
+            if (mine > 0) {
+                for (int w = 0; w < WAVES; ++w) {
+                    const unsigned other = blockIdx.x * WAVES + w;
+                    if (other >= waves) break;
+                    const long long a = (long long)deal.first(other);
+                    if (a >= before * HQ && a < (before + mine) * HQ) {
+                        long long at = before;
+                        int s = s0;
+                        for (;; ++s) {
+                            const int t = tiles_of(length_of(p.lens[s], p.max_pages, p.shift));
+                            if (a < (at + t) * HQ) break;
+                            at += t;
+                        }
+                        found_seq[w] = s;
+                        found_at[w] = at;
+                    }
+                }
+            }
+            __syncthreads();
+            if (gw < waves) {
+                cur.seq = __builtin_amdgcn_readfirstlane(found_seq[wave]);
+                cur.len = __builtin_amdgcn_readfirstlane(p.lens[cur.seq]);
+                const unsigned long long in = deal.first(gw) - (unsigned long long)found_at[wave] * HQ;
+                const int t = tiles_of(cur.len);
+                cur.hq = __builtin_amdgcn_readfirstlane((int)quotient(in, t));
+                cur.tile = __builtin_amdgcn_readfirstlane((int)(in - (unsigned long long)cur.hq * t));
             }
         }
-    }
-    __syncthreads();
-
-    const unsigned gw = blockIdx.x * kWaves + wave;
-    if (gw < W) {
-        const long long a = first_of(gw);
-        int left = __builtin_amdgcn_readfirstlane((int)(first_of(gw + 1) - a));
-        Place cur;
-        cur.seq = __builtin_amdgcn_readfirstlane(found_seq[wave]);
-        cur.len = __builtin_amdgcn_readfirstlane(p.lens[cur.seq]);
-        {
-            const long long in = a - found_at[wave] * HQ;      // tiles of the sequence before
-            const int t = tiles_of(cur.len);
-            cur.hq = __builtin_amdgcn_readfirstlane((int)(in / t));
-            cur.tile = __builtin_amdgcn_readfirstlane((int)(in - (long long)cur.hq * t));
+        if (gw < waves) {
+            end = deal.first(gw + 1);
+            left = __builtin_amdgcn_readfirstlane((int)(end - deal.first(gw)));
         }
+    }
+
+    if (left > 0) {
         auto after = [&](Place c) __attribute__((always_inline)) {
             if ((c.tile + 1) * kTile < c.len) {
                 ++c.tile;
@@ -479,10 +590,10 @@ attention_kernel(AttnParams p) {
                             }
                     }
                 } else {
-                    const int rec = 2 * wave + n_records++;
+                    const int rec = RECORDS / WAVES * wave + n_records++;
                     if (lane == 0) {
                         meta[rec] = make_int4(cur.seq, cur.hq, begin == 0, ends);
-                        head_end[rec] = first_of(gw + 1) - left - cur.tile + tiles_of(cur.len);
+                        head_end[rec] = end - left - cur.tile + tiles_of(cur.len);
                     }
                     if (valid) {
                         float* dst = records + (size_t)rec * slot_floats + n * RS;
@@ -514,14 +625,14 @@ attention_kernel(AttnParams p) {
     // end of one begun in an earlier workgroup to slot 0, the start of one that goes
     // on in the next to slot 1.
     int4 join = make_int4(-1, 0, 0, 0);
-    for (int r = 0; r < 2 * kWaves;) {
+    for (int r = 0; r < RECORDS;) {
         const int4 a = meta[r];
         if (a.x < 0) {
             ++r;
             continue;
         }
         int e = r + 1, ends = a.w;      // records r .. e - 1, absent ones among them
-        for (; e < 2 * kWaves; ++e) {
+        for (; e < RECORDS; ++e) {
             const int4 b = meta[e];
             if (b.x < 0) continue;
             if (b.x != a.x || b.y != a.y) break;
@@ -529,8 +640,7 @@ attention_kernel(AttnParams p) {
         }
         const int kvh = a.y / p.q_tiles, r0 = (a.y - kvh * p.q_tiles) * 16, rows = min(16, p.group - r0);
         float* slot = p.slots + ((size_t)blockIdx.x * 2 + (a.z ? 1 : 0)) * slot_floats;
-        if (a.z && !ends)   // the wave with the head's last tile u: the largest w with N w / W < u + 1
-            join = make_int4(a.x, a.y, (int)(((unsigned long long)head_end[r] * W - 1) / N) / kWaves, 0);
+        if (!WHOLE && a.z && !ends) join = make_int4(a.x, a.y, deal.owner(head_end[r] - 1) / WAVES, 0);
         for (int item = tid; item < rows * (HD / 4); item += kThreads) {
             const int row = item / (HD / 4), col = 4 * (item % (HD / 4));
             float mx = -INFINITY, L = 0.f;
@@ -563,7 +673,7 @@ attention_kernel(AttnParams p) {
         }
         r = e;
     }
-    if (tid == 0) p.joins[blockIdx.x] = join;
+    if (!WHOLE && tid == 0) p.joins[blockIdx.x] = join;
 }
 
 // One workgroup for each of the first kernel's: the head that it begins and others go
@@ -578,16 +688,9 @@ join_kernel(AttnParams p) {
     __shared__ __align__(16) f32x4_t accs[kJoinThreads];
     __shared__ float2 mls[kJoinThreads];
     const int tid = threadIdx.x;
-    // sequences without tokens, or of a length out of range
     for (int s = blockIdx.x; s < p.n_seq; s += gridDim.x) {
-        const int len = p.lens[s];
-        const bool bad = len != 0 && length_of(len, p.max_pages, p.shift) == 0;
-        if (len != 0 && !bad) continue;
-        if (bad && tid == 0) *p.status = RIFT_ERR_SHAPE;
-        for (int i = tid; i < p.n_kv * p.group * HD; i += kJoinThreads) {
-            if constexpr (sizeof(T) == 2) static_cast<bf16_t*>(p.out)[(size_t)s * p.ld_out + i] = bad ? 0x7FC0 : 0;
-            else static_cast<float*>(p.out)[(size_t)s * p.ld_out + i] = bad ? NAN : 0.f;
-        }
+        const int given = p.lens[s];
+        if (length_of(given, p.max_pages, p.shift) == 0) fill_heads<T>(p, s, given, -1, HD, tid, kJoinThreads);
     }
     const int4 join = p.joins[blockIdx.x];
     if (join.x < 0) return;
@@ -645,8 +748,25 @@ int64_t most_tiles(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t ma
     return n_seq * c.n_kv_heads * q_tiles_of(c, n_heads) * ((max_pages * c.page_size + kTile - 1) / kTile);
 }
 int workgroups(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages) {
-    const int64_t wgs = (most_tiles(c, n_heads, n_seq, max_pages) + kWaves * kMinTiles - 1) / (kWaves * kMinTiles);
+    const int64_t wgs = (most_tiles(c, n_heads, n_seq, max_pages) + kSplitWaves - 1) / kSplitWaves;
     return (int)(wgs < 1 ? 1 : wgs > kMaxWgs ? kMaxWgs : wgs);
+}
+
+// Waves of a workgroup that takes a head whole, or 0: heads are split.  A split costs the
+// scan of the lengths and the join, which short heads do not repay; a head taken whole is
+// read at one CU's rate, so it is bounded by what the table can hold.  In us, split / whole
+// with 1, 2 and 4 waves, bf16 of 128 dimensions and 8 key heads if not said otherwise:
+//   8 heads of 256 tokens            10.1 / 11.6  8.4  7.7    of 1,024   11.4 / 27.8 19.3 13.7
+//   128 of 300 to 512                15.9 / 22.1 14.5 11.9    512 of 64  11.1 /  6.2  6.7  7.2
+//   1,024 of 32 to 512, fp8          25.6 / 28.4 20.5 24.5    of 1,024, 4 waves  48.4 / 44.7
+//   2,048 of 30 to 200, 64 dims      22.7 / 16.0 16.1 20.0    2,048 of 256  48.1 / 44.0 46.9 47.1
+//   4,096 of 64                      30.6 / 25.8 29.4 38.3    16,384 of 64  93.8 / 88.8 92.2 129.8
+//   3,200 of 131 to 643             110.1 / 106.0 106.5 104.4
+int whole_waves(const riftkv_cache& c, int64_t heads, int64_t max_pages) {
+    const int64_t most = max_pages * c.page_size;
+    if (most > 1024 || (most > 512 && heads < 256)) return 0;
+    if (most <= 64 || (most <= 512 && heads >= 2048)) return 1;
+    return most <= 128 || (most <= 512 && heads >= 1024) ? 2 : 4;
 }
 
 }  // namespace
@@ -658,7 +778,7 @@ size_t kv_attention_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq,
 }
 
 bool kv_attention_counts(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages) {
-    return most_tiles(c, n_heads, n_seq, max_pages) < (1ll << 41);   // times 2,048 waves in 64 bits, a wave's share in 31
+    return most_tiles(c, n_heads, n_seq, max_pages) < (1ll << 41);   // a wave's share (one of 2,048) in 31 bits
 }
 
 hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipStream_t st) {
@@ -685,21 +805,33 @@ hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipS
     p.group = a.n_heads / c.n_kv_heads;
     p.q_tiles = q_tiles_of(c, a.n_heads);
     p.rows = rows_of(c, a.n_heads);
+    p.few = a.n_seq <= kFewSeqs && (int64_t)a.n_seq * (((int64_t)a.max_pages * c.page_size + kTile - 1) / kTile) < (1ll << 31);
     p.scale_log2 = a.scale * 1.4426950408889634f;
-    const size_t lds = 2 * kWaves * (size_t)p.rows * (c.head_dim + 4) * sizeof(float);
-    auto launch = [&](auto kernel, auto join) {
+    const size_t record = (size_t)p.rows * (c.head_dim + 4) * sizeof(float);
+    auto launch = [&](auto kernel, unsigned grid, int waves, size_t lds) {
         if (lds > 64 * 1024) {   // 16 query rows of 128 dimensions; the attribute is the current device's
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e != hipSuccess) return e;
         }
-        hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kThreads), lds, st, p);
-        hipLaunchKernelGGL(join, dim3(wgs), dim3(kJoinThreads), 0, st, p);
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), lds, st, p);
+        return hipGetLastError();
+    };
+    const int64_t heads_of_all = (int64_t)a.n_seq * c.n_kv_heads * p.q_tiles;
+    const int whole = whole_waves(c, heads_of_all, a.max_pages);
+    auto run = [&](auto t, auto dt, auto hd) {
+        using T = decltype(t);
+        const unsigned all = (unsigned)heads_of_all;
+        if (whole == 1) return launch(attention_kernel<T, dt.value, hd.value, 1, true>, all, 1, record);
+        if (whole == 2) return launch(attention_kernel<T, dt.value, hd.value, 2, true>, all, 2, 2 * record);
+        if (whole == 4) return launch(attention_kernel<T, dt.value, hd.value, 4, true>, all, 4, 4 * record);
+        const hipError_t e = launch(attention_kernel<T, dt.value, hd.value, kSplitWaves, false>, (unsigned)wgs, kSplitWaves, 2 * kSplitWaves * record);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((join_kernel<T, hd.value>), dim3(wgs), dim3(kJoinThreads), 0, st, p);
         return hipGetLastError();
     };
     auto heads = [&](auto t, auto dt) {
-        using T = decltype(t);
-        if (c.head_dim == 128) return launch(attention_kernel<T, dt.value, 128>, join_kernel<T, 128>);
-        return launch(attention_kernel<T, dt.value, 64>, join_kernel<T, 64>);
+        if (c.head_dim == 128) return run(t, dt, std::integral_constant<int, 128>{});
+        return run(t, dt, std::integral_constant<int, 64>{});
     };
     auto types = [&](auto dt) {
         if constexpr (dt.value != RIFTKV_F32)
