@@ -8,7 +8,6 @@ rows themselves may be any stride apart (slices of a projection).  All tensors
 of a call are on one device, which need not be the current one."""
 from __future__ import annotations
 
-import contextlib
 import ctypes
 from typing import Optional
 
@@ -64,38 +63,39 @@ def _load() -> ctypes.CDLL:
 
 
 # ----------------------------------------------------------------------------- checks
+# Devices are compared by index: a call's checks are part of its cost.
 def _dense(t, dtype, shape, device, name):
-    """A contiguous device tensor; shape None: any."""
+    """Address of a contiguous device tensor; shape None: any."""
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
-    if t.device != device:
-        raise ValueError(f"{name}: must be on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: must be on device {device}")
     return t.data_ptr()
 
 
 def _rows(t, dtype, shape, device, name):
-    """[rows][heads][head_dim], the last two contiguous: (pointer, elements between rows)."""
+    """[rows][heads][head_dim], the last two contiguous: (address, elements between rows)."""
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name}: must be on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: must be on device {device}")
     n, heads, hd = shape
-    st = t.stride()
-    if (hd > 1 and st[2] != 1) or (heads > 1 and st[1] != hd):
+    ld, sh, se = t.stride()
+    if (hd > 1 and se != 1) or (heads > 1 and sh != hd):
         raise ValueError(f"{name}: heads and elements must be contiguous")
-    return t.data_ptr(), (st[0] if n > 1 else heads * hd)
+    return t.data_ptr(), (ld if n > 1 else heads * hd)
 
 
 def _device_of(t, name):
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a device tensor")
-    return t.device
+    return t.get_device()
 
 
 def _row_type(t, name):
@@ -105,19 +105,23 @@ def _row_type(t, name):
     return dt
 
 
-_HERE = contextlib.nullcontext()
-
-
-def _on(device):
-    """The device as the current one for a call."""
-    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-
 def _stream(stream, device):
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    if s.device != device:
-        raise ValueError(f"stream: must be on {device}")
-    return s.cuda_stream or None
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device) or None
+    if stream.device.index != device:
+        raise ValueError(f"stream: must be on device {device}")
+    return stream.cuda_stream or None
+
+
+def _call(name, device, fn, *args):
+    """fn with `device` as the current one."""
+    if device == torch.cuda.current_device():
+        st = fn(*args)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args)
+    if st:
+        _check(st, name)
 
 
 # ----------------------------------------------------------------------------- the pages
@@ -196,11 +200,8 @@ def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "h
     if freqs.dtype != "float64" or not freqs.flags.c_contiguous:
         raise TypeError("freqs: expected a contiguous float64 array")
     pos = _dense(positions, torch.int32, (rows,), dev, "positions")
-    with _on(dev):
-        st = L.riftkv_rope(*args, dt, pos, rows, hd, 2 * freqs.size, ROPE_LAYOUTS[layout], freqs.ctypes.data,
-                           magnitude, _stream(stream, dev))
-    if st:
-        _check(st, "riftkv_rope")
+    _call("riftkv_rope", dev, L.riftkv_rope, *args, dt, pos, rows, hd, 2 * freqs.size, ROPE_LAYOUTS[layout],
+          freqs.__array_interface__["data"][0], magnitude, _stream(stream, dev))
 
 
 # ----------------------------------------------------------------------------- rows
@@ -215,11 +216,8 @@ def _move(name, cache, k, v, page_table, positions, status, seq_ids, stream):
     pos = _dense(positions, torch.int32, (rows,), dev, "positions")
     ids = None if seq_ids is None else _dense(seq_ids, torch.int32, (rows,), dev, "seq_ids")
     word = _dense(status, torch.int32, (1,), dev, "status")
-    with _on(dev):
-        st = getattr(_load(), name)(cache.ref, pk, ldk, pv, ldv, dt, table, n_seq, max_pages, ids, pos, rows, word,
-                                    _stream(stream, dev))
-    if st:
-        _check(st, name)
+    _call(name, dev, getattr(_lib, name), cache.ref, pk, ldk, pv, ldv, dt, table, n_seq, max_pages, ids, pos, rows, word,
+          _stream(stream, dev))
 
 
 def riftkv_write(cache: KvCache, k, v, page_table, positions, status, seq_ids=None, stream=None) -> None:
@@ -253,9 +251,5 @@ def riftkv_attention(cache: KvCache, q, page_table, lens, out, workspace, status
     n = _dense(lens, torch.int32, (n_seq,), dev, "lens")
     word = _dense(status, torch.int32, (1,), dev, "status")
     ws = _dense(workspace, torch.uint8, None, dev, "workspace")
-    with _on(dev):
-        st = _load().riftkv_attention(cache.ref, pq, ldq, shape[1], dt, table, n_seq, max_pages, n,
-                                      cache.head_dim ** -0.5 if scale is None else scale, po, ldo, word, ws,
-                                      workspace.numel(), _stream(stream, dev))
-    if st:
-        _check(st, "riftkv_attention")
+    _call("riftkv_attention", dev, _lib.riftkv_attention, cache.ref, pq, ldq, shape[1], dt, table, n_seq, max_pages, n,
+          cache.head_dim ** -0.5 if scale is None else scale, po, ldo, word, ws, workspace.numel(), _stream(stream, dev))
