@@ -32,7 +32,9 @@ namespace rift {
 namespace {
 
 constexpr int kTile = 32;                 // tokens of a tile
+constexpr int kBegins = 1, kEnds = 2;     // a part holds a head's first, last tile
 constexpr int kSplitWaves = 4;            // of a workgroup, where heads are split over workgroups
+constexpr int kMaxWgs = 512;              // two workgroups a CU
 constexpr int kFewSeqs = 256;             // sequences whose lengths a wave holds in registers
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -47,15 +49,15 @@ struct AttnParams {
     const int* lens;
     int* status;
     float* slots;          // [wgs][2][rows][HD + 4]: weighted values, max, sum
-    int4* joins;           // [wgs]: sequence, head group and last workgroup of a head begun here
+    int4* joins;           // [wgs]: sequence (-1: none), first head, heads, last workgroup of a head group begun here
     int n_seq, max_pages, n_pages, n_kv, shift, group, q_tiles, rows;
-    int few;               // at most kFewSeqs sequences, and 31 bits hold their tiles
+    int few;               // at most kFewSeqs sequences, and 31 bits hold their tiles of all heads
     float scale_log2;
 };
 
-// A place in the sequence of tiles.
+// A place in the sequence of tiles: of head group hq, the qt-th of key head kvh.
 struct Place {
-    int seq, hq, tile, len;
+    int seq, hq, kvh, qt, tile, len;
 };
 
 __device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile; }
@@ -85,8 +87,14 @@ __device__ __forceinline__ int wave_scan(int x) {
 
 // How N tiles are dealt to W waves (W <= N): wave w's run begins at w q + min(w, r).
 struct Deal {
-    unsigned long long q, r;
-    __device__ __forceinline__ Deal(unsigned long long N, unsigned W) : q(quotient(N, W)), r(N - q * W) {}
+    unsigned long long q = 1, r = 0;
+    __device__ __forceinline__ Deal() {}
+    __device__ __forceinline__ Deal(unsigned long long N, unsigned W) {
+        if (N != W) {
+            q = quotient(N, W);
+            r = N - q * W;
+        }
+    }
     __device__ __forceinline__ unsigned long long first(unsigned w) const { return w * q + (w < r ? w : r); }
     __device__ __forceinline__ int owner(unsigned long long tile) const {
         const unsigned long long longer = r * (q + 1);
@@ -192,7 +200,7 @@ attention_kernel(AttnParams p) {
     constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
     constexpr int RS = HD + 4;               // floats of a part's row: values, max, sum (and odd to the banks)
     extern __shared__ __align__(16) float records[];   // [RECORDS][rows][RS]
-    __shared__ int4 meta[RECORDS];           // sequence (-1: no record), head group, whether it begins and ends the head
+    __shared__ int4 meta[RECORDS];           // sequence (-1: no record), first head, heads, which ends of their tiles it holds
     __shared__ unsigned long long head_end[RECORDS];   // the tile after the head's last
     __shared__ long long sums[WAVES];
     __shared__ int found_seq[WAVES];
@@ -208,7 +216,7 @@ attention_kernel(AttnParams p) {
     int left = 0;                       // tiles of this wave from cur on
     unsigned long long end = 0;         // and the tile after them, among all
     unsigned waves = 0;                 // waves with tiles, and their shares
-    Deal deal(0, 1);
+    Deal deal;
     if constexpr (WHOLE) {
         cur.seq = blockIdx.x / HQ;
         cur.hq = blockIdx.x - cur.seq * HQ;
@@ -244,26 +252,24 @@ attention_kernel(AttnParams p) {
             waves = (unsigned)(N < all ? N : all);
             if (gw < waves) {
                 deal = Deal(N, waves);
-                const unsigned long long first = deal.first(gw);
-                const int at = (int)quotient(first, HQ);      // tiles of sequences, one head group each
-                int c0 = 0, ch = 0;
+                const int at = (int)deal.first(gw);
+                int before = 0, ch = 0;
                 unsigned long long mask = 0;
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
                     if (mask == 0 && 64 * c < p.n_seq) {
-                        mask = __ballot(incl[c] > at);
+                        mask = __ballot(incl[c] * HQ > at);
                         if (mask != 0) {
                             ch = c;
                             const int l = __ffsll(mask) - 1;
                             cur.len = __builtin_amdgcn_readlane(len[c], l);
-                            c0 = __builtin_amdgcn_readlane(incl[c], l) - tiles_of(cur.len);
+                            before = (__builtin_amdgcn_readlane(incl[c], l) - tiles_of(cur.len)) * HQ;
                         }
                     }
                 cur.seq = 64 * ch + __ffsll(mask) - 1;
-                const unsigned long long in = first - (unsigned long long)c0 * HQ;
-                const int t = tiles_of(cur.len);
-                cur.hq = (int)quotient(in, t);
-                cur.tile = (int)(in - (unsigned long long)cur.hq * t);
+                const unsigned t = tiles_of(cur.len), in = at - before;
+                cur.hq = __builtin_amdgcn_readfirstlane(in / t);
+                cur.tile = in - cur.hq * t;
             }
         } else {
             // A thread sums a run of sequences, the workgroup scans the sums, and whoever
@@ -324,14 +330,20 @@ attention_kernel(AttnParams p) {
     }
 
     if (left > 0) {
+        cur.kvh = p.q_tiles == 1 ? cur.hq : cur.hq / p.q_tiles;
+        cur.qt = cur.hq - cur.kvh * p.q_tiles;
         auto after = [&](Place c) __attribute__((always_inline)) {
             if ((c.tile + 1) * kTile < c.len) {
                 ++c.tile;
                 return c;
             }
             c.tile = 0;
+            if (++c.qt == p.q_tiles) {
+                c.qt = 0;
+                ++c.kvh;
+            }
             if (++c.hq == HQ) {
-                c.hq = 0;
+                c.hq = c.kvh = c.qt = 0;
                 do {
                     ++c.seq;
                     c.len = length_of(p.lens[c.seq], p.max_pages, p.shift);
@@ -355,7 +367,7 @@ attention_kernel(AttnParams p) {
         // first row of a half's keys and values among the pages' rows
         auto row_of = [&](const Place& c, int page, int h) __attribute__((always_inline)) {
             page = (unsigned)page < (unsigned)p.n_pages ? page : 0;
-            return ((((size_t)page * p.n_kv) + c.hq / p.q_tiles) << p.shift) + ((c.tile * kTile + 16 * h) & ((1 << p.shift) - 1));
+            return ((((size_t)page * p.n_kv) + c.kvh) << p.shift) + ((c.tile * kTile + 16 * h) & ((1 << p.shift) - 1));
         };
         auto load_k = [&](const Place& c, const Pages& pg, bool live) __attribute__((always_inline)) {
             const unsigned off = live ? k_lane : 0;
@@ -384,8 +396,12 @@ attention_kernel(AttnParams p) {
         Pages cur_pages = pages_at(cur);
         load_k(cur, cur_pages, true);
         load_v(cur, cur_pages, true);
-        Place nxt = left > 1 ? after(cur) : cur;
-        Pages nxt_pages = pages_at(nxt);
+        Place nxt = cur;
+        Pages nxt_pages = cur_pages;
+        if (left > 1) {
+            nxt = after(cur);
+            nxt_pages = pages_at(nxt);
+        }
 
         bf16x8_t qf[F32 ? 1 : NQ][F32 ? 1 : HD / 32];
         float qs[F32 ? HD / 4 : 1];
@@ -395,9 +411,9 @@ attention_kernel(AttnParams p) {
         int begin = cur.tile;      // this wave's first tile of the head
         int n_records = 0;
         auto start_head = [&](const Place& c) __attribute__((always_inline)) {
-            const int kvh = c.hq / p.q_tiles, r = (c.hq - kvh * p.q_tiles) * 16 + n;   // this lane's query
+            const int r = 16 * c.qt + n;   // this lane's query
             const bool there = r < p.group;
-            const size_t q0 = (size_t)c.seq * p.ld_q + (size_t)(kvh * p.group + (there ? r : 0)) * HD;
+            const size_t q0 = (size_t)c.seq * p.ld_q + (size_t)(c.kvh * p.group + (there ? r : 0)) * HD;
             if constexpr (F32) {
 #pragma unroll
                 for (int i = 0; i < HD / 16; ++i) {
@@ -556,8 +572,12 @@ attention_kernel(AttnParams p) {
                 }
             }
             load_v(nxt, nxt_pages, live);
-            const Place nn = left > 2 ? after(nxt) : nxt;
-            const Pages nn_pages = pages_at(nn);
+            Place nn = nxt;
+            Pages nn_pages = nxt_pages;
+            if (left > 2) {
+                nn = after(nxt);
+                nn_pages = pages_at(nn);
+            }
 
             const bool ends = (cur.tile + 1) * kTile >= cur.len;
             if (ends || !live) {   // the wave's last tile of this head: o[c][i] is column (4 g + i) C + c of query n
@@ -566,12 +586,12 @@ attention_kernel(AttnParams p) {
                     sum = NAN;
                     if (lane == 0) *p.status = RIFT_ERR_SHAPE;
                 }
-                const int kvh = cur.hq / p.q_tiles, r0 = (cur.hq - kvh * p.q_tiles) * 16;
-                const bool valid = r0 + n < p.group;
+                const int h0 = cur.kvh * p.group + 16 * cur.qt, rows = min(16, p.group - 16 * cur.qt);   // first head, heads
+                const bool valid = n < rows;
                 if (begin == 0 && ends) {
                     if (valid) {
                         const float inv = 1.f / sum;
-                        const size_t o0 = (size_t)cur.seq * p.ld_out + (size_t)(kvh * p.group + r0 + n) * HD;
+                        const size_t o0 = (size_t)cur.seq * p.ld_out + (size_t)(h0 + n) * HD;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -592,7 +612,7 @@ attention_kernel(AttnParams p) {
                 } else {
                     const int rec = RECORDS / WAVES * wave + n_records++;
                     if (lane == 0) {
-                        meta[rec] = make_int4(cur.seq, cur.hq, begin == 0, ends);
+                        meta[rec] = make_int4(cur.seq, h0, rows, (begin == 0 ? kBegins : 0) | (ends ? kEnds : 0));
                         head_end[rec] = end - left - cur.tile + tiles_of(cur.len);
                     }
                     if (valid) {
@@ -624,38 +644,56 @@ attention_kernel(AttnParams p) {
     // Neighbouring records of one head are joined: a whole head goes to the output, the
     // end of one begun in an earlier workgroup to slot 0, the start of one that goes
     // on in the next to slot 1.
-    int4 join = make_int4(-1, 0, 0, 0);
-    for (int r = 0; r < RECORDS;) {
+    // (All records are read, whether there or not, so that the reads follow each other.)
+    int4 mt[RECORDS], join = make_int4(-1, 0, 0, 0);
+    unsigned rest = 0;
+    int last = 0;       // a record of the head that goes on
+#pragma unroll
+    for (int i = 0; i < RECORDS; ++i) mt[i] = meta[i];
+#pragma unroll
+    for (int i = 0; i < RECORDS; ++i) rest |= mt[i].x >= 0 ? 1u << i : 0u;
+    rest = __builtin_amdgcn_readfirstlane(rest);
+    while (rest != 0) {
+        const int r = __ffs(rest) - 1;
         const int4 a = meta[r];
-        if (a.x < 0) {
-            ++r;
-            continue;
-        }
-        int e = r + 1, ends = a.w;      // records r .. e - 1, absent ones among them
-        for (; e < RECORDS; ++e) {
-            const int4 b = meta[e];
-            if (b.x < 0) continue;
-            if (b.x != a.x || b.y != a.y) break;
-            ends = b.w;
-        }
-        const int kvh = a.y / p.q_tiles, r0 = (a.y - kvh * p.q_tiles) * 16, rows = min(16, p.group - r0);
-        float* slot = p.slots + ((size_t)blockIdx.x * 2 + (a.z ? 1 : 0)) * slot_floats;
-        if (!WHOLE && a.z && !ends) join = make_int4(a.x, a.y, deal.owner(head_end[r] - 1) / WAVES, 0);
-        for (int item = tid; item < rows * (HD / 4); item += kThreads) {
-            const int row = item / (HD / 4), col = 4 * (item % (HD / 4));
-            float mx = -INFINITY, L = 0.f;
-            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-            for (int i = r; i < e; ++i)
-                if (meta[i].x >= 0) mx = fmaxf(mx, records[(size_t)i * slot_floats + row * RS + HD]);
-            for (int i = r; i < e; ++i) {
-                if (meta[i].x < 0) continue;
-                const float* src = records + (size_t)i * slot_floats + row * RS;
-                const float f = __builtin_amdgcn_exp2f(src[HD] - ref_of(mx));
-                L = fmaf(f, src[HD + 1], L);
-                acc += f * *reinterpret_cast<const f32x4_t*>(src + col);
+        unsigned mask = 0;
+        int held = 0;
+#pragma unroll
+        for (int i = 0; i < RECORDS; ++i)
+            if ((rest >> i & 1) && mt[i].x == a.x && mt[i].y == a.y) {
+                mask |= 1u << i;
+                held |= mt[i].w;
             }
-            if (a.z && ends) {
-                const size_t at = (size_t)a.x * p.ld_out + (size_t)(kvh * p.group + r0 + row) * HD + col;
+        mask = __builtin_amdgcn_readfirstlane(mask);
+        rest &= ~mask;
+        held = __builtin_amdgcn_readfirstlane(held);
+        float* slot = p.slots + ((size_t)blockIdx.x * 2 + (held & kBegins ? 1 : 0)) * slot_floats;
+        if (held == kBegins) {
+            join = a;
+            last = r;
+        }
+        for (int item = tid; item < a.z * (HD / 4); item += kThreads) {
+            const int row = item / (HD / 4), col = 4 * (item % (HD / 4));
+            const float* src = records + row * RS;
+            float m[RECORDS], mx = -INFINITY, L = 0.f;
+            f32x4_t x[RECORDS], acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < RECORDS; ++i) {
+                m[i] = src[i * slot_floats + HD];
+                x[i] = *reinterpret_cast<const f32x4_t*>(src + i * slot_floats + col);
+            }
+#pragma unroll
+            for (int i = 0; i < RECORDS; ++i)
+                if (mask >> i & 1) mx = fmaxf(mx, m[i]);
+#pragma unroll
+            for (int i = 0; i < RECORDS; ++i)
+                if (mask >> i & 1) {
+                    const float f = __builtin_amdgcn_exp2f(m[i] - ref_of(mx));
+                    L = fmaf(f, src[i * slot_floats + HD + 1], L);
+                    acc += f * x[i];
+                }
+            if (held == (kBegins | kEnds)) {
+                const size_t at = (size_t)a.x * p.ld_out + (size_t)(a.y + row) * HD + col;
                 acc *= 1.f / L;
                 if constexpr (sizeof(T) == 2)
                     *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + at) =
@@ -671,9 +709,11 @@ attention_kernel(AttnParams p) {
                 }
             }
         }
-        r = e;
     }
-    if (!WHOLE && tid == 0) p.joins[blockIdx.x] = join;
+    if (!WHOLE && tid == 0) {
+        if (join.x >= 0) join.w = deal.owner(head_end[last] - 1) / WAVES;
+        p.joins[blockIdx.x] = join;
+    }
 }
 
 // One workgroup for each of the first kernel's: the head that it begins and others go
@@ -688,27 +728,38 @@ join_kernel(AttnParams p) {
     __shared__ __align__(16) f32x4_t accs[kJoinThreads];
     __shared__ float2 mls[kJoinThreads];
     const int tid = threadIdx.x;
+    const int4 join = p.joins[blockIdx.x];
     for (int s = blockIdx.x; s < p.n_seq; s += gridDim.x) {
         const int given = p.lens[s];
         if (length_of(given, p.max_pages, p.shift) == 0) fill_heads<T>(p, s, given, -1, HD, tid, kJoinThreads);
     }
-    const int4 join = p.joins[blockIdx.x];
     if (join.x < 0) return;
-    const int kvh = join.y / p.q_tiles, r0 = (join.y - kvh * p.q_tiles) * 16, rows = min(16, p.group - r0);
-    const int items = rows * CV, PG = kJoinThreads / items;       // at least 2 (16 rows of 32 vectors)
-    const int parts = join.z - (int)blockIdx.x + 1, slot_floats = p.rows * RS;
+    const int items = join.z * CV, PG = kJoinThreads / items;     // at least 2 (16 heads of 32 vectors)
+    const int parts = join.w - (int)blockIdx.x + 1, slot_floats = p.rows * RS;
     const int pg = tid / items, item = tid - pg * items, row = item / CV, col = 4 * (item - row * CV);
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     if (pg < PG) {
-        for (int i = pg; i < parts; i += PG) {
-            const float* src = p.slots + ((size_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * slot_floats + row * RS;
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(src + col);
-            const float mi = src[HD], li = src[HD + 1], mn = fmaxf(m, mi);
-            const float f = __builtin_amdgcn_exp2f(m - ref_of(mn)), fi = __builtin_amdgcn_exp2f(mi - ref_of(mn));
-            acc = acc * f + x * fi;
-            l = l * f + li * fi;
-            m = mn;
+        constexpr int U = 4;   // parts in flight
+        for (int i = pg; i < parts; i += U * PG) {
+            f32x4_t x[U];
+            float2 ml[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {   // past the last: its values, not used
+                const int at = min(i + u * PG, parts - 1);
+                const float* src = p.slots + ((size_t)(blockIdx.x + at) * 2 + (at == 0 ? 1 : 0)) * slot_floats + row * RS;
+                x[u] = *reinterpret_cast<const f32x4_t*>(src + col);
+                ml[u] = *reinterpret_cast<const float2*>(src + HD);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i + u * PG >= parts) continue;
+                const float mn = fmaxf(m, ml[u].x);
+                const float f = __builtin_amdgcn_exp2f(m - ref_of(mn)), fi = __builtin_amdgcn_exp2f(ml[u].x - ref_of(mn));
+                acc = acc * f + x[u] * fi;
+                l = l * f + ml[u].y * fi;
+                m = mn;
+            }
         }
     }
     accs[tid] = acc;
@@ -728,7 +779,7 @@ join_kernel(AttnParams p) {
         l += f * ml.y;
     }
     acc *= 1.f / l;
-    const size_t at = (size_t)join.x * p.ld_out + (size_t)(kvh * p.group + r0 + row) * HD + col;
+    const size_t at = (size_t)join.x * p.ld_out + (size_t)(join.y + row) * HD + col;
     if constexpr (sizeof(T) == 2)
         *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + at) =
             make_uint2((uint32_t)round_bf16(acc[0]) | (uint32_t)round_bf16(acc[1]) << 16,
@@ -736,8 +787,6 @@ join_kernel(AttnParams p) {
     else
         *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + at) = acc;
 }
-
-constexpr int kMaxWgs = 512;   // two workgroups a CU
 
 int q_tiles_of(const riftkv_cache& c, int n_heads) { return (n_heads / c.n_kv_heads + 15) / 16; }
 int rows_of(const riftkv_cache& c, int n_heads) {
@@ -805,7 +854,7 @@ hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipS
     p.group = a.n_heads / c.n_kv_heads;
     p.q_tiles = q_tiles_of(c, a.n_heads);
     p.rows = rows_of(c, a.n_heads);
-    p.few = a.n_seq <= kFewSeqs && (int64_t)a.n_seq * (((int64_t)a.max_pages * c.page_size + kTile - 1) / kTile) < (1ll << 31);
+    p.few = a.n_seq <= kFewSeqs && most_tiles(c, a.n_heads, a.n_seq, a.max_pages) < (1ll << 31);
     p.scale_log2 = a.scale * 1.4426950408889634f;
     const size_t record = (size_t)p.rows * (c.head_dim + 4) * sizeof(float);
     auto launch = [&](auto kernel, unsigned grid, int waves, size_t lds) {
