@@ -197,11 +197,13 @@ def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "h
         p, ld = _rows(t, x.dtype, shape, dev, name)
         po, ldo = (p, ld) if o is None else _rows(o, x.dtype, shape, dev, name + "_out")
         args += [p, ld, shape[1], po, ldo]
-    if freqs.dtype != "float64" or not freqs.flags.c_contiguous:
+    if freqs.dtype.char != "d" or not freqs.flags.c_contiguous or freqs.size == 0:
         raise TypeError("freqs: expected a contiguous float64 array")
+    # (an array's own .ctypes takes three times as long)
+    fp = ctypes.byref(ctypes.c_double.from_buffer(freqs)) if freqs.flags.writeable else freqs.ctypes.data
     pos = _dense(positions, torch.int32, (rows,), dev, "positions")
     _call("riftkv_rope", dev, L.riftkv_rope, *args, dt, pos, rows, hd, 2 * freqs.size, ROPE_LAYOUTS[layout],
-          freqs.__array_interface__["data"][0], magnitude, _stream(stream, dev))
+          fp, magnitude, _stream(stream, dev))
 
 
 # ----------------------------------------------------------------------------- rows
