@@ -10,6 +10,7 @@
  *                     quantised as they are written
  *   riftkv_read       rows of the pages back, as dense rows
  *   riftkv_attention  one new token of every sequence over its pages
+ *   riftkv_decode_step  a decode step of rift.h's model over them
  *
  * The conventions of rift.h hold: device pointers unless marked [host], buffers
  * and workspace owned by the caller, calls asynchronous and ordered on
@@ -193,6 +194,40 @@ RIFT_API rift_status riftkv_attention(const riftkv_cache* cache, const void* q, 
                                       rift_dtype dt, const int32_t* page_table, int32_t n_seq, int32_t max_pages,
                                       const int32_t* lens, float scale, void* out, int64_t ld_out, int32_t* status,
                                       void* workspace, size_t ws_bytes, rift_stream stream);
+
+/* ------------------------------------------------------------------ decode */
+
+/* Workspace bytes of riftkv_decode_step (0 for shapes that it refuses).  Not smaller for
+ * more sequences or wider tables. */
+RIFT_API size_t riftkv_decode_workspace_size(const rift_model_cfg* cfg, const riftkv_cache* cache, int32_t n_seq,
+                                             int32_t max_pages);
+
+/*
+ * riftkv_decode_step -- one generated token of every sequence through the decoder layers of
+ * rift_prefill, keys and values in pages: rift_decode_step for prompts that come and go, any
+ * length, and quantised caches.  Per layer the new token's rotated key and its value are
+ * written (riftkv_write), and it attends to its sequence's tokens up to itself
+ * (riftkv_attention).  A prompt's earlier rows are rift_prefill's kv_cache, written with
+ * riftkv_write layer by layer (seq_ids and its position_ids say where); prompts with a shared
+ * prefix may share the pages that the prefix fills.
+ * cfg, layers  [host] as for rift_prefill; bfloat16 models
+ * x_new        [n_seq][d] bf16  input embeddings of the new tokens
+ * cache        [host] layer 0's pages; layer l's k, v, k_scale and v_scale follow those of layer
+ *              l - 1 ([n_layers][n_pages]...).  n_kv_heads and head_dim are the model's;
+ *              bf16, fp8 or int8
+ * page_table   [n_seq][max_pages] i32, the same pages for every layer
+ * positions    [n_seq] i32  the new token's position: the tokens that its sequence holds
+ *              already.  Negative: no sequence here (padding); nothing is written for it
+ *              and its hidden_out row means nothing
+ * hidden_out   [n_seq][d] f32 out  residual stream of the new tokens after the last layer
+ * status       as for riftkv_write and riftkv_attention; the row of a sequence that sets it is NaN
+ * Shape rules: those of rift_prefill's model and of riftkv_attention; n_seq * ffn < 2^31.
+ * Errors: RIFT_ERR_UNSUPPORTED also for float32 models and pages.
+ */
+RIFT_API rift_status riftkv_decode_step(const rift_model_cfg* cfg, const rift_layer_weights* layers, const void* x_new,
+                                        const riftkv_cache* cache, const int32_t* page_table, int32_t n_seq,
+                                        int32_t max_pages, const int32_t* positions, float* hidden_out,
+                                        int32_t* status, void* workspace, size_t ws_bytes, rift_stream stream);
 
 #ifdef __cplusplus
 }

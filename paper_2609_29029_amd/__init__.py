@@ -10,5 +10,5 @@ from ._lib import (EXPORTS, LIB_PATH, RIFT_BF16, RIFT_F32, LayerWeights, ModelCf
                    rift_score_workspace_size,
                    rift_select_tokens, rift_set_debug, rift_split_budgets)
 from .kv import (KV_EXPORTS, RIFTKV_BF16, RIFTKV_F32, RIFTKV_FP8, RIFTKV_INT8, KvCache, riftkv_attention,  # noqa: F401
-                 riftkv_attention_workspace_size, riftkv_cache, riftkv_read, riftkv_rope, riftkv_rope_freqs,
-                 riftkv_write)
+                 riftkv_attention_workspace_size, riftkv_cache, riftkv_decode_step, riftkv_decode_workspace_size,
+                 riftkv_read, riftkv_rope, riftkv_rope_freqs, riftkv_write)

@@ -10,6 +10,7 @@
 
 #include <mutex>
 
+#include "kv.h"
 #include "launch.h"
 #include "rift_common.h"
 
@@ -760,6 +761,42 @@ DecodeLayout decode_layout(const rift_model_cfg& c, int64_t n_seq, int64_t n_pos
     L.total = off;
     return L;
 }
+// The second half of a decode layer, from the attention's output in h on: the output
+// projection, the residual, the FFN.  With split-K products (partial sums in `part`) the last
+// reduction also leaves the next layer's normalised rows in h.
+hipError_t decode_after_attention_split(const rift_model_cfg& c, const rift_layer_weights* layers, int l, int n_seq,
+                                        uint16_t* h, uint16_t* a, float* part, float* hidden_out, hipStream_t st) {
+    const rift_layer_weights& w = layers[l];
+    const int d = c.d, F = c.ffn;
+    const SkinnySplit s_o = skinny_split(d, d), s_gu = skinny_split(2 * F, d), s_dn = skinny_split(d, F);
+    hipError_t e = launch_skinny_gemm(h, static_cast<const uint16_t*>(w.wo), nullptr, nullptr, d, n_seq, d, d, part, st);
+    if (e != hipSuccess) return e;
+    e = launch_skinny_resid_norm(part, s_o, n_seq, d, hidden_out, static_cast<const uint16_t*>(w.g_ffn), h, c.rms_eps, st);
+    if (e != hipSuccess) return e;
+    e = launch_skinny_gemm(h, static_cast<const uint16_t*>(w.w_gate), static_cast<const uint16_t*>(w.w_up), nullptr, F,
+                           n_seq, 2 * F, d, part, st);
+    if (e != hipSuccess) return e;
+    e = launch_skinny_swiglu(part, s_gu, n_seq, F, a, st);
+    if (e != hipSuccess) return e;
+    e = launch_skinny_gemm(a, static_cast<const uint16_t*>(w.w_down), nullptr, nullptr, d, n_seq, d, F, part, st);
+    if (e != hipSuccess) return e;
+    const bool last = l + 1 == c.n_layers;
+    return launch_skinny_resid_norm(part, s_dn, n_seq, d, hidden_out,
+                                    last ? nullptr : static_cast<const uint16_t*>(layers[l + 1].g_attn),
+                                    last ? nullptr : h, c.rms_eps, st);
+}
+hipError_t decode_after_attention(const rift_model_cfg& c, const rift_layer_weights& w, int n_seq, uint16_t* h,
+                                  uint16_t* a, float* hidden_out, hipStream_t st) {
+    const int d = c.d;
+    hipError_t e = launch_gemm_resid(h, static_cast<const uint16_t*>(w.wo), hidden_out, n_seq, d, d, st);
+    if (e != hipSuccess) return e;
+    e = launch_rmsnorm(hidden_out, false, nullptr, w.g_ffn, true, h, true, n_seq, d, c.rms_eps, st);
+    if (e != hipSuccess) return e;
+    e = launch_gemm_swiglu(h, static_cast<const uint16_t*>(w.w_gate), static_cast<const uint16_t*>(w.w_up), a, n_seq,
+                           c.ffn, d, st);
+    if (e != hipSuccess) return e;
+    return launch_gemm_resid(a, static_cast<const uint16_t*>(w.w_down), hidden_out, n_seq, d, c.ffn, st);
+}
 }  // namespace
 
 size_t rift_decode_workspace_size(const rift_model_cfg* cfg, int32_t n_seq, int32_t max_seqlen,
@@ -826,8 +863,6 @@ rift_status rift_decode_step(const rift_model_cfg* cfg, const rift_layer_weights
         // split-K GEMMs; the residual reduce of each layer's last GEMM also
         // applies the next layer's attention RMSNorm
         float* part = reinterpret_cast<float*>(ws + L.part);
-        const int F = c.ffn;
-        const SkinnySplit s_o = skinny_split(d, d), s_gu = skinny_split(2 * F, d), s_dn = skinny_split(d, F);
         const SkinnySplit s_qkv = skinny_split(3 * d, d);
         const bool many = decode_many(n_seq, c.n_heads, c.head_dim, n_pos);
         qkv.part = many ? nullptr : part;
@@ -848,19 +883,7 @@ rift_status rift_decode_step(const rift_model_cfg* cfg, const rift_layer_weights
                                              static_cast<const uint16_t*>(kv_cache) + (size_t)(2 * l + 1) * td, kn,
                                              vn, cu_p, n_seq, total_tokens, n_prefix, c.n_heads, c.head_dim,
                                              n_pos, max_new, step, list, h, st));
-            RIFT_TRY(launch_skinny_gemm(h, static_cast<const uint16_t*>(w.wo), nullptr, nullptr, d, n_seq, d, d,
-                                        part, st));
-            RIFT_TRY(launch_skinny_resid_norm(part, s_o, n_seq, d, hidden_out, static_cast<const uint16_t*>(w.g_ffn),
-                                              h, c.rms_eps, st));
-            RIFT_TRY(launch_skinny_gemm(h, static_cast<const uint16_t*>(w.w_gate),
-                                        static_cast<const uint16_t*>(w.w_up), nullptr, F, n_seq, 2 * F, d, part, st));
-            RIFT_TRY(launch_skinny_swiglu(part, s_gu, n_seq, F, a, st));
-            RIFT_TRY(launch_skinny_gemm(a, static_cast<const uint16_t*>(w.w_down), nullptr, nullptr, d, n_seq, d, F,
-                                        part, st));
-            const bool last = l + 1 == c.n_layers;
-            RIFT_TRY(launch_skinny_resid_norm(part, s_dn, n_seq, d, hidden_out,
-                                              last ? nullptr : static_cast<const uint16_t*>(layers[l + 1].g_attn),
-                                              last ? nullptr : h, c.rms_eps, st));
+            RIFT_TRY(decode_after_attention_split(c, layers, l, n_seq, h, a, part, hidden_out, st));
         }
         return RIFT_OK;
     }
@@ -892,14 +915,141 @@ rift_status rift_decode_step(const rift_model_cfg* cfg, const rift_layer_weights
         RIFT_TRY(launch_kv_append(kb, vb, kn, vn, n_seq, d, max_new, step, st));
         RIFT_TRY(launch_decode_attention(qb, qkv, kp, vp, kn, vn, cu_p, n_seq, total_tokens, n_prefix, c.n_heads,
                                          c.head_dim, n_pos, max_new, step, list, h, st));
-        RIFT_TRY(launch_gemm_resid(h, static_cast<const uint16_t*>(w.wo), hidden_out, n_seq, d, d, st));
-        RIFT_TRY(launch_rmsnorm(hidden_out, false, nullptr, w.g_ffn, true, h, true, n_seq, d, c.rms_eps, st));
-        RIFT_TRY(launch_gemm_swiglu(h, static_cast<const uint16_t*>(w.w_gate), static_cast<const uint16_t*>(w.w_up),
-                                    a, n_seq, c.ffn, d, st));
-        RIFT_TRY(launch_gemm_resid(a, static_cast<const uint16_t*>(w.w_down), hidden_out, n_seq, d, c.ffn, st));
+        RIFT_TRY(decode_after_attention(c, w, n_seq, h, a, hidden_out, st));
     }
-#undef RIFT_TRY
     return RIFT_OK;
 }
+
+namespace {
+// workspace of a decode step over pages: RoPE rows and lengths of the sequences, row numbers,
+// h, q, k, v [n_seq][d], the SwiGLU activation, the GEMMs' partial sums, the attention's own
+struct KvDecodeLayout {
+    size_t rope, lens, rows, h, q, k, v, a, part, attn, total;
+};
+KvDecodeLayout kv_decode_layout(const rift_model_cfg& c, const riftkv_cache& kv, int64_t n_seq, int64_t max_pages) {
+    KvDecodeLayout L{};
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += align_up(bytes);
+        return at;
+    };
+    const size_t row = (size_t)n_seq * c.d * 2;
+    L.rope = take((size_t)n_seq * (size_t)(c.head_dim / 2) * sizeof(float2));
+    L.lens = take((size_t)n_seq * sizeof(int));
+    L.rows = take((size_t)n_seq * sizeof(int));
+    L.h = take(row);
+    L.q = take(row);
+    L.k = take(row);
+    L.v = take(row);
+    L.a = take((size_t)n_seq * c.ffn * 2);
+    L.part = take(decode_gemm_floats(c, n_seq) * sizeof(float));
+    L.attn = take(kv_attention_workspace(kv, c.n_heads, n_seq, max_pages));
+    L.total = off;
+    return L;
+}
+// model and pages that fit each other
+rift_status check_kv_decode(const rift_model_cfg* cfg, const riftkv_cache* kv, int32_t n_seq, int32_t max_pages, bool arrays) {
+    const rift_status cs = check_cfg(cfg);
+    if (cs != RIFT_OK) return cs;
+    const rift_status ks = kv_check_cache(kv, arrays);
+    if (ks != RIFT_OK) return ks;
+    if (cfg->dt != RIFT_BF16 || kv->dt == RIFTKV_F32) return RIFT_ERR_UNSUPPORTED;
+    if (kv->n_kv_heads != cfg->n_heads || kv->head_dim != cfg->head_dim || n_seq < 0 || n_seq > 65535 || max_pages < 0 ||
+        (int64_t)max_pages * kv->page_size > INT32_MAX || (int64_t)n_seq * cfg->ffn >= (1ll << 31))
+        return RIFT_ERR_SHAPE;
+    return kv_attention_counts(*kv, cfg->n_heads, n_seq, max_pages) ? RIFT_OK : RIFT_ERR_UNSUPPORTED;
+}
+}  // namespace
+
+size_t riftkv_decode_workspace_size(const rift_model_cfg* cfg, const riftkv_cache* cache, int32_t n_seq, int32_t max_pages) {
+    if (check_kv_decode(cfg, cache, n_seq, max_pages, false) != RIFT_OK) return 0;
+    return kv_decode_layout(*cfg, *cache, n_seq, max_pages).total;
+}
+
+rift_status riftkv_decode_step(const rift_model_cfg* cfg, const rift_layer_weights* layers, const void* x_new,
+                               const riftkv_cache* cache, const int32_t* page_table, int32_t n_seq, int32_t max_pages,
+                               const int32_t* positions, float* hidden_out, int32_t* status, void* workspace,
+                               size_t ws_bytes, rift_stream stream) {
+    const rift_status cs = check_kv_decode(cfg, cache, n_seq, max_pages, true);
+    if (cs != RIFT_OK) return cs;
+    const rift_model_cfg c = *cfg;
+    if (status == nullptr) return RIFT_ERR_NULL;
+    if (n_seq == 0 || c.n_layers == 0) return RIFT_OK;
+    if (x_new == nullptr || positions == nullptr || hidden_out == nullptr || workspace == nullptr || layers == nullptr ||
+        (page_table == nullptr && max_pages > 0))
+        return RIFT_ERR_NULL;
+    for (int l = 0; l < c.n_layers; ++l) {
+        const rift_layer_weights& w = layers[l];
+        if (!w.wq || !w.wk || !w.wv || !w.wo || !w.w_gate || !w.w_up || !w.w_down || !w.g_attn || !w.g_ffn)
+            return RIFT_ERR_NULL;
+    }
+    const KvDecodeLayout L = kv_decode_layout(c, *cache, n_seq, max_pages);
+    if (misaligned(workspace) || ws_bytes < L.total) return RIFT_ERR_WORKSPACE;
+    if (init_kernel_attributes() != hipSuccess) return RIFT_ERR_HIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    float2* rope = reinterpret_cast<float2*>(ws + L.rope);
+    int* lens = reinterpret_cast<int*>(ws + L.lens);
+    int* rows = reinterpret_cast<int*>(ws + L.rows);
+    uint16_t* h = reinterpret_cast<uint16_t*>(ws + L.h);
+    uint16_t* q = reinterpret_cast<uint16_t*>(ws + L.q);
+    uint16_t* k = reinterpret_cast<uint16_t*>(ws + L.k);
+    uint16_t* v = reinterpret_cast<uint16_t*>(ws + L.v);
+    uint16_t* a = reinterpret_cast<uint16_t*>(ws + L.a);
+    float* part = reinterpret_cast<float*>(ws + L.part);
+    const int d = c.d;
+    const bool split = decode_skinny(c);
+    // a layer's arrays follow the previous one's
+    const size_t page_rows = (size_t)cache->n_pages * cache->n_kv_heads * cache->page_size;
+    const size_t layer_bytes = page_rows * cache->head_dim * (cache->dt == RIFTKV_BF16 ? 2 : 1);
+    RIFT_TRY(launch_kv_decode_prep(positions, n_seq, max_pages * (int64_t)cache->page_size, c.head_dim, c.rope_base, rope,
+                                   lens, rows, st));
+    for (int l = 0; l < c.n_layers; ++l) {
+        const rift_layer_weights& w = layers[l];
+        riftkv_cache kv = *cache;
+        kv.k = static_cast<unsigned char*>(kv.k) + l * layer_bytes;
+        kv.v = static_cast<unsigned char*>(kv.v) + l * layer_bytes;
+        if (kv.k_scale) kv.k_scale += l * page_rows;
+        if (kv.v_scale) kv.v_scale += l * page_rows;
+        if (l == 0)
+            RIFT_TRY(launch_rmsnorm(x_new, true, hidden_out, w.g_attn, true, h, true, n_seq, d, c.rms_eps, st));
+        else if (!split)
+            RIFT_TRY(launch_rmsnorm(hidden_out, false, nullptr, w.g_attn, true, h, true, n_seq, d, c.rms_eps, st));
+        // row i of the RoPE table is sequence i's position
+        if (split) {
+            RIFT_TRY(launch_skinny_gemm(h, static_cast<const uint16_t*>(w.wq), static_cast<const uint16_t*>(w.wk),
+                                        static_cast<const uint16_t*>(w.wv), d, n_seq, 3 * d, d, part, st));
+            RIFT_TRY(launch_skinny_qkv(part, skinny_split(3 * d, d), n_seq, d, c.head_dim, rope, rows, n_seq, q, k, v, 1, 0, st));
+        } else {
+            QkvArgs qa{};
+            qa.a = h;
+            qa.wq = static_cast<const uint16_t*>(w.wq);
+            qa.wk = static_cast<const uint16_t*>(w.wk);
+            qa.wv = static_cast<const uint16_t*>(w.wv);
+            qa.q = q;
+            qa.k = k;
+            qa.v = v;
+            qa.rope = rope;
+            qa.pos = rows;
+            qa.n_pos = n_seq;
+            qa.M = n_seq;
+            qa.d = d;
+            qa.hd = c.head_dim;
+            RIFT_TRY(launch_gemm_qkv_rope(qa, st));
+        }
+        const KvPlaces at{page_table, n_seq, max_pages, nullptr, positions, n_seq, status};
+        RIFT_TRY(launch_kv_write(kv, k, d, v, d, true, at, st));
+        const KvAttention attn{q, h, d, d, c.n_heads, true, page_table, n_seq, max_pages, lens,
+                               1.0f / sqrtf((float)c.head_dim), status, ws + L.attn};
+        RIFT_TRY(launch_kv_attention(kv, attn, st));
+        if (split)
+            RIFT_TRY(decode_after_attention_split(c, layers, l, n_seq, h, a, part, hidden_out, st));
+        else
+            RIFT_TRY(decode_after_attention(c, w, n_seq, h, a, hidden_out, st));
+    }
+    return RIFT_OK;
+}
+#undef RIFT_TRY
 
 }  // extern "C"

@@ -10,6 +10,9 @@
 
 namespace rift {
 
+// RIFT_OK, or what is wrong with the pages' shape, and with `arrays` their pointers
+rift_status kv_check_cache(const riftkv_cache* c, bool arrays);
+
 constexpr int kMaxRotary = 256;
 
 // One of the two row sets that a rotation takes: n heads a row.
@@ -38,6 +41,12 @@ hipError_t launch_kv_write(const riftkv_cache& c, const void* k, int64_t ld_k, c
                            const KvPlaces& at, hipStream_t st);
 hipError_t launch_kv_read(const riftkv_cache& c, void* k, int64_t ld_k, void* v, int64_t ld_v, bool bf16,
                           const KvPlaces& at, hipStream_t st);
+
+// What a decode step over pages needs before its layers, per sequence: the row of
+// (cos, sin) of its position [n_seq][hd / 2]; its length with the new token (0 for a negative
+// position, -1 for one past `capacity`); its own number.
+hipError_t launch_kv_decode_prep(const int* positions, int n_seq, int64_t capacity, int hd, float rope_base, float2* rope,
+                                 int* lens, int* rows, hipStream_t st);
 
 struct KvAttention {
     const void* q;

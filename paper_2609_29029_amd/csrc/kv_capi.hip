@@ -25,8 +25,11 @@ inline bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uint
 
 inline rift_status hip_status(hipError_t e) { return e == hipSuccess ? RIFT_OK : RIFT_ERR_HIP; }
 
-// The cache's shape, and with `arrays` its pointers too.
-rift_status check_cache(const riftkv_cache* c, bool arrays) {
+}  // namespace
+
+namespace rift {
+
+rift_status kv_check_cache(const riftkv_cache* c, bool arrays) {
     if (c == nullptr) return RIFT_ERR_NULL;
     const int dt = enum_bits(c->dt);
     if (dt < (int)RIFTKV_F32 || dt > (int)RIFTKV_INT8) return RIFT_ERR_DTYPE;
@@ -43,6 +46,10 @@ rift_status check_cache(const riftkv_cache* c, bool arrays) {
     return RIFT_OK;
 }
 
+}  // namespace rift
+
+namespace {
+
 bool check_table(const riftkv_cache& c, int32_t n_seq, int32_t max_pages) {
     return n_seq >= 0 && max_pages >= 0 && (int64_t)max_pages * c.page_size <= INT32_MAX;
 }
@@ -57,7 +64,7 @@ bool check_rows(const void* x, int64_t ld, int64_t width, rift_dtype dt) {
 rift_status check_places(const riftkv_cache* cache, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                          const rift_dtype& dt, const int32_t* table, int32_t n_seq, int32_t max_pages,
                          const int32_t* positions, int32_t rows, int32_t* status) {
-    const rift_status cs = check_cache(cache, true);
+    const rift_status cs = kv_check_cache(cache, true);
     if (cs != RIFT_OK) return cs;
     if (!rows_dt_valid(dt)) return RIFT_ERR_DTYPE;
     if (rows < 0 || !check_table(*cache, n_seq, max_pages)) return RIFT_ERR_SHAPE;
@@ -182,7 +189,7 @@ bool attention_shape(const riftkv_cache& c, int32_t n_heads, int32_t n_seq, int3
 }  // namespace
 
 size_t riftkv_attention_workspace_size(const riftkv_cache* cache, int32_t n_heads, int32_t n_seq, int32_t max_pages) {
-    if (check_cache(cache, false) != RIFT_OK || !attention_shape(*cache, n_heads, n_seq, max_pages)) return 0;
+    if (kv_check_cache(cache, false) != RIFT_OK || !attention_shape(*cache, n_heads, n_seq, max_pages)) return 0;
     return kv_attention_workspace(*cache, n_heads, n_seq, max_pages);
 }
 
@@ -190,7 +197,7 @@ rift_status riftkv_attention(const riftkv_cache* cache, const void* q, int64_t l
                              const int32_t* page_table, int32_t n_seq, int32_t max_pages, const int32_t* lens,
                              float scale, void* out, int64_t ld_out, int32_t* status, void* workspace, size_t ws_bytes,
                              rift_stream stream) {
-    const rift_status cs = check_cache(cache, true);
+    const rift_status cs = kv_check_cache(cache, true);
     if (cs != RIFT_OK) return cs;
     if (!rows_dt_valid(dt) || (dt == RIFT_BF16 && cache->dt == RIFTKV_F32)) return RIFT_ERR_DTYPE;
     if (!attention_shape(*cache, n_heads, n_seq, max_pages)) return RIFT_ERR_SHAPE;

@@ -171,6 +171,18 @@ rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int rows,
     }
 }
 
+// A sequence a workgroup.  The angles are the prefill's, bit for bit.
+__global__ void __launch_bounds__(64)
+decode_prep_kernel(const int* __restrict__ positions, int64_t capacity, int hd, double base, float2* __restrict__ rope,
+                   int* __restrict__ lens, int* __restrict__ rows) {
+    const int i = blockIdx.x, pos = positions[i], half = hd / 2;
+    if (threadIdx.x < half) rope[(size_t)i * half + threadIdx.x] = rope_entry(max(pos, 0), threadIdx.x, hd, base);
+    if (threadIdx.x == 0) {
+        lens[i] = pos < 0 ? 0 : pos >= capacity ? -1 : pos + 1;
+        rows[i] = i;
+    }
+}
+
 // ---------------------------------------------------------------- pages
 
 // Index of (page, head 0, row in page) among the pages' rows; -1 where the row is
@@ -420,6 +432,13 @@ hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const
     };
     if (bf16) interleaved ? launch(rope_kernel<bf16_t, true>) : launch(rope_kernel<bf16_t, false>);
     else interleaved ? launch(rope_kernel<float, true>) : launch(rope_kernel<float, false>);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_decode_prep(const int* positions, int n_seq, int64_t capacity, int hd, float rope_base, float2* rope,
+                                 int* lens, int* rows, hipStream_t st) {
+    hipLaunchKernelGGL(decode_prep_kernel, dim3((unsigned)n_seq), dim3(64), 0, st, positions, capacity, hd, (double)rope_base,
+                       rope, lens, rows);
     return hipGetLastError();
 }
 

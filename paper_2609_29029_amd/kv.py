@@ -9,14 +9,15 @@ of a call are on one device, which need not be the current one."""
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
+from typing import Optional, Sequence
 
-from ._lib import RIFT_BF16, RIFT_F32, _check, load
+from ._lib import RIFT_BF16, RIFT_F32, LayerWeights, ModelCfg, _check, layer_struct, load
 
 RIFTKV_F32, RIFTKV_BF16, RIFTKV_FP8, RIFTKV_INT8 = 0, 1, 2, 3
 # Every symbol include/rift_kv.h declares, in declaration order.
 KV_EXPORTS = ("riftkv_abi_version", "riftkv_rope_freqs", "riftkv_rope", "riftkv_write", "riftkv_read",
-              "riftkv_attention_workspace_size", "riftkv_attention")
+              "riftkv_attention_workspace_size", "riftkv_attention", "riftkv_decode_workspace_size",
+              "riftkv_decode_step")
 ROPE_SCALINGS = ("none", "linear", "base", "ramp", "bands")
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 
@@ -58,6 +59,10 @@ def _load() -> ctypes.CDLL:
         L.riftkv_attention_workspace_size.argtypes = [P, I32, I32, I32]
         L.riftkv_attention.restype = I32
         L.riftkv_attention.argtypes = [P, P, I64, I32, I32, P, I32, I32, P, F32, P, I64, P, P, SZ, P]
+        L.riftkv_decode_workspace_size.restype = SZ
+        L.riftkv_decode_workspace_size.argtypes = [P, P, I32, I32]
+        L.riftkv_decode_step.restype = I32
+        L.riftkv_decode_step.argtypes = [P, P, P, P, P, I32, I32, P, P, P, P, SZ, P]
         _lib = L
     return _lib
 
@@ -126,7 +131,9 @@ def _call(name, device, fn, *args):
 
 # ----------------------------------------------------------------------------- the pages
 class KvCache:
-    """One layer's pages, as riftkv_cache made them: what the calls take."""
+    """One layer's pages, or several layers', as riftkv_cache made them: what the calls
+    take.  riftkv_decode_step goes through all layers, the others act on the first;
+    layer(l) is layer l on its own."""
 
     def __init__(self, k, v, k_scale, v_scale):
         _load()
@@ -134,27 +141,35 @@ class KvCache:
         dt = _STORES.get(k.dtype)
         if dt is None:
             raise TypeError(f"k: unsupported storage dtype {k.dtype}")
-        if k.dim() != 4:
-            raise ValueError("k: expected [n_pages][n_kv_heads][page_size][head_dim]")
         shape = tuple(k.shape)
+        if len(shape) not in (4, 5) or 0 in shape:
+            raise ValueError("k: expected [n_pages][n_kv_heads][page_size][head_dim], or several layers of these")
         scaled = dt in (RIFTKV_FP8, RIFTKV_INT8)
         if scaled != (k_scale is not None) or scaled != (v_scale is not None):
             raise ValueError("k_scale and v_scale go with 8-bit pages, and only with them")
         p = [_dense(k, k.dtype, shape, dev, "k"), _dense(v, k.dtype, shape, dev, "v"), None, None]
         if scaled:
-            p[2] = _dense(k_scale, torch.uint8, shape[:3], dev, "k_scale")
-            p[3] = _dense(v_scale, torch.uint8, shape[:3], dev, "v_scale")
+            p[2] = _dense(k_scale, torch.uint8, shape[:-1], dev, "k_scale")
+            p[3] = _dense(v_scale, torch.uint8, shape[:-1], dev, "v_scale")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.device, self.dt = dev, dt
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
-        self.struct = _CacheStruct(*p, shape[0], shape[2], shape[1], shape[3], dt)
+        self.n_layers = shape[0] if len(shape) == 5 else 1
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape[-4:]
+        self.struct = _CacheStruct(*p, shape[-4], shape[-2], shape[-3], shape[-1], dt)
         self.ref = ctypes.byref(self.struct)
+
+    def layer(self, l: int) -> "KvCache":
+        if self.k.dim() == 4:
+            if l != 0:
+                raise IndexError(f"layer {l} of 1")
+            return self
+        return KvCache(*(None if t is None else t[l] for t in (self.k, self.v, self.k_scale, self.v_scale)))
 
 
 def riftkv_cache(k, v, k_scale=None, v_scale=None) -> KvCache:
-    """A handle on pages k, v [n_pages][n_kv_heads][page_size][head_dim] (bf16, f32,
-    float8_e4m3fn or int8; 8-bit ones with scale bytes [n_pages][n_kv_heads][page_size],
-    uint8).  It keeps the tensors; make it once."""
+    """A handle on pages k, v [n_pages][n_kv_heads][page_size][head_dim], or [n_layers] of
+    these (bf16, f32, float8_e4m3fn or int8; 8-bit ones with scale bytes
+    [n_pages][n_kv_heads][page_size], uint8).  It keeps the tensors; make it once."""
     return KvCache(k, v, k_scale, v_scale)
 
 
@@ -255,3 +270,31 @@ def riftkv_attention(cache: KvCache, q, page_table, lens, out, workspace, status
     ws = _dense(workspace, torch.uint8, None, dev, "workspace")
     _call("riftkv_attention", dev, _lib.riftkv_attention, cache.ref, pq, ldq, shape[1], dt, table, n_seq, max_pages, n,
           cache.head_dim ** -0.5 if scale is None else scale, po, ldo, word, ws, workspace.numel(), _stream(stream, dev))
+
+
+# ----------------------------------------------------------------------------- decode
+def riftkv_decode_workspace_size(cfg: ModelCfg, cache: KvCache, n_seq: int, max_pages: int) -> int:
+    return int(_load().riftkv_decode_workspace_size(ctypes.byref(cfg), cache.ref, int(n_seq), int(max_pages)))
+
+
+def riftkv_decode_step(cfg: ModelCfg, layers: Sequence[dict], x_new, cache: KvCache, page_table, positions, hidden_out,
+                       workspace, status, stream=None) -> None:
+    """One generated token of every sequence through the decoder layers, its keys and
+    values in pages (include/rift_kv.h).  x_new [n_seq][d] bf16; cache of cfg.n_layers
+    layers; positions [n_seq] i32: the tokens each sequence holds already."""
+    dev = cache.device
+    if len(layers) != cfg.n_layers or cache.n_layers != cfg.n_layers:
+        raise ValueError("need one weight set and one layer of pages per layer")
+    for w in layers:
+        for n, t in w.items():
+            _dense(t, torch.bfloat16, None, dev, n)
+    n_seq, max_pages = page_table.shape
+    x = _dense(x_new, torch.bfloat16, (n_seq, cfg.d), dev, "x_new")
+    out = _dense(hidden_out, torch.float32, (n_seq, cfg.d), dev, "hidden_out")
+    table = _dense(page_table, torch.int32, None, dev, "page_table")
+    pos = _dense(positions, torch.int32, (n_seq,), dev, "positions")
+    word = _dense(status, torch.int32, (1,), dev, "status")
+    ws = _dense(workspace, torch.uint8, None, dev, "workspace")
+    arr = (LayerWeights * max(1, len(layers)))(*[layer_struct(w) for w in layers])
+    _call("riftkv_decode_step", dev, _lib.riftkv_decode_step, ctypes.byref(cfg), arr, x, cache.ref, table, n_seq, max_pages,
+          pos, out, word, ws, workspace.numel(), _stream(stream, dev))

@@ -168,6 +168,39 @@ def test_rope_frequencies(R):
     assert mid.sum() >= 5 and np.allclose(g[mid], f5[mid] * s + f5[mid] / 8 * (1 - s), rtol=1e-13)
 
 
+def test_decode_step_is_checked(R, L):
+    layer = R.LayerWeights(*[FAKE] * 9)
+    bad_layer = R.LayerWeights(*([FAKE] * 8 + [None]))
+    model = dict(d=512, n_heads=4, head_dim=128, ffn=1408, n_layers=1, rms_eps=1e-6, rope_base=1e4, dt_code=R.RIFT_BF16)
+
+    def call(c=None, w=layer, over=None, x=FAKE, table=FAKE, n_seq=3, pages=4, pos=FAKE, out=FAKE, status=FAKE, ws=FAKE,
+             wsb=1 << 30):
+        cfg = R.model_cfg(**dict(model, **(over or {})))
+        return L.riftkv_decode_step(ctypes.byref(cfg), None if w is None else ctypes.byref(w), x,
+                                    ctypes.byref(cache() if c is None else c), table, n_seq, pages, pos, out, status, ws,
+                                    wsb, None)
+
+    for over, status in BAD_CACHES:
+        assert call(cache(**over)) in (status, 2), over      # (other heads than the model's: a shape too)
+    for bad in (dict(x=None), dict(w=None), dict(w=bad_layer), dict(table=None), dict(pos=None), dict(out=None),
+                dict(status=None), dict(ws=None)):
+        assert call(**bad) == 1, bad
+    assert call(cache(heads=2)) == 2 and call(cache(hd=64)) == 2
+    for bad in (dict(n_seq=-1), dict(n_seq=65536), dict(pages=-1), dict(pages=1 << 27)):
+        assert call(**bad) == 2, bad
+    assert call(cache(dt=0, ks=None, vs=None)) == 8                       # float32 pages
+    assert call(over=dict(dt_code=R.RIFT_F32)) == 8
+    assert call(over=dict(d=500)) == 2
+    assert call(ws=FAKE + 16) == 5 and call(wsb=4096) == 5
+    assert call(n_seq=0) == 0 and call(over=dict(n_layers=0)) == 0
+    cfg = R.model_cfg(**model)
+    c = cache()
+    size = lambda n, p: L.riftkv_decode_workspace_size(ctypes.byref(cfg), ctypes.byref(c), n, p)
+    assert size(-1, 4) == 0 and size(4, -1) == 0
+    sizes = [size(n, 64) for n in (0, 1, 2, 9, 60, 700, 5000)]
+    assert sizes == sorted(sizes) and size(9, 64) <= size(9, 640)
+
+
 @pytest.mark.parametrize("over, status", [
     (dict(rotary_dim=0), 2), (dict(rotary_dim=7), 2), (dict(rotary_dim=258), 2), (dict(base=1.0), 7),
     (dict(base=float("inf")), 7), (dict(scaling="linear", factor=0.5), 7), (dict(scaling="linear", factor=float("nan")), 7),
