@@ -393,15 +393,16 @@ attention_kernel(AttnParams p) {
             }
         };
 
+        // the next tile's pages are asked for with the first one's, and from then on a tile ahead
         Pages cur_pages = pages_at(cur);
-        load_k(cur, cur_pages, true);
-        load_v(cur, cur_pages, true);
         Place nxt = cur;
         Pages nxt_pages = cur_pages;
         if (left > 1) {
             nxt = after(cur);
             nxt_pages = pages_at(nxt);
         }
+        load_k(cur, cur_pages, true);
+        load_v(cur, cur_pages, true);
 
         bf16x8_t qf[F32 ? 1 : NQ][F32 ? 1 : HD / 32];
         float qs[F32 ? HD / 4 : 1];
@@ -740,7 +741,7 @@ join_kernel(AttnParams p) {
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     if (pg < PG) {
-        constexpr int U = 4;   // parts in flight
+        constexpr int U = 2;   // parts in flight
         for (int i = pg; i < parts; i += U * PG) {
             f32x4_t x[U];
             float2 ml[U];
