@@ -177,9 +177,9 @@ RIFT_API size_t riftkv_attention_workspace_size(const riftkv_cache* cache, int32
  * query head h with key-value head h / (n_heads / n_kv_heads).  Scores, softmax and
  * sums in float32; a sequence of length 0 gives zeros.
  * q        [n_seq][n_heads][head_dim] dt, sequences ld_q elements apart
- * out      [n_seq][n_heads][head_dim] dt, ld_out apart
+ * out      [n_seq][n_heads][head_dim] dt, ld_out apart; overlaps no input
  * lens     [n_seq] i32 in [0, max_pages * page_size]
- * scale    finite (1/sqrt(head_dim) as a rule)
+ * scale    1/sqrt(head_dim) as a rule; it and its product with log2(e) are finite
  * A length out of range, or a page outside [0, n_pages) among a sequence's tokens,
  * sets the status and makes that sequence's (with a page: those heads') output NaN.
  * What lies in a page past a sequence's length has no effect, whatever its bits.

@@ -202,7 +202,7 @@ rift_status riftkv_attention(const riftkv_cache* cache, const void* q, int64_t l
     if (!rows_dt_valid(dt) || (dt == RIFT_BF16 && cache->dt == RIFTKV_F32)) return RIFT_ERR_DTYPE;
     if (!attention_shape(*cache, n_heads, n_seq, max_pages)) return RIFT_ERR_SHAPE;
     if (!kv_attention_counts(*cache, n_heads, n_seq, max_pages)) return RIFT_ERR_UNSUPPORTED;
-    if (!isfinite(scale)) return RIFT_ERR_NONFINITE;
+    if (!isfinite(scale * 1.4426950408889634f)) return RIFT_ERR_NONFINITE;   // the base-2 exponent's
     if (status == nullptr || workspace == nullptr) return RIFT_ERR_NULL;
     if (misaligned(workspace, 256) || ws_bytes < kv_attention_workspace(*cache, n_heads, n_seq, max_pages))
         return RIFT_ERR_WORKSPACE;

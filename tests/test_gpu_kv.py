@@ -490,6 +490,78 @@ def test_decode_steps_in_a_graph(R, store):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
+def test_offsets_past_32_bits(R):
+    """Pages at the end of a pool whose arrays pass 4 GB (2^32 bytes, 2^31 values): written, read and attended to."""
+    n_pages, n_kv, page, hd = 140_000, 8, 16, 128
+    k = torch.empty(n_pages, n_kv, page, hd, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    assert k.numel() > 2 ** 31
+    cache = R.riftkv_cache(k, v)
+    n = 100
+    table = torch.arange(n_pages - 1, n_pages - 1 - 7, -1, dtype=torch.int32, device="cuda")[None].contiguous()
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    a, b = randn(1, n, n_kv, hd), randn(2, n, n_kv, hd)
+    R.riftkv_write(cache, a, b, table, pos, status, seq_ids=ids)
+    ko, vo = torch.empty_like(a), torch.empty_like(b)
+    R.riftkv_read(cache, table, pos, ko, vo, status, seq_ids=ids)
+    q = randn(3, 1, 32, hd)
+    out = torch.empty_like(q)
+    ws = torch.empty(R.riftkv_attention_workspace_size(cache, 1, 32, 7), dtype=torch.uint8, device="cuda")
+    R.riftkv_attention(cache, q, table, torch.tensor([n], dtype=torch.int32, device="cuda"), out, ws, status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and torch.equal(ko, a) and torch.equal(vo, b)
+    assert torch.equal(k[n_pages - 1, :, 3], a[3]) and torch.equal(v[n_pages - 7, :, 2], b[98])
+    ref, err = attend(q[0].double().cpu(), a.double().cpu(), b.double().cpu(), hd ** -0.5)
+    got = out[0].double().cpu()
+    # (weights in two bf16 terms: 2^-16 of each, of values up to 5)
+    assert bool(((got - ref).abs() <= err + 2.0 ** -8 * ref.abs() * 1.001 + 2.0 ** -16 * 5).all())
+
+
+def test_calls_on_two_streams_at_once(R):
+    """Each with its own workspace and outputs, over the same pages: as one after the other."""
+    lens = [3000, 17, 900]
+    P = filled(R, "fp8", 2, 128, 16, lens)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    qs = [randn(40 + i, 3, 2 * g, 128) for i, g in enumerate((4, 16))]
+    size = [R.riftkv_attention_workspace_size(P.cache, 3, q.shape[1], P.table.shape[1]) for q in qs]
+    want = [attention(R, P, q, n) for q in qs]
+    ws = [torch.empty(s, dtype=torch.uint8, device="cuda") for s in size]
+    outs = [torch.empty_like(q) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, o, w, st in zip(qs, outs, ws, streams):
+            attention(R, P, q, n, out=o, ws=w, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, outs)) and int(P.status) == 0
+
+
+@pytest.mark.parametrize("store, dt, group, lens", [("bf16", "bf16", 16, [5000, 70]), ("int8", "f32", 16, [2100] * 3),
+                                                    ("f32", "f32", 17, [40, 1500]), ("fp8", "bf16", 40, [64] * 40)])
+def test_attention_in_a_graph(R, store, dt, group, lens):
+    """Large groups (more than 64 KB of LDS), captured and replayed with lengths that change between replays."""
+    P = filled(R, store, 1, 128, 16, lens, dtype=TYPES[dt])
+    q = randn(7, len(lens), group, 128, dtype=TYPES[dt])
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    ws = torch.empty(R.riftkv_attention_workspace_size(P.cache, len(lens), group, P.table.shape[1]), dtype=torch.uint8, device="cuda")
+    attention(R, P, q, n, out=out, ws=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        attention(R, P, q, n, out=out, ws=ws)
+    for cut in (0, 1, 33, 0):
+        n.copy_(torch.tensor([max(0, x - cut) for x in lens], dtype=torch.int32))
+        out.fill_(7)
+        g.replay()
+        torch.cuda.synchronize()
+        check(P, q, out, [max(0, x - cut) for x in lens])
+        assert torch.equal(out, attention(R, P, q, n))
+    assert int(P.status) == 0
+
+
 def test_refusals_leave_the_outputs(R):
     P = filled(R, "bf16", 2, 64, 16, [20])
     q = randn(2, 1, 4, 64)
