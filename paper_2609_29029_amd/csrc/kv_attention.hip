@@ -810,12 +810,13 @@ int workgroups(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pa
 //   128 of 300 to 512                15.9 / 22.1 14.5 11.9    512 of 64  11.1 /  6.2  6.7  7.2
 //   1,024 of 32 to 512, fp8          25.6 / 28.4 20.5 24.5    of 1,024, 4 waves  48.4 / 44.7
 //   2,048 of 30 to 200, 64 dims      22.7 / 16.0 16.1 20.0    2,048 of 256  48.1 / 44.0 46.9 47.1
+//   2,400 of 1 to 400, int8          39.1 / 39.8 36.8 39.9
 //   4,096 of 64                      30.6 / 25.8 29.4 38.3    16,384 of 64  93.8 / 88.8 92.2 129.8
 //   3,200 of 131 to 643             110.1 / 106.0 106.5 104.4
 int whole_waves(const riftkv_cache& c, int64_t heads, int64_t max_pages) {
     const int64_t most = max_pages * c.page_size;
     if (most > 1024 || (most > 512 && heads < 256)) return 0;
-    if (most <= 64 || (most <= 512 && heads >= 2048)) return 1;
+    if (most <= 64 || (most <= 256 && heads >= 2048)) return 1;
     return most <= 128 || (most <= 512 && heads >= 1024) ? 2 : 4;
 }
 

@@ -120,7 +120,7 @@ def _stream(stream, device):
 
 def _call(name, device, fn, *args):
     """fn with `device` as the current one."""
-    if device == torch.cuda.current_device():
+    if device == torch._C._cuda_getDevice():
         st = fn(*args)
     else:
         with torch.cuda.device(device):
@@ -198,26 +198,31 @@ def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "h
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
-    dev, dt, rows, hd = _device_of(x, "rows"), _row_type(x, "rows"), x.shape[0], x.shape[-1]
-    args = []
-    for t, o, name in ((q, q_out, "q"), (k, k_out, "k")):
-        if t is None:
-            if o is not None:
-                raise ValueError(f"{name}_out without {name}")
-            args += [None, 0, 0, None, 0]
-            continue
-        if t.dim() != 3:
-            raise ValueError(f"{name}: expected [rows][heads][head_dim]")
-        shape = (rows, t.shape[1], hd)
-        p, ld = _rows(t, x.dtype, shape, dev, name)
-        po, ldo = (p, ld) if o is None else _rows(o, x.dtype, shape, dev, name + "_out")
-        args += [p, ld, shape[1], po, ldo]
+    if x.dim() != 3:
+        raise ValueError("rows: expected [rows][heads][head_dim]")
+    dev, dtype = _device_of(x, "rows"), x.dtype
+    dt, (rows, _, hd) = _row_type(x, "rows"), x.shape
+    pq = lq = nq = poq = loq = pk = lk = nk = pok = lok = 0
+    if q is not None:
+        nq = q.shape[1]
+        pq, lq = _rows(q, dtype, (rows, nq, hd), dev, "q")
+        poq, loq = (pq, lq) if q_out is None else _rows(q_out, dtype, q.shape, dev, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if k is not None:
+        if k.dim() != 3:
+            raise ValueError("rows: expected [rows][heads][head_dim]")
+        nk = k.shape[1]
+        pk, lk = _rows(k, dtype, (rows, nk, hd), dev, "k")
+        pok, lok = (pk, lk) if k_out is None else _rows(k_out, dtype, k.shape, dev, "k_out")
+    elif k_out is not None:
+        raise ValueError("k_out without k")
     if freqs.dtype.char != "d" or not freqs.flags.c_contiguous or freqs.size == 0:
         raise TypeError("freqs: expected a contiguous float64 array")
     # (an array's own .ctypes takes three times as long)
     fp = ctypes.byref(ctypes.c_double.from_buffer(freqs)) if freqs.flags.writeable else freqs.ctypes.data
     pos = _dense(positions, torch.int32, (rows,), dev, "positions")
-    _call("riftkv_rope", dev, L.riftkv_rope, *args, dt, pos, rows, hd, 2 * freqs.size, ROPE_LAYOUTS[layout],
+    _call("riftkv_rope", dev, L.riftkv_rope, pq, lq, nq, poq, loq, pk, lk, nk, pok, lok, dt, pos, rows, hd, 2 * freqs.size, ROPE_LAYOUTS[layout],
           fp, magnitude, _stream(stream, dev))
 
 
