@@ -98,75 +98,73 @@ rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int h
     for (int j = rotary_dim + threadIdx.x; j < head_dim; j += 64) store_f32<T>(r.y, y0 + j, load_f32<T>(r.x, x0 + j));
 }
 
-// Eights of elements: a workgroup takes `per` heads of `tile` rows.  A head's items are,
-// in the half layout, rotary_dim / 16 pairs of eights, then the eights that are
-// copied; interleaved, head_dim / 8 eights of four pairs each or copied.
+// Eights of elements: a workgroup takes `per` heads of a row.  (Several rows a workgroup
+// save launches of workgroups and lose more in the wait for the first sines: 16,384 rows of 40 heads,
+// half layout, 57.5 us, in twos 60.6, in fours 63.6.)  A head's items are, in the half
+// layout, rotary_dim / 16 pairs of eights, then the eights that are copied; interleaved,
+// head_dim / 8 eights of four pairs each or copied.
 template <typename T, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads)
-rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int rows, int tile, int per, int head_dim,
-            int rotary_dim, RopeFreqs freqs, float magnitude) {
-    extern __shared__ __align__(16) float2 turns[];   // [tile][rotary_dim / 2]
-    const int row0 = blockIdx.x * tile, n_rows = min(tile, rows - row0);
-    const int heads = q.n + k.n, h0 = blockIdx.y * per, n_heads = min(per, heads - h0);
+rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int per, int head_dim, int rotary_dim,
+            RopeFreqs freqs, float magnitude) {
+    __shared__ float2 turns[kMaxRotary / 2];
+    const int row = blockIdx.x, heads = q.n + k.n, h0 = blockIdx.y * per;
     const int half = rotary_dim / 2;
     const int turned = INTERLEAVED ? rotary_dim / 8 : rotary_dim / 16, items = turned + (head_dim - rotary_dim) / 8;
-    for (int i = threadIdx.x; i < n_rows * half; i += kThreads) {
-        const int r = i / half, j = i - r * half;
-        turns[i] = rope_turn(positions[row0 + r], freqs.f[j], magnitude);
-    }
-    __syncthreads();
-    // item v of head h of row r
-    int v = threadIdx.x % items, h = threadIdx.x / items;
-    int r = h / n_heads;
-    h -= r * n_heads;
-    const int dv = kThreads % items, dh = kThreads / items;
-    while (r < n_rows) {
-        const int head = h0 + h;
-        const bool is_q = head < q.n;
+    // item v of head h; its values are asked for before they are needed, the first before
+    // the sines
+    int v = threadIdx.x % items, h = h0 + threadIdx.x / items;
+    const int dv = kThreads % items, dh = kThreads / items, end = min(h0 + per, heads);
+    Eight<T> xa, xb;
+    void* y;
+    size_t at;
+    auto load = [&]() __attribute__((always_inline)) {
+        const bool is_q = h < q.n;
         const void* x = is_q ? q.x : k.x;
-        void* y = is_q ? q.y : k.y;
-        const size_t hoff = (size_t)(is_q ? head : head - q.n) * head_dim;
-        const size_t x0 = (size_t)(row0 + r) * (is_q ? q.ld_x : k.ld_x) + hoff;
-        const size_t y0 = (size_t)(row0 + r) * (is_q ? q.ld_y : k.ld_y) + hoff;
-        const float2* cs = turns + r * half;
-        if (v >= turned) {
-            const int e = rotary_dim + 8 * (v - turned);
-            float f[8];
-            widen_eight<T>(load_eight<T>(x, x0 + e), f);
-            store_eight<T>(y, y0 + e, f);
-        } else if constexpr (INTERLEAVED) {
-            float f[8];
-            widen_eight<T>(load_eight<T>(x, x0 + 8 * v), f);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 o = rotate_pair(f[2 * j], f[2 * j + 1], cs[4 * v + j]);
-                f[2 * j] = o.x;
-                f[2 * j + 1] = o.y;
-            }
-            store_eight<T>(y, y0 + 8 * v, f);
-        } else {
-            float a[8], b[8];
-            const Eight<T> xa = load_eight<T>(x, x0 + 8 * v), xb = load_eight<T>(x, x0 + half + 8 * v);
-            widen_eight<T>(xa, a);
-            widen_eight<T>(xb, b);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float2 o = rotate_pair(a[j], b[j], cs[8 * v + j]);
-                a[j] = o.x;
-                b[j] = o.y;
-            }
-            store_eight<T>(y, y0 + 8 * v, a);
-            store_eight<T>(y, y0 + half + 8 * v, b);
-        }
+        y = is_q ? q.y : k.y;
+        const size_t hoff = (size_t)(is_q ? h : h - q.n) * head_dim;
+        const size_t from = (size_t)row * (is_q ? q.ld_x : k.ld_x) + hoff;
+        at = (size_t)row * (is_q ? q.ld_y : k.ld_y) + hoff;
+        const int e = INTERLEAVED || v < turned ? 8 * v : rotary_dim + 8 * (v - turned);
+        xa = load_eight<T>(x, from + e);
+        if (!INTERLEAVED && v < turned) xb = load_eight<T>(x, from + half + e);
+    };
+    if (h < end) load();
+    if (threadIdx.x < half) turns[threadIdx.x] = rope_turn(positions[row], freqs.f[threadIdx.x], magnitude);
+    __syncthreads();
+    while (h < end) {
+        const int v0 = v;
+        void* const y0 = y;
+        const size_t at0 = at;
+        float a[8], b[8];
+        widen_eight<T>(xa, a);
+        if constexpr (!INTERLEAVED) widen_eight<T>(xb, b);
         v += dv;
         h += dh;
         if (v >= items) {
             v -= items;
             ++h;
         }
-        while (h >= n_heads) {
-            h -= n_heads;
-            ++r;
+        if (h < end) load();
+        if (v0 >= turned) {
+            store_eight<T>(y0, at0 + (INTERLEAVED ? 8 * v0 : rotary_dim + 8 * (v0 - turned)), a);
+        } else if constexpr (INTERLEAVED) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 o = rotate_pair(a[2 * j], a[2 * j + 1], turns[4 * v0 + j]);
+                a[2 * j] = o.x;
+                a[2 * j + 1] = o.y;
+            }
+            store_eight<T>(y0, at0 + 8 * v0, a);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 o = rotate_pair(a[j], b[j], turns[8 * v0 + j]);
+                a[j] = o.x;
+                b[j] = o.y;
+            }
+            store_eight<T>(y0, at0 + 8 * v0, a);
+            store_eight<T>(y0, at0 + half + 8 * v0, b);
         }
     }
 }
@@ -419,16 +417,13 @@ hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const
         else launch(rope_any_kernel<float>);
         return hipGetLastError();
     }
-    // 4 rows of all heads a workgroup, so that the sines are worked out once a row; fewer
-    // rows, then heads, where that leaves CUs without work
-    int tile = 4, per = heads;
-    while (tile > 1 && rows / tile < 1024) tile /= 2;
-    while (per > 4 && (int64_t)rows * ((heads + per - 1) / per) < 512) per = (per + 1) / 2;
-    const dim3 grid((unsigned)((rows + tile - 1) / tile), (unsigned)((heads + per - 1) / per));
-    const size_t lds = (size_t)tile * (rotary_dim / 2) * sizeof(float2);
+    // all heads of a row a workgroup, so that its sines are worked out once, or fewer where that
+    // leaves CUs without work (32 rows of 40 heads: 2.6 us, with 512 workgroups 3.4)
+    int per = heads;
+    while (per > 4 && (int64_t)rows * ((heads + per - 1) / per) < 256) per = (per + 1) / 2;
+    const dim3 grid((unsigned)rows, (unsigned)((heads + per - 1) / per));
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, q, k, positions, rows, tile, per, head_dim, rotary_dim,
-                           freqs, magnitude);
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, q, k, positions, per, head_dim, rotary_dim, freqs, magnitude);
     };
     if (bf16) interleaved ? launch(rope_kernel<bf16_t, true>) : launch(rope_kernel<bf16_t, false>);
     else interleaved ? launch(rope_kernel<float, true>) : launch(rope_kernel<float, false>);
