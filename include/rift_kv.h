@@ -143,7 +143,7 @@ RIFT_API rift_status riftkv_rope(const void* q, int64_t ld_q, int32_t n_q, void*
  * whose page is outside [0, n_pages) sets the status and is skipped.  Of two
  * rows of a call for the same place either may be there afterwards, or parts
  * of both.  f32 rows in bf16 pages are rounded to nearest even.
- * Shape rules: rows, n_seq, max_pages >= 0, max_pages * page_size <= INT32_MAX, ld >=
+ * Shape rules: rows, n_seq, max_pages >= 0, max_pages * page_size <= 2^30, ld >=
  * n_kv_heads * head_dim.  Errors: RIFT_ERR_DTYPE also for bf16 rows in f32 pages.
  */
 RIFT_API rift_status riftkv_write(const riftkv_cache* cache, const void* k, int64_t ld_k, const void* v,
@@ -181,13 +181,13 @@ RIFT_API size_t riftkv_attention_workspace_size(const riftkv_cache* cache, int32
  * lens     [n_seq] i32 in [0, max_pages * page_size]
  * scale    1/sqrt(head_dim) as a rule; it and its product with log2(e) are finite
  * A length out of range, or a page outside [0, n_pages) among a sequence's tokens,
- * sets the status and makes that sequence's (with a page: those heads') output NaN.
+ * sets the status and makes that sequence's output NaN.
  * What lies in a page past a sequence's length has no effect, whatever its bits.
  * How the keys are dealt out depends on all sequences' lengths: a result may differ in
  * its last bits between batches, never between two calls with the same ones.
  * dt bf16 with pages of bf16, fp8 or int8; dt f32 with any.
  * Shape rules: n_heads a multiple of n_kv_heads, at most 4096; 0 <= n_seq <= 65535; max_pages >=
- * 0, max_pages * page_size <= INT32_MAX.  workspace >= riftkv_attention_workspace_size
+ * 0, max_pages * page_size <= 2^30.  workspace >= riftkv_attention_workspace_size
  * bytes, 256-byte aligned; calls that may overlap in time need one each.
  */
 RIFT_API rift_status riftkv_attention(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads,

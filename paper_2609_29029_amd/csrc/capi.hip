@@ -956,7 +956,7 @@ rift_status check_kv_decode(const rift_model_cfg* cfg, const riftkv_cache* kv, i
     if (ks != RIFT_OK) return ks;
     if (cfg->dt != RIFT_BF16 || kv->dt == RIFTKV_F32) return RIFT_ERR_UNSUPPORTED;
     if (kv->n_kv_heads != cfg->n_heads || kv->head_dim != cfg->head_dim || n_seq < 0 || n_seq > 65535 || max_pages < 0 ||
-        (int64_t)max_pages * kv->page_size > INT32_MAX || (int64_t)n_seq * cfg->ffn >= (1ll << 31))
+        (int64_t)max_pages * kv->page_size > kMaxTokens || (int64_t)n_seq * cfg->ffn >= (1ll << 31))
         return RIFT_ERR_SHAPE;
     return kv_attention_counts(*kv, cfg->n_heads, n_seq, max_pages) ? RIFT_OK : RIFT_ERR_UNSUPPORTED;
 }

@@ -14,6 +14,7 @@ namespace rift {
 rift_status kv_check_cache(const riftkv_cache* c, bool arrays);
 
 constexpr int kMaxRotary = 256;
+constexpr int64_t kMaxTokens = 1 << 30;   // of a table: a tile's end is within 31 bits
 
 // One of the two row sets that a rotation takes: n heads a row.
 struct RopeRows {

@@ -21,8 +21,8 @@
 // query columns cost nothing: the bytes of keys and values bound this kernel.
 //
 // Scores, weights and sums are float32; each weight goes into the matrix product as
-// bf16 terms that add up to it (two: 2^-17 of it, three: 2^-25, for float32 rows),
-// each float32 query as three.
+// bf16 terms that add up to it (two: all but 2^-18 of it; three, for float32 rows, all but
+// 2^-27), each float32 query as three.
 #include <type_traits>
 
 #include "kv_device.h"
@@ -36,8 +36,6 @@ constexpr int kBegins = 1, kEnds = 2;     // a part holds a head's first, last t
 constexpr int kSplitWaves = 4;            // of a workgroup, where heads are split over workgroups
 constexpr int kMaxWgs = 512;              // two workgroups a CU
 constexpr int kFewSeqs = 256;             // sequences whose lengths a wave holds in registers
-
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 struct AttnParams {
     const void* q;

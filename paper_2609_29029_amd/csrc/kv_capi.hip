@@ -51,7 +51,7 @@ rift_status kv_check_cache(const riftkv_cache* c, bool arrays) {
 namespace {
 
 bool check_table(const riftkv_cache& c, int32_t n_seq, int32_t max_pages) {
-    return n_seq >= 0 && max_pages >= 0 && (int64_t)max_pages * c.page_size <= INT32_MAX;
+    return n_seq >= 0 && max_pages >= 0 && (int64_t)max_pages * c.page_size <= kMaxTokens;
 }
 
 // A row set [rows][heads * head_dim], `ld` elements apart (16 bytes hold 8 or 4)

@@ -217,6 +217,8 @@ def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "h
         pok, lok = (pk, lk) if k_out is None else _rows(k_out, dtype, k.shape, dev, "k_out")
     elif k_out is not None:
         raise ValueError("k_out without k")
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout: one of {tuple(ROPE_LAYOUTS)}")
     if freqs.dtype.char != "d" or not freqs.flags.c_contiguous or freqs.size == 0:
         raise TypeError("freqs: expected a contiguous float64 array")
     # (an array's own .ctypes takes three times as long)

@@ -66,7 +66,7 @@ def test_rows_are_checked(L, name):
     assert getattr(L, name)(None, FAKE, 512, FAKE, 512, 1, FAKE, 4, 2, None, FAKE, 5, FAKE, None) == 1
     for over in (dict(k=None), dict(v=None), dict(table=None), dict(pos=None), dict(status=None)):
         assert call(**over) == 1, over
-    for over in (dict(rows=-1), dict(n_seq=-1), dict(pages=-1), dict(pages=1 << 27), dict(ldk=511), dict(ldv=508),
+    for over in (dict(rows=-1), dict(n_seq=-1), dict(pages=-1), dict(pages=1 << 27), dict(pages=(1 << 26) + 1), dict(ldk=511), dict(ldv=508),
                  dict(ldk=516), dict(k=FAKE + 2)):
         assert call(**over) == 2, over
     assert call(dt=2) == 3
@@ -93,11 +93,12 @@ def test_attention_is_checked(L):
     for over in (dict(q=None), dict(out=None), dict(lens=None), dict(table=None), dict(status=None), dict(ws=None)):
         assert call(**over) == 1, over
     for over in (dict(heads=6), dict(heads=0), dict(heads=4100), dict(n_seq=-1), dict(n_seq=65536), dict(pages=-1),
-                 dict(pages=1 << 27), dict(ldq=1016), dict(ldo=1028), dict(out=FAKE + 8)):
+                 dict(pages=1 << 27), dict(pages=(1 << 26) + 1), dict(ldq=1016), dict(ldo=1028), dict(out=FAKE + 8)):
         assert call(**over) == 2, over
     assert call(dt=3) == 3
     assert call(cache(dt=0, ks=None, vs=None)) == 3                     # bf16 queries on f32 pages
     assert call(scale=float("nan")) == 7 and call(scale=float("inf")) == 7
+    assert call(n_seq=65535, pages=1 << 26) == 8                        # more tiles than a wave counts
     assert call(ws=FAKE + 16) == 5 and call(wsb=16) == 5
     assert call(n_seq=0, q=None, out=None, lens=None, table=None) == 0
 
