@@ -812,15 +812,15 @@ int workgroups(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pa
 // scan of the lengths and the join, which short heads do not repay; a head taken whole is
 // read at one CU's rate, so it is bounded by what the table can hold.  In us, split / whole
 // with 1, 2 and 4 waves, bf16 of 128 dimensions and groups of 4 if not said otherwise:
-//   8 heads of 256 tokens         7.9 / 10.2  7.0  5.5    of 1,024      9.0 / 30.5 22.3 14.5
-//   128 of 300 to 512            13.2 / 21.9 13.3  9.7    of 1,024     18.0 / 41.7 24.4 17.2
-//   512 of 64                     9.3 /  5.4  5.8  5.9    of 1,024     45.9 / 49.5 43.2 43.5
-//   256 of 300 to 1,024          23.7 / 42.2 24.9 19.3    512, fp8     26.3 / 48.8 29.9 22.9
-//   1,024 of 32 to 512, fp8      25.2 / 28.7 20.4 22.6    3,200 of 50 to 1,024  151.5 / 154 151 148
-//   2,048 of 30 to 200, 64 dims  22.0 / 15.3 15.3 17.0    of 256       46.0 / 42.9 46.8 44.6
-//   2,400 of 1 to 400, int8      40.2 / 39.9 36.3 37.0    4,096 of 64  29.0 / 25.0 26.7 31.1
-//   16,384 of 64, group 1        92.3 / 88.6 90.5 102.8   3,200 of 131 to 643, group 1  109.7 / 106.3 106.1 104.1
-//   32 of 647, group 1            9.9 / 22.0 14.4 10.5    512 of 512 to 2,048, group 1   60.2 / 89.1 61.4  57.8
+//   8 heads of 256 tokens         8.2 / 11.3  7.5  5.9    of 1,024      9.2 / 30.1 22.0 14.8
+//   128 of 300 to 512            13.1 / 22.3 13.6  9.9    of 1,024     17.8 / 42.5 24.9 17.3
+//   512 of 64                     9.4 /  5.4  5.9  6.0    of 1,024     45.8 / 50.7 43.2 43.0
+//   256 of 300 to 1,024          23.2 / 43.2 25.6 19.2    512, fp8     25.6 / 48.7 31.2 21.7
+//   1,024 of 32 to 512, fp8      24.6 / 28.0 20.6 22.3    3,200 of 50 to 1,024  148 / 153 146 141
+//   2,048 of 30 to 200, 64 dims  22.0 / 15.0 14.9 17.3    of 256       47.4 / 44.3 46.6 46.8
+//   2,400 of 1 to 400, int8      39.7 / 40.7 35.7 36.3    4,096 of 64  28.7 / 24.9 27.8 37.8
+//   16,384 of 64, group 1        91.4 / 84.1 89.4 133.7   3,200 of 131 to 643, group 1  106.8 / 104.8 101.5 97.4
+//   32 of 647, group 1            9.9 / 22.4 14.6 10.7    512 of 512 to 2,048, group 1   59.2 / 90.0 61.4  57.2
 int whole_waves(const riftkv_cache& c, int64_t heads, int64_t max_pages) {
     const int64_t most = max_pages * c.page_size;
     if (most > 1024 || (most > 512 && heads < 128)) return 0;
