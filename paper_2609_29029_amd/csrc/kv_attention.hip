@@ -825,7 +825,8 @@ int whole_waves(const riftkv_cache& c, int64_t heads, int64_t max_pages) {
     const int64_t most = max_pages * c.page_size;
     if (most > 1024 || (most > 512 && heads < 128)) return 0;
     if (most <= 64 || (most <= 256 && heads >= 2048)) return 1;
-    return most <= 128 || (most <= 512 && heads >= 1024) ? 2 : 4;
+    const int waves = most <= 128 || (most <= 512 && heads >= 1024) ? 2 : 4;
+    return heads * waves < (1 << 26) ? waves : 1;   // a launch has less than 2^32 threads (at most 65,535 x 1,024 heads)
 }
 
 }  // namespace

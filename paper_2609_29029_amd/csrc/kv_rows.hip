@@ -11,6 +11,7 @@ namespace rift {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kMostThreads = (1ll << 32) - 1;   // of a launch along x: more rows take several launches
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
@@ -257,6 +258,7 @@ struct MoveParams {
     int64_t ld[2];
     int n_pages, shift, n_kv;
     int tile_log2, per;          // rows and heads of a workgroup
+    int row0;                    // first row of the launch
     KvPlaces at;
 };
 constexpr int kTileRows = 16, kUnroll = 4;
@@ -267,7 +269,7 @@ move_kernel(MoveParams p) {
     constexpr int G = HD / 8, E = DT == RIFTKV_F32 ? 4 : DT == RIFTKV_BF16 ? 2 : 1;
     constexpr bool SCALED = E == 1;
     __shared__ int64_t places[kTileRows];
-    const int which = blockIdx.z, row0 = blockIdx.x << p.tile_log2, h0 = blockIdx.y * p.per;
+    const int which = blockIdx.z, row0 = p.row0 + (blockIdx.x << p.tile_log2), h0 = blockIdx.y * p.per;
     const int n_heads = min(p.per, p.n_kv - h0);
     unsigned char* pages = p.pages[which];
     uint8_t* scales = p.scales[which];
@@ -375,10 +377,16 @@ hipError_t launch_move(const riftkv_cache& c, const void* k, int64_t ld_k, const
     const unsigned splits = (c.n_kv_heads + p.per - 1) / p.per;
     p.tile_log2 = WRITE ? 3 : 4;
     while (p.tile_log2 > 0 && (int64_t)(at.rows >> p.tile_log2) * splits * 2 < 512) --p.tile_log2;
-    const dim3 grid((unsigned)((at.rows + (1 << p.tile_log2) - 1) >> p.tile_log2), splits, 2);
+    const int64_t most_rows = (kMostThreads / kThreads) << p.tile_log2;
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, p);
-        return hipGetLastError();
+        for (int64_t r = 0; r < at.rows; r += most_rows) {
+            const int64_t n = at.rows - r < most_rows ? at.rows - r : most_rows;
+            p.row0 = (int)r;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((n + (1 << p.tile_log2) - 1) >> p.tile_log2), splits, 2), dim3(kThreads), 0, st, p);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     };
     auto heads = [&](auto t, auto dt) {
         using U = decltype(t);
@@ -403,31 +411,48 @@ hipError_t launch_move(const riftkv_cache& c, const void* k, int64_t ld_k, const
 hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, int rows, int head_dim,
                           int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st) {
     const int heads = q.n + k.n;
+    // rows from r on
+    auto from = [&](const RopeRows& x, int64_t r) {
+        const int64_t e = bf16 ? 2 : 4;
+        if (x.n == 0) return x;
+        return RopeRows{static_cast<const unsigned char*>(x.x) + r * x.ld_x * e, static_cast<unsigned char*>(x.y) + r * x.ld_y * e,
+                        x.ld_x, x.ld_y, x.n};
+    };
+    // launch(rows, first row), as often as the rows need
+    auto in_pieces = [&](int64_t most, auto launch) {
+        for (int64_t r = 0; r < rows; r += most) {
+            launch((unsigned)(rows - r < most ? rows - r : most), r);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    };
     auto aligned = [&](const RopeRows& r) {   // 16-byte eights
         const int64_t per = bf16 ? 8 : 4;
         return r.n == 0 || (((reinterpret_cast<uintptr_t>(r.x) | reinterpret_cast<uintptr_t>(r.y)) & 15) == 0 &&
                             r.ld_x % per == 0 && r.ld_y % per == 0);
     };
     if (head_dim % 8 != 0 || rotary_dim % 16 != 0 || !aligned(q) || !aligned(k)) {
-        auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)rows * (unsigned)heads), dim3(64), 0, st, q, k, positions, head_dim,
-                               rotary_dim, interleaved ? 1 : 0, freqs, magnitude);
+        auto run = [&](auto kernel) {
+            return in_pieces(kMostThreads / 64 / heads, [&](unsigned n, int64_t r) {
+                hipLaunchKernelGGL(kernel, dim3(n * (unsigned)heads), dim3(64), 0, st, from(q, r), from(k, r), positions + r,
+                                   head_dim, rotary_dim, interleaved ? 1 : 0, freqs, magnitude);
+            });
         };
-        if (bf16) launch(rope_any_kernel<bf16_t>);
-        else launch(rope_any_kernel<float>);
-        return hipGetLastError();
+        return bf16 ? run(rope_any_kernel<bf16_t>) : run(rope_any_kernel<float>);
     }
     // all heads of a row a workgroup, so that its sines are worked out once, or fewer where that
     // leaves CUs without work (32 rows of 40 heads: 2.6 us, with 512 workgroups 3.4)
     int per = heads;
     while (per > 4 && (int64_t)rows * ((heads + per - 1) / per) < 256) per = (per + 1) / 2;
-    const dim3 grid((unsigned)rows, (unsigned)((heads + per - 1) / per));
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, q, k, positions, per, head_dim, rotary_dim, freqs, magnitude);
+    auto run = [&](auto kernel) {
+        return in_pieces(kMostThreads / kThreads, [&](unsigned n, int64_t r) {
+            hipLaunchKernelGGL(kernel, dim3(n, (unsigned)((heads + per - 1) / per)), dim3(kThreads), 0, st, from(q, r), from(k, r),
+                               positions + r, per, head_dim, rotary_dim, freqs, magnitude);
+        });
     };
-    if (bf16) interleaved ? launch(rope_kernel<bf16_t, true>) : launch(rope_kernel<bf16_t, false>);
-    else interleaved ? launch(rope_kernel<float, true>) : launch(rope_kernel<float, false>);
-    return hipGetLastError();
+    if (bf16) return interleaved ? run(rope_kernel<bf16_t, true>) : run(rope_kernel<bf16_t, false>);
+    return interleaved ? run(rope_kernel<float, true>) : run(rope_kernel<float, false>);
 }
 
 hipError_t launch_kv_decode_prep(const int* positions, int n_seq, int64_t capacity, int hd, float rope_base, float2* rope,

@@ -219,7 +219,7 @@ def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "h
         raise ValueError("k_out without k")
     if layout not in ROPE_LAYOUTS:
         raise ValueError(f"layout: one of {tuple(ROPE_LAYOUTS)}")
-    if freqs.dtype.char != "d" or not freqs.flags.c_contiguous or freqs.size == 0:
+    if freqs.dtype.str != "<f8" or not freqs.flags.c_contiguous or freqs.size == 0:
         raise TypeError("freqs: expected a contiguous float64 array")
     # (an array's own .ctypes takes three times as long)
     fp = ctypes.byref(ctypes.c_double.from_buffer(freqs)) if freqs.flags.writeable else freqs.ctypes.data
