@@ -922,7 +922,8 @@ rift_status rift_decode_step(const rift_model_cfg* cfg, const rift_layer_weights
 
 namespace {
 // workspace of a decode step over pages: RoPE rows and lengths of the sequences, row numbers,
-// h, q, k, v [n_seq][d], the SwiGLU activation, the GEMMs' partial sums, the attention's own
+// h, q (without split K also k and v) [n_seq][d], the SwiGLU activation, the GEMMs' partial sums,
+// the attention's own
 struct KvDecodeLayout {
     size_t rope, lens, rows, h, q, k, v, a, part, attn, total;
 };
@@ -934,14 +935,14 @@ KvDecodeLayout kv_decode_layout(const rift_model_cfg& c, const riftkv_cache& kv,
         off += align_up(bytes);
         return at;
     };
-    const size_t row = (size_t)n_seq * c.d * 2;
+    const size_t row = (size_t)n_seq * c.d * 2, whole = decode_skinny(c) ? 0 : row;
     L.rope = take((size_t)n_seq * (size_t)(c.head_dim / 2) * sizeof(float2));
     L.lens = take((size_t)n_seq * sizeof(int));
     L.rows = take((size_t)n_seq * sizeof(int));
     L.h = take(row);
     L.q = take(row);
-    L.k = take(row);
-    L.v = take(row);
+    L.k = take(whole);
+    L.v = take(whole);
     L.a = take((size_t)n_seq * c.ffn * 2);
     L.part = take(decode_gemm_floats(c, n_seq) * sizeof(float));
     L.attn = take(kv_attention_workspace(kv, c.n_heads, n_seq, max_pages));
@@ -1005,6 +1006,7 @@ rift_status riftkv_decode_step(const rift_model_cfg* cfg, const rift_layer_weigh
     const size_t layer_bytes = page_rows * cache->head_dim * (cache->dt == RIFTKV_BF16 ? 2 : 1);
     RIFT_TRY(launch_kv_decode_prep(positions, n_seq, max_pages * (int64_t)cache->page_size, c.head_dim, c.rope_base, rope,
                                    lens, rows, st));
+    const KvPlaces at{page_table, n_seq, max_pages, nullptr, positions, n_seq, status};
     for (int l = 0; l < c.n_layers; ++l) {
         const rift_layer_weights& w = layers[l];
         riftkv_cache kv = *cache;
@@ -1020,7 +1022,7 @@ rift_status riftkv_decode_step(const rift_model_cfg* cfg, const rift_layer_weigh
         if (split) {
             RIFT_TRY(launch_skinny_gemm(h, static_cast<const uint16_t*>(w.wq), static_cast<const uint16_t*>(w.wk),
                                         static_cast<const uint16_t*>(w.wv), d, n_seq, 3 * d, d, part, st));
-            RIFT_TRY(launch_skinny_qkv(part, skinny_split(3 * d, d), n_seq, d, c.head_dim, rope, rows, n_seq, q, k, v, 1, 0, st));
+            RIFT_TRY(launch_kv_decode_qkv(kv, part, skinny_split(3 * d, d), d, rope, at, q, st));
         } else {
             QkvArgs qa{};
             qa.a = h;
@@ -1037,9 +1039,8 @@ rift_status riftkv_decode_step(const rift_model_cfg* cfg, const rift_layer_weigh
             qa.d = d;
             qa.hd = c.head_dim;
             RIFT_TRY(launch_gemm_qkv_rope(qa, st));
+            RIFT_TRY(launch_kv_write(kv, k, d, v, d, true, at, st));
         }
-        const KvPlaces at{page_table, n_seq, max_pages, nullptr, positions, n_seq, status};
-        RIFT_TRY(launch_kv_write(kv, k, d, v, d, true, at, st));
         const KvAttention attn{q, h, d, d, c.n_heads, true, page_table, n_seq, max_pages, lens,
                                1.0f / sqrtf((float)c.head_dim), status, ws + L.attn};
         RIFT_TRY(launch_kv_attention(kv, attn, st));

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "../../include/rift_kv.h"
+#include "launch.h"
 
 namespace rift {
 
@@ -48,6 +49,12 @@ hipError_t launch_kv_read(const riftkv_cache& c, void* k, int64_t ld_k, void* v,
 // position, -1 for one past `capacity`); its own number.
 hipError_t launch_kv_decode_prep(const int* positions, int n_seq, int64_t capacity, int hd, float rope_base, float2* rope,
                                  int* lens, int* rows, hipStream_t st);
+
+// The new tokens' q|k|v as a product's partial sums [slots][n][3 d] (launch_skinny_gemm): added up,
+// q and k rotated by row i of rope, q as rows, k and v (rounded to bf16) to the places `at`
+// of sequence i, as launch_kv_write would.  d = n_kv_heads * head_dim; pages of bf16 or 8 bits.
+hipError_t launch_kv_decode_qkv(const riftkv_cache& c, const float* part, SkinnySplit sp, int d, const float2* rope,
+                                const KvPlaces& at, uint16_t* q, hipStream_t st);
 
 struct KvAttention {
     const void* q;
