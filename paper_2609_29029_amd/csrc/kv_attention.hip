@@ -180,7 +180,7 @@ __device__ void fill_heads(const AttnParams& p, int seq, int given, int hq, int 
 // T: type of queries and outputs.  WHOLE: a workgroup takes a head group of a sequence;
 // otherwise a run of all tiles.
 template <typename T, riftkv_dtype DT, int HD, int WAVES, bool WHOLE>
-__global__ void __launch_bounds__(64 * WAVES, 2)
+__global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 1 : 2)
 attention_kernel(AttnParams p) {
     constexpr int kThreads = 64 * WAVES;
     constexpr int RECORDS = WHOLE ? WAVES : 2 * WAVES;   // a wave's parts of heads
@@ -810,22 +810,39 @@ int workgroups(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pa
 
 // Waves of a workgroup that takes a head whole, or 0: heads are split.  A split costs the
 // scan of the lengths and the join, which short heads do not repay; a head taken whole is
-// read at one CU's rate, so it is bounded by what the table can hold.  In us, split / whole
-// with 1, 2 and 4 waves, bf16 of 128 dimensions and groups of 4 if not said otherwise:
-//   8 heads of 256 tokens         8.2 / 11.3  7.5  5.9    of 1,024      9.2 / 30.1 22.0 14.8
-//   128 of 300 to 512            13.1 / 22.3 13.6  9.9    of 1,024     17.8 / 42.5 24.9 17.3
-//   512 of 64                     9.4 /  5.4  5.9  6.0    of 1,024     45.8 / 50.7 43.2 43.0
-//   256 of 300 to 1,024          23.2 / 43.2 25.6 19.2    512, fp8     25.6 / 48.7 31.2 21.7
-//   1,024 of 32 to 512, fp8      24.6 / 28.0 20.6 22.3    3,200 of 50 to 1,024  148 / 153 146 141
-//   2,048 of 30 to 200, 64 dims  22.0 / 15.0 14.9 17.3    of 256       47.4 / 44.3 46.6 46.8
-//   2,400 of 1 to 400, int8      39.7 / 40.7 35.7 36.3    4,096 of 64  28.7 / 24.9 27.8 37.8
-//   16,384 of 64, group 1        91.4 / 84.1 89.4 133.7   3,200 of 131 to 643, group 1  106.8 / 104.8 101.5 97.4
-//   32 of 647, group 1            9.9 / 22.4 14.6 10.7    512 of 512 to 2,048, group 1   59.2 / 90.0 61.4  57.2
+// read at one CU's rate (and float32 ones multiplied at its rate), so it is bounded by what the
+// table can hold.  Eight waves (a CU's worth of registers) where every head has a CU and tiles
+// enough for them.  In us, split / whole with 1, 2, 4 and 8 waves, groups of 4 query heads if not
+// said otherwise:
+//   bf16, 128 dims:   8 heads of 256    8.2 / 11.3  7.5  5.4  6.3     8 of 512           8.4 /   -    -   7.5  7.8
+//     8 of 640        8.8 /   -    -   8.6  9.1     8 of 1,024         9.2 / 30.1 22.0 12.2 11.2
+//     96 of 512      12.1 /   -    -   9.8  9.8     96 of 1,024       16.0 /   -    -  16.8 15.6
+//     192 of 768     19.4 /   -    -  15.2 15.0     256 of 768        22.8 /   -    -  18.1 18.8
+//     512 of 64       9.4 /  5.4  5.9  6.0   -      512 of 1,024      45.8 / 50.7 43.2 43.0 45.3
+//     4,096 of 64    28.7 / 24.9 27.8 37.8   -      2,048 of 256      47.4 / 44.3 46.6 46.8   -
+//     3,200 of 50 to 1,024            148 / 153 146 141   -
+//     group 1: 3,200 of 131 to 643    107 / 105 102  97.4 -      512 of 512 to 2,048    59.2 / 90.0 61.4 57.2 57.7
+//              16,384 of 64          91.4 / 84.1 89.4 134 -      32 of 647               9.9 / 22.4 14.6 10.7  9.9
+//   e4m3, 128 dims:   8 of 512          8.5 /   -    -   7.7  7.6     8 of 768           8.9 /   -    -   9.9  9.1
+//     192 of 448     13.4 /   -    -   9.7  9.4     192 of 1,024      18.9 /   -    -  16.5 13.4
+//     256 of 1,024   19.6 /   -    -  17.1 15.3     320 of 1,024      24.4 /   -    -  21.3 25.3
+//     1,024 of 32 to 512  24.6 / 28.0 20.6 22.3 -   2,400 of 1 to 400, int8  39.7 / 40.7 35.7 36.3 -
+//   bf16, 64 dims:    8 of 768          8.3 /   -    -   8.9  7.8     8 of 1,024         8.6 /   -    -  11.6  9.5
+//     32 of 384       8.4 /   -    -   6.2  6.5     256 of 1,024      18.0 /   -    -  15.8 14.0
+//     2,048 of 30 to 200  22.0 / 15.0 14.9 17.3 -
+//   float32, 128 dims:  8 of 256     11.7 / 20.5 12.9 10.7   -        8 of 512          12.5 / 38.8 22.9 16.7   -
+//     128 of 384     21.1 / 35.2 22.3 19.5   -      256 of 512        32.1 / 47.1 29.9 26.9   -
 int whole_waves(const riftkv_cache& c, int64_t heads, int64_t max_pages) {
     const int64_t most = max_pages * c.page_size;
-    if (most > 1024 || (most > 512 && heads < 128)) return 0;
+    const bool f32 = c.dt == RIFTKV_F32, wide = c.dt == RIFTKV_BF16 && c.head_dim == 128;
+    int longest = 1024;
+    if (f32 && heads < 256) longest = heads < 128 ? 256 : 384;
+    if (!f32 && heads < 96) longest = c.head_dim == 64 ? 768 : 512;
+    if (most > longest) return 0;
     if (most <= 64 || (most <= 256 && heads >= 2048)) return 1;
-    const int waves = most <= 128 || (most <= 512 && heads >= 1024) ? 2 : 4;
+    int waves = 4;
+    if (most <= 128 || (most <= 512 && heads >= 1024)) waves = 2;
+    else if (!f32 && most > 384 && heads <= (wide ? 192 : 256)) waves = 8;
     return heads * waves < (1 << 26) ? waves : 1;   // a launch has less than 2^32 threads (at most 65,535 x 1,024 heads)
 }
 
@@ -883,6 +900,8 @@ hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipS
         const unsigned all = (unsigned)heads_of_all;
         if (whole == 1) return launch(attention_kernel<T, dt.value, hd.value, 1, true>, all, 1, record);
         if (whole == 2) return launch(attention_kernel<T, dt.value, hd.value, 2, true>, all, 2, 2 * record);
+        if constexpr (dt.value != RIFTKV_F32)
+            if (whole == 8) return launch(attention_kernel<T, dt.value, hd.value, 8, true>, all, 8, 8 * record);
         if (whole == 4) return launch(attention_kernel<T, dt.value, hd.value, 4, true>, all, 4, 4 * record);
         const hipError_t e = launch(attention_kernel<T, dt.value, hd.value, kSplitWaves, false>, (unsigned)wgs, kSplitWaves, 2 * kSplitWaves * record);
         if (e != hipSuccess) return e;
