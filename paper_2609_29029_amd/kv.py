@@ -33,14 +33,16 @@ class _RopeStruct(ctypes.Structure):
 
 
 _lib: Optional[ctypes.CDLL] = None
-torch = _ROWS = _STORES = None   # set by the first call: importing the package does not import torch
+# Set by the first call: importing the package does not import torch.
+torch = _ROWS = _STORES = _I32 = _U8 = _device = _raw_stream = None
 
 
 def _load() -> ctypes.CDLL:
-    global _lib, torch, _ROWS, _STORES
+    global _lib, torch, _ROWS, _STORES, _I32, _U8, _device, _raw_stream
     if _lib is None:
         import torch as t
-        torch = t
+        torch, _I32, _U8 = t, t.int32, t.uint8
+        _device, _raw_stream = t._C._cuda_getDevice, t._C._cuda_getCurrentRawStream
         _ROWS = {t.bfloat16: RIFT_BF16, t.float32: RIFT_F32}
         _STORES = {t.float32: RIFTKV_F32, t.bfloat16: RIFTKV_BF16, t.float8_e4m3fn: RIFTKV_FP8, t.int8: RIFTKV_INT8}
         L = load()
@@ -68,7 +70,9 @@ def _load() -> ctypes.CDLL:
 
 
 # ----------------------------------------------------------------------------- checks
-# Devices are compared by index: a call's checks are part of its cost.
+# A call's checks are part of its cost: devices are compared by index, and what the calls of a decode
+# step check of each tensor stands in them in line (a write 7.3 -> 6.7 us a call, 3.1 of it the launch); these functions then say what is
+# wrong, or that nothing is.
 def _dense(t, dtype, shape, device, name):
     """Address of a contiguous device tensor; shape None: any."""
     if t.dtype != dtype:
@@ -92,7 +96,7 @@ def _rows(t, dtype, shape, device, name):
         raise ValueError(f"{name}: must be on device {device}")
     n, heads, hd = shape
     ld, sh, se = t.stride()
-    if (hd > 1 and se != 1) or (heads > 1 and sh != hd):
+    if (se != 1 and hd > 1) or (sh != hd and heads > 1):
         raise ValueError(f"{name}: heads and elements must be contiguous")
     return t.data_ptr(), (ld if n > 1 else heads * hd)
 
@@ -111,22 +115,15 @@ def _row_type(t, name):
 
 
 def _stream(stream, device):
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device) or None
     if stream.device.index != device:
         raise ValueError(f"stream: must be on device {device}")
     return stream.cuda_stream or None
 
 
-def _call(name, device, fn, *args):
+def _elsewhere(device, fn, *args):
     """fn with `device` as the current one."""
-    if device == torch._C._cuda_getDevice():
-        st = fn(*args)
-    else:
-        with torch.cuda.device(device):
-            st = fn(*args)
-    if st:
-        _check(st, name)
+    with torch.cuda.device(device):
+        return fn(*args)
 
 
 # ----------------------------------------------------------------------------- the pages
@@ -194,66 +191,103 @@ def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "h
     """Rotates the rows q and k (either may be None) into q_out and k_out (None: in
     place) by positions [rows] i32.  freqs: float64 numpy array of rotary_dim / 2
     angles a position (riftkv_rope_freqs)."""
-    L = _load()
+    L = _lib or _load()
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
     if x.dim() != 3:
         raise ValueError("rows: expected [rows][heads][head_dim]")
-    dev, dtype = _device_of(x, "rows"), x.dtype
-    dt, (rows, _, hd) = _row_type(x, "rows"), x.shape
+    dev, dtype, (rows, _, hd) = x.get_device(), x.dtype, x.shape
+    dt = _ROWS.get(dtype)
+    if dt is None or dev < 0:
+        _device_of(x, "rows")
+        _row_type(x, "rows")
     pq = lq = nq = poq = loq = pk = lk = nk = pok = lok = 0
     if q is not None:
-        nq = q.shape[1]
-        pq, lq = _rows(q, dtype, (rows, nq, hd), dev, "q")
-        poq, loq = (pq, lq) if q_out is None else _rows(q_out, dtype, q.shape, dev, "q_out")
+        nq = x.shape[1]
+        shape = (rows, nq, hd)
+        pq, lq = _rows(q, dtype, shape, dev, "q")
+        poq, loq = (pq, lq) if q_out is None else _rows(q_out, dtype, shape, dev, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
     if k is not None:
         if k.dim() != 3:
             raise ValueError("rows: expected [rows][heads][head_dim]")
         nk = k.shape[1]
-        pk, lk = _rows(k, dtype, (rows, nk, hd), dev, "k")
-        pok, lok = (pk, lk) if k_out is None else _rows(k_out, dtype, k.shape, dev, "k_out")
+        shape = (rows, nk, hd)
+        pk, lk = _rows(k, dtype, shape, dev, "k")
+        pok, lok = (pk, lk) if k_out is None else _rows(k_out, dtype, shape, dev, "k_out")
     elif k_out is not None:
         raise ValueError("k_out without k")
-    if layout not in ROPE_LAYOUTS:
+    lay = ROPE_LAYOUTS.get(layout)
+    if lay is None:
         raise ValueError(f"layout: one of {tuple(ROPE_LAYOUTS)}")
-    if freqs.dtype.str != "<f8" or not freqs.flags.c_contiguous or freqs.size == 0:
+    flags = freqs.flags
+    if freqs.dtype.str != "<f8" or not flags.c_contiguous or freqs.size == 0:
         raise TypeError("freqs: expected a contiguous float64 array")
     # (an array's own .ctypes takes three times as long)
-    fp = ctypes.byref(ctypes.c_double.from_buffer(freqs)) if freqs.flags.writeable else freqs.ctypes.data
-    pos = _dense(positions, torch.int32, (rows,), dev, "positions")
-    _call("riftkv_rope", dev, L.riftkv_rope, pq, lq, nq, poq, loq, pk, lk, nk, pok, lok, dt, pos, rows, hd, 2 * freqs.size, ROPE_LAYOUTS[layout],
-          fp, magnitude, _stream(stream, dev))
+    fp = ctypes.byref(ctypes.c_double.from_buffer(freqs)) if flags.writeable else freqs.ctypes.data
+    if positions.dtype is not _I32 or positions.shape != (rows,) or not positions.is_contiguous() or positions.get_device() != dev:
+        _dense(positions, _I32, (rows,), dev, "positions")
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (pq, lq, nq, poq, loq, pk, lk, nk, pok, lok, dt, positions.data_ptr(), rows, hd, 2 * freqs.size, lay, fp, magnitude, st)
+    st = L.riftkv_rope(*args) if dev == _device() else _elsewhere(dev, L.riftkv_rope, *args)
+    if st:
+        _check(st, "riftkv_rope")
 
 
 # ----------------------------------------------------------------------------- rows
-def _move(name, cache, k, v, page_table, positions, status, seq_ids, stream):
-    dev, rows = cache.device, k.shape[0]
-    dt = _row_type(k, "k")
-    shape = (rows, cache.n_kv_heads, cache.head_dim)
-    pk, ldk = _rows(k, k.dtype, shape, dev, "k")
-    pv, ldv = _rows(v, k.dtype, shape, dev, "v")
+def _move(name, fn, cache, k, v, page_table, positions, status, seq_ids, stream):
+    dev, hd, dtype, i32, rows = cache.device, cache.head_dim, k.dtype, _I32, k.shape[0]
+    shape, one = (rows, cache.n_kv_heads, hd), (rows,)
+    dt = _ROWS.get(dtype)
+    if dt is None:
+        _row_type(k, "k")
+    if k.shape != shape or k.get_device() != dev:
+        _rows(k, dtype, shape, dev, "k")
+    if v.dtype is not dtype or v.shape != shape or v.get_device() != dev:
+        _rows(v, dtype, shape, dev, "v")
+    pk, pv = k.data_ptr(), v.data_ptr()
+    ldk, sh, se = k.stride()
+    if se != 1 or sh != hd:
+        pk, ldk = _rows(k, dtype, shape, dev, "k")
+    elif rows < 2:
+        ldk = shape[1] * hd
+    ldv, sh, se = v.stride()
+    if se != 1 or sh != hd:
+        pv, ldv = _rows(v, dtype, shape, dev, "v")
+    elif rows < 2:
+        ldv = shape[1] * hd
     n_seq, max_pages = page_table.shape
-    table = _dense(page_table, torch.int32, None, dev, "page_table")
-    pos = _dense(positions, torch.int32, (rows,), dev, "positions")
-    ids = None if seq_ids is None else _dense(seq_ids, torch.int32, (rows,), dev, "seq_ids")
-    word = _dense(status, torch.int32, (1,), dev, "status")
-    _call(name, dev, getattr(_lib, name), cache.ref, pk, ldk, pv, ldv, dt, table, n_seq, max_pages, ids, pos, rows, word,
-          _stream(stream, dev))
+    if page_table.dtype is not i32 or not page_table.is_contiguous() or page_table.get_device() != dev:
+        _dense(page_table, i32, None, dev, "page_table")
+    if positions.dtype is not i32 or positions.shape != one or not positions.is_contiguous() or positions.get_device() != dev:
+        _dense(positions, i32, one, dev, "positions")
+    ids = None
+    if seq_ids is not None:
+        if seq_ids.dtype is not i32 or seq_ids.shape != one or not seq_ids.is_contiguous() or seq_ids.get_device() != dev:
+            _dense(seq_ids, i32, one, dev, "seq_ids")
+        ids = seq_ids.data_ptr()
+    if status.dtype is not i32 or status.shape != (1,) or status.get_device() != dev:
+        _dense(status, i32, (1,), dev, "status")
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (cache.ref, pk, ldk, pv, ldv, dt, page_table.data_ptr(), n_seq, max_pages, ids, positions.data_ptr(), rows,
+            status.data_ptr(), st)
+    st = fn(*args) if dev == _device() else _elsewhere(dev, fn, *args)
+    if st:
+        _check(st, name)
 
 
 def riftkv_write(cache: KvCache, k, v, page_table, positions, status, seq_ids=None, stream=None) -> None:
     """Rows k, v [rows][n_kv_heads][head_dim] into the pages of their sequences:
     row i is at positions[i] of sequence seq_ids[i] (None: i); page_table
     [n_seq][max_pages], all i32.  Negative ones are skipped."""
-    _move("riftkv_write", cache, k, v, page_table, positions, status, seq_ids, stream)
+    _move("riftkv_write", _lib.riftkv_write, cache, k, v, page_table, positions, status, seq_ids, stream)
 
 
 def riftkv_read(cache: KvCache, page_table, positions, k_out, v_out, status, seq_ids=None, stream=None) -> None:
     """The same rows out of the pages, into k_out and v_out."""
-    _move("riftkv_read", cache, k_out, v_out, page_table, positions, status, seq_ids, stream)
+    _move("riftkv_read", _lib.riftkv_read, cache, k_out, v_out, page_table, positions, status, seq_ids, stream)
 
 
 # ----------------------------------------------------------------------------- attention
@@ -265,18 +299,42 @@ def riftkv_attention(cache: KvCache, q, page_table, lens, out, workspace, status
                      stream=None) -> None:
     """out[i] := attention of q[i] [n_heads][head_dim] over the first lens[i] tokens of
     sequence i's pages; scale None: 1 / sqrt(head_dim)."""
-    dev = cache.device
-    dt = _row_type(q, "q")
+    dev, hd, dtype, i32 = cache.device, cache.head_dim, q.dtype, _I32
     n_seq, max_pages = page_table.shape
-    shape = (n_seq, q.shape[1], cache.head_dim)
-    pq, ldq = _rows(q, q.dtype, shape, dev, "q")
-    po, ldo = _rows(out, q.dtype, shape, dev, "out")
-    table = _dense(page_table, torch.int32, None, dev, "page_table")
-    n = _dense(lens, torch.int32, (n_seq,), dev, "lens")
-    word = _dense(status, torch.int32, (1,), dev, "status")
-    ws = _dense(workspace, torch.uint8, None, dev, "workspace")
-    _call("riftkv_attention", dev, _lib.riftkv_attention, cache.ref, pq, ldq, shape[1], dt, table, n_seq, max_pages, n,
-          cache.head_dim ** -0.5 if scale is None else scale, po, ldo, word, ws, workspace.numel(), _stream(stream, dev))
+    n_heads = q.shape[1]
+    shape = (n_seq, n_heads, hd)
+    dt = _ROWS.get(dtype)
+    if dt is None:
+        _row_type(q, "q")
+    if q.shape != shape or q.get_device() != dev:
+        _rows(q, dtype, shape, dev, "q")
+    if out.dtype is not dtype or out.shape != shape or out.get_device() != dev:
+        _rows(out, dtype, shape, dev, "out")
+    pq, po = q.data_ptr(), out.data_ptr()
+    ldq, sh, se = q.stride()
+    if se != 1 or sh != hd:
+        pq, ldq = _rows(q, dtype, shape, dev, "q")
+    elif n_seq < 2:
+        ldq = n_heads * hd
+    ldo, sh, se = out.stride()
+    if se != 1 or sh != hd:
+        po, ldo = _rows(out, dtype, shape, dev, "out")
+    elif n_seq < 2:
+        ldo = n_heads * hd
+    if page_table.dtype is not i32 or not page_table.is_contiguous() or page_table.get_device() != dev:
+        _dense(page_table, i32, None, dev, "page_table")
+    if lens.dtype is not i32 or lens.shape != (n_seq,) or not lens.is_contiguous() or lens.get_device() != dev:
+        _dense(lens, i32, (n_seq,), dev, "lens")
+    if status.dtype is not i32 or status.shape != (1,) or status.get_device() != dev:
+        _dense(status, i32, (1,), dev, "status")
+    if workspace.dtype is not _U8 or not workspace.is_contiguous() or workspace.get_device() != dev:
+        _dense(workspace, _U8, None, dev, "workspace")
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (cache.ref, pq, ldq, n_heads, dt, page_table.data_ptr(), n_seq, max_pages, lens.data_ptr(),
+            hd ** -0.5 if scale is None else scale, po, ldo, status.data_ptr(), workspace.data_ptr(), workspace.numel(), st)
+    st = _lib.riftkv_attention(*args) if dev == _device() else _elsewhere(dev, _lib.riftkv_attention, *args)
+    if st:
+        _check(st, "riftkv_attention")
 
 
 # ----------------------------------------------------------------------------- decode
@@ -303,5 +361,8 @@ def riftkv_decode_step(cfg: ModelCfg, layers: Sequence[dict], x_new, cache: KvCa
     word = _dense(status, torch.int32, (1,), dev, "status")
     ws = _dense(workspace, torch.uint8, None, dev, "workspace")
     arr = (LayerWeights * max(1, len(layers)))(*[layer_struct(w) for w in layers])
-    _call("riftkv_decode_step", dev, _lib.riftkv_decode_step, ctypes.byref(cfg), arr, x, cache.ref, table, n_seq, max_pages,
-          pos, out, word, ws, workspace.numel(), _stream(stream, dev))
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (ctypes.byref(cfg), arr, x, cache.ref, table, n_seq, max_pages, pos, out, word, ws, workspace.numel(), st)
+    st = _lib.riftkv_decode_step(*args) if dev == _device() else _elsewhere(dev, _lib.riftkv_decode_step, *args)
+    if st:
+        _check(st, "riftkv_decode_step")
