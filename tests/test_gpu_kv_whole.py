@@ -55,3 +55,41 @@ def test_a_whole_head_in_a_graph(R, store):
         torch.cuda.synchronize()
         check(P, q, out, lens)
     assert int(P.status) == 0
+
+
+@pytest.mark.parametrize("store", ["bf16", "int8"])
+@pytest.mark.parametrize("page, hd, lens", [(4096, 64, [4096, 1, 4097, 0, 4095]), (1024, 128, [1025, 3000, 1024])])
+def test_large_pages(R, store, page, hd, lens):
+    P = filled(R, store, 2, hd, page, lens, seed=21)
+    q = randn(9, len(lens), 6, hd, scale=2)
+    out = attention(R, P, q, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert int(P.status) == 0
+    check(P, q, out, lens)
+
+
+@pytest.mark.parametrize("dt, store", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+@pytest.mark.parametrize("n_kv, group, n, long", [(1, 3, 257, {200: 3000}), (2, 1, 700, {0: 1500, 350: 1, 699: 2049}), (1, 18, 300, {299: 1300}),
+                                                  (1, 2, 1030, {})])
+def test_more_sequences_than_a_wave_holds(R, dt, store, n_kv, group, n, long):
+    """Split heads of many ragged sequences, most short, many without tokens."""
+    lens = [(7 * i) % 40 if i % 3 else 0 for i in range(n)]
+    for i, x in long.items():
+        lens[i] = x
+    room = lens if long else [1100] + lens[1:]     # a wide table all the same
+    P = filled(R, store, n_kv, 64, 16, room, seed=31, dtype=TYPES[dt])
+    q = randn(10, n, n_kv * group, 64, dtype=TYPES[dt], scale=2)
+    t = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out = attention(R, P, q, t)
+    again = attention(R, P, q, t)
+    torch.cuda.synchronize()
+    assert int(P.status) == 0 and torch.equal(out, again)
+    check(P, q, out, lens)
+
+
+def test_many_sequences_none_with_tokens(R):
+    P = filled(R, "bf16", 1, 64, 16, [1100] + [1] * 299, seed=32)
+    q = randn(12, 300, 2, 64)
+    out = attention(R, P, q, torch.zeros(300, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert int(P.status) == 0 and not bool(out.any())
