@@ -47,7 +47,8 @@ struct AttnParams {
     const int* lens;
     int* status;
     float* slots;          // [wgs][2][rows][HD + 4]: weighted values, max, sum
-    int4* joins;           // [wgs]: sequence (-1: none), first head, heads, last workgroup of a head group begun here
+    int4* joins;           // [wgs][2]: of the head groups that end and that begin here, shared with others: sequence
+                           // (-1: none), first head and heads (16 bits each), first and last workgroup
     int n_seq, max_pages, n_pages, n_kv, shift, group, q_tiles, rows;
     int few;               // at most kFewSeqs sequences, and 31 bits hold their tiles of all heads
     float scale_log2;
@@ -455,6 +456,16 @@ attention_kernel(AttnParams p) {
             bad = false;
         };
         start_head(cur);
+        if constexpr (!WHOLE)
+            if (wave == 0) {   // the head that an earlier workgroup began: worked out while the loads are under way
+                int4 join = make_int4(-1, 0, 0, 0);
+                if (cur.tile > 0 && p.rows > 1) {   // (a single row is joined where it begins)
+                    const unsigned long long first = end - left - cur.tile;
+                    join = make_int4(cur.seq, (cur.kvh * p.group + 16 * cur.qt) << 16 | min(16, p.group - 16 * cur.qt),
+                                     deal.owner(first) / WAVES, deal.owner(first + tiles_of(cur.len) - 1) / WAVES);
+                }
+                if (lane == 0) p.joins[2 * blockIdx.x] = join;
+            }
 
         for (;;) {
             const bool live = left > 1;
@@ -645,6 +656,8 @@ attention_kernel(AttnParams p) {
             nxt_pages = nn_pages;
             --left;
         }
+    } else if (!WHOLE && tid == 0) {
+        p.joins[2 * blockIdx.x] = make_int4(-1, 0, 0, 0);
     }
     __syncthreads();
 
@@ -717,36 +730,39 @@ attention_kernel(AttnParams p) {
             }
         }
     }
-    if (!WHOLE && tid == 0) {
-        if (join.x >= 0) join.w = deal.owner(head_end[last] - 1) / WAVES;
-        p.joins[blockIdx.x] = join;
-    }
+    if (!WHOLE && tid == 0)
+        p.joins[2 * blockIdx.x + 1] = join.x < 0 ? join : make_int4(join.x, join.y << 16 | join.z, blockIdx.x, deal.owner(head_end[last] - 1) / WAVES);
 }
 
-// One workgroup for each of the first kernel's: the head that it begins and others go
-// on with, from its slot 1 and their slots 0.  Threads take four columns of a row and
-// every PG-th part, then join over LDS.
-constexpr int kJoinThreads = 1024;
+// One workgroup for each of the first kernel's.  The rows of a head that several of those share are
+// dealt out to them; a row's parts are slot 1 of the first and slot 0 of the others.  Half of the
+// threads are for the head that ended in the workgroup, half for the one that went on; they
+// take four columns of a row and every PG-th part, then join over LDS.
+constexpr int kJoinThreads = 512;   // of a head
 
 template <typename T, int HD>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(2 * kJoinThreads)
 join_kernel(AttnParams p) {
     constexpr int RS = HD + 4, CV = HD / 4;
-    __shared__ __align__(16) f32x4_t accs[kJoinThreads];
-    __shared__ float2 mls[kJoinThreads];
-    const int tid = threadIdx.x;
-    const int4 join = p.joins[blockIdx.x];
+    __shared__ __align__(16) f32x4_t accs[2 * kJoinThreads];
+    __shared__ float2 mls[2 * kJoinThreads];
+    const int half = __builtin_amdgcn_readfirstlane(threadIdx.x / kJoinThreads), tid = threadIdx.x % kJoinThreads;
+    const int4 ended = p.joins[2 * blockIdx.x], went_on = p.joins[2 * blockIdx.x + 1], join = half ? went_on : ended;
     for (int s = blockIdx.x; s < p.n_seq; s += gridDim.x) {
         const int given = p.lens[s];
-        if (length_of(given, p.max_pages, p.shift) == 0) fill_heads<T>(p, s, given, -1, HD, tid, kJoinThreads);
+        if (length_of(given, p.max_pages, p.shift) == 0) fill_heads<T>(p, s, given, -1, HD, threadIdx.x, 2 * kJoinThreads);
     }
-    if (join.x < 0) return;
-    const int items = join.z * CV, PG = kJoinThreads / items;     // at least 2 (16 heads of 32 vectors)
-    const int parts = join.w - (int)blockIdx.x + 1, slot_floats = p.rows * RS;
-    const int pg = tid / items, item = tid - pg * items, row = item / CV, col = 4 * (item - row * CV);
+    if (ended.x < 0 && went_on.x < 0) return;
+    const int first = join.z, parts = join.w - first + 1, heads = join.y & 0xFFFF;
+    const int row0 = (int)blockIdx.x - first;                    // rows row0, row0 + parts, ... are this workgroup's
+    const bool some = join.x >= 0 && row0 < heads;
+    const int items = some && heads - row0 > parts ? ((heads - row0 + parts - 1) / parts) * CV : CV;   // of at most 8 rows
+    const int PG = kJoinThreads / items;
+    const int pg = tid / items, item = tid - pg * items, row = row0 + item / CV * parts, col = 4 * (item % CV);
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    if (pg < PG) {
+    if (some && pg < PG) {
+        const int slot_floats = p.rows * RS;
         constexpr int U = 2;   // parts in flight
         for (int i = pg; i < parts; i += U * PG) {
             f32x4_t x[U];
@@ -754,7 +770,7 @@ join_kernel(AttnParams p) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {   // past the last: its values, not used
                 const int at = min(i + u * PG, parts - 1);
-                const float* src = p.slots + ((size_t)(blockIdx.x + at) * 2 + (at == 0 ? 1 : 0)) * slot_floats + row * RS;
+                const float* src = p.slots + ((size_t)(first + at) * 2 + (at == 0 ? 1 : 0)) * slot_floats + row * RS;
                 x[u] = *reinterpret_cast<const f32x4_t*>(src + col);
                 ml[u] = *reinterpret_cast<const float2*>(src + HD);
             }
@@ -769,24 +785,24 @@ join_kernel(AttnParams p) {
             }
         }
     }
-    accs[tid] = acc;
-    mls[tid] = make_float2(m, l);
+    accs[threadIdx.x] = acc;
+    mls[threadIdx.x] = make_float2(m, l);
     __syncthreads();
-    if (tid >= items) return;
+    if (!some || tid >= items) return;
     float mx = m;
     const int used = min(PG, parts);
-    for (int i = 1; i < used; ++i) mx = fmaxf(mx, mls[i * items + tid].x);
+    for (int i = 1; i < used; ++i) mx = fmaxf(mx, mls[i * items + threadIdx.x].x);
     float f = __builtin_amdgcn_exp2f(m - ref_of(mx));
     acc *= f;
     l *= f;
     for (int i = 1; i < used; ++i) {
-        const float2 ml = mls[i * items + tid];
+        const float2 ml = mls[i * items + threadIdx.x];
         f = __builtin_amdgcn_exp2f(ml.x - ref_of(mx));
-        acc += f * accs[i * items + tid];
+        acc += f * accs[i * items + threadIdx.x];
         l += f * ml.y;
     }
     acc *= 1.f / l;
-    const size_t at = (size_t)join.x * p.ld_out + (size_t)(join.y + row) * HD + col;
+    const size_t at = (size_t)join.x * p.ld_out + (size_t)((join.y >> 16) + row) * HD + col;
     if constexpr (sizeof(T) == 2)
         *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + at) =
             make_uint2((uint32_t)round_bf16(acc[0]) | (uint32_t)round_bf16(acc[1]) << 16,
@@ -850,7 +866,7 @@ int whole_waves(const riftkv_cache& c, int64_t heads, int64_t max_pages) {
 
 size_t kv_attention_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages) {
     const size_t wgs = workgroups(c, n_heads, n_seq, max_pages);
-    const size_t joins = (wgs * sizeof(int4) + 255) / 256 * 256;
+    const size_t joins = (wgs * 2 * sizeof(int4) + 255) / 256 * 256;
     return joins + wgs * 2 * rows_of(c, n_heads) * (c.head_dim + 4) * sizeof(float);
 }
 
@@ -873,7 +889,7 @@ hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipS
     p.status = a.status;
     const int wgs = workgroups(c, a.n_heads, a.n_seq, a.max_pages);
     p.joins = static_cast<int4*>(a.workspace);
-    p.slots = reinterpret_cast<float*>(static_cast<unsigned char*>(a.workspace) + (wgs * sizeof(int4) + 255) / 256 * 256);
+    p.slots = reinterpret_cast<float*>(static_cast<unsigned char*>(a.workspace) + (wgs * 2 * sizeof(int4) + 255) / 256 * 256);
     p.n_seq = a.n_seq;
     p.max_pages = a.max_pages;
     p.n_pages = c.n_pages;
@@ -905,7 +921,7 @@ hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipS
         if (whole == 4) return launch(attention_kernel<T, dt.value, hd.value, 4, true>, all, 4, 4 * record);
         const hipError_t e = launch(attention_kernel<T, dt.value, hd.value, kSplitWaves, false>, (unsigned)wgs, kSplitWaves, 2 * kSplitWaves * record);
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((join_kernel<T, hd.value>), dim3(wgs), dim3(kJoinThreads), 0, st, p);
+        hipLaunchKernelGGL((join_kernel<T, hd.value>), dim3(wgs), dim3(2 * kJoinThreads), 0, st, p);
         return hipGetLastError();
     };
     auto heads = [&](auto t, auto dt) {
