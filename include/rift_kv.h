@@ -221,7 +221,8 @@ RIFT_API size_t riftkv_decode_workspace_size(const rift_model_cfg* cfg, const ri
  *              and its hidden_out row means nothing
  * hidden_out   [n_seq][d] f32 out  residual stream of the new tokens after the last layer
  * status       as for riftkv_write and riftkv_attention; the row of a sequence that sets it is NaN
- * Shape rules: those of rift_prefill's model and of riftkv_attention; n_seq * ffn < 2^31.
+ * Shape rules: those of rift_prefill's model and of riftkv_attention; n_seq * d and
+ * n_seq * ffn < 2^31.
  * Errors: RIFT_ERR_UNSUPPORTED also for float32 models and pages.
  */
 RIFT_API rift_status riftkv_decode_step(const rift_model_cfg* cfg, const rift_layer_weights* layers, const void* x_new,

@@ -956,8 +956,10 @@ rift_status check_kv_decode(const rift_model_cfg* cfg, const riftkv_cache* kv, i
     const rift_status ks = kv_check_cache(kv, arrays);
     if (ks != RIFT_OK) return ks;
     if (cfg->dt != RIFT_BF16 || kv->dt == RIFTKV_F32) return RIFT_ERR_UNSUPPORTED;
+    // the bf16 GEMMs address their rows, of d or ffn elements, with 32-bit byte offsets
     if (kv->n_kv_heads != cfg->n_heads || kv->head_dim != cfg->head_dim || n_seq < 0 || n_seq > 65535 || max_pages < 0 ||
-        (int64_t)max_pages * kv->page_size > kMaxTokens || (int64_t)n_seq * cfg->ffn >= (1ll << 31))
+        (int64_t)max_pages * kv->page_size > kMaxTokens ||
+        (int64_t)n_seq * (cfg->d > cfg->ffn ? cfg->d : cfg->ffn) >= (1ll << 31))
         return RIFT_ERR_SHAPE;
     return kv_attention_counts(*kv, cfg->n_heads, n_seq, max_pages) ? RIFT_OK : RIFT_ERR_UNSUPPORTED;
 }

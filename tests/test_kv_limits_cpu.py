@@ -1,0 +1,25 @@
+"""Sizes and values at which the paged key-value cache's calls have to refuse, on the CPU: nothing is launched."""
+import ctypes
+
+import pytest
+
+from tests.test_kv_cpu import FAKE, L, R, cache  # noqa: F401  (fixtures)
+
+
+def test_decode_step_of_rows_past_32_bit_offsets(R, L):  # noqa: F811
+    """The step's products address their rows by 32-bit byte offsets: n_seq * d as well as n_seq * ffn stays below 2^31."""
+    layer = R.LayerWeights(*[FAKE] * 9)
+
+    def call(d, heads, ffn, n_seq):
+        cfg = R.model_cfg(d=d, n_heads=heads, head_dim=128, ffn=ffn, n_layers=1, rms_eps=1e-6, rope_base=1e4, dt_code=R.RIFT_BF16)
+        c = cache(heads=heads)
+        size = L.riftkv_decode_workspace_size(ctypes.byref(cfg), ctypes.byref(c), n_seq, 4)
+        # a workspace that is always too small, so that nothing is launched
+        return size, L.riftkv_decode_step(ctypes.byref(cfg), ctypes.byref(layer), FAKE, ctypes.byref(c), FAKE, n_seq, 4, FAKE, FAKE,
+                                          FAKE, FAKE, 0, None)
+
+    for d, ffn, most in ((65536, 4096, (1 << 15) - 1), (65536, 8192, (1 << 15) - 1), (4096, 65536, (1 << 15) - 1)):
+        size, status = call(d, d // 128, ffn, most)
+        assert size > 0 and status == 5, (d, ffn, most)
+        for n in (most + 1, 40000, 65535):
+            assert call(d, d // 128, ffn, n) == (0, 2), (d, ffn, n)
