@@ -174,8 +174,10 @@ RIFT_API size_t riftkv_attention_workspace_size(const riftkv_cache* cache, int32
  * riftkv_attention -- one query token of every sequence over the first lens[i]
  * tokens of its pages (its own among them, once written):
  *   out = sum_j softmax_j(scale q . k_j) v_j, j < lens[i],
- * query head h with key-value head h / (n_heads / n_kv_heads).  Scores, softmax and
- * sums in float32; a sequence of length 0 gives zeros.
+ * query head h with key-value head h / (n_heads / n_kv_heads).  Scores, weights and
+ * sums in float32 (with 8-bit pages the product of a weight, at most 1, and its row's
+ * scale is cut off at 2^-133, fewer bits than float32 holds where the scale is below
+ * 2^-110); a sequence of length 0 gives zeros.
  * q        [n_seq][n_heads][head_dim] dt, sequences ld_q elements apart
  * out      [n_seq][n_heads][head_dim] dt, ld_out apart; overlaps no input
  * lens     [n_seq] i32 in [0, max_pages * page_size]

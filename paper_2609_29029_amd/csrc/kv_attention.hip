@@ -20,9 +20,11 @@
 // passes through LDS, and the softmax is a lane's own but for two swaps.  Unused
 // query columns cost nothing: the bytes of keys and values bound this kernel.
 //
-// Scores, weights and sums are float32; each weight goes into the matrix product as
-// bf16 terms that add up to it (two: all but 2^-18 of it; three, for float32 rows, all but
-// 2^-27), each float32 query as three.
+// Scores, weights and sums are float32: each weight, and each float32 query, goes into the
+// matrix product as three bf16 terms that add up to it.  (Two terms, short by up to 2^-16 of a weight:
+// 30 sequences of 29,813 tokens, 3 key heads of 64 dimensions, e4m3, 75.4 us and with three 76.2; 64 of
+// 3,000 to 5,000, 8 of 128, int8, 97.3 and 99; 96 of 17 to 24,001, e4m3, 392.7 and 394; bf16 pages within
+// 0.3%.)
 #include <type_traits>
 
 #include "kv_device.h"
@@ -126,13 +128,17 @@ __device__ __forceinline__ uint32_t widen(uint32_t w) {
     }
 }
 
-// Terms of bf16 that add up to x.
+// Pairs of bf16 terms that add up to a and b: each takes the leading 8 of the bits that are left, so that
+// three hold all 24 (of numbers from 2^-110 on; below, to 2^-133, the last bit of the smallest bf16).  Cut off, not
+// rounded: no term can pass the largest number, and what is left is exact.
 template <int N>
-__device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[N]) {
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t (&w)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        t[i] = static_cast<__bf16>(x);
-        x -= static_cast<float>(t[i]);
+        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+        w[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        a -= __uint_as_float(x & 0xFFFF0000u);
+        b -= __uint_as_float(y & 0xFFFF0000u);
     }
 }
 
@@ -196,7 +202,7 @@ attention_kernel(AttnParams p) {
     constexpr int I = 4 / E;                 // a lane's scores of those
     constexpr int VW = HD * B / 64;          // words of a lane of one value row
     constexpr int C = HD / 16;               // columns of a lane of one value row
-    constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
+    constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = 3;
     constexpr int RS = HD + 4;               // floats of a part's row: values, max, sum (and odd to the banks)
     extern __shared__ __align__(16) float records[];   // [RECORDS][rows][RS]
     __shared__ int4 meta[RECORDS];           // sequence (-1: no record), first head, heads, which ends of their tiles it holds
@@ -439,13 +445,16 @@ attention_kernel(AttnParams p) {
                         qf[0][f] = __builtin_bit_cast(bf16x8_t, x);
                     } else {
                         const float* src = static_cast<const float*>(p.q) + at;
+                        u32x4_t x[NQ];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            __bf16 t[NQ];
-                            split_bf16<NQ>(there ? src[e] : 0.f, t);
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w[NQ];
+                            split_bf16<NQ>(there ? src[2 * e] : 0.f, there ? src[2 * e + 1] : 0.f, w);
 #pragma unroll
-                            for (int i = 0; i < NQ; ++i) qf[i][f][e] = t[i];
+                            for (int i = 0; i < NQ; ++i) x[i][e] = w[i];
                         }
+#pragma unroll
+                        for (int i = 0; i < NQ; ++i) qf[i][f] = __builtin_bit_cast(bf16x8_t, x[i]);
                     }
                 }
             }
@@ -557,18 +566,19 @@ attention_kernel(AttnParams p) {
                     for (int c = 0; c < C; ++c)
                         o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j >> 2][j & 3][c]), pr[j], o[c], 0, 0, 0);
             } else {
-                bf16x8_t pf[NP];
+                u32x4_t pf[NP];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    __bf16 t[NP];
-                    split_bf16<NP>(pr[j], t);
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t w[NP];
+                    split_bf16<NP>(pr[2 * j], pr[2 * j + 1], w);
 #pragma unroll
-                    for (int i = 0; i < NP; ++i) pf[i][j] = t[i];
+                    for (int i = 0; i < NP; ++i) pf[i][j] = w[i];
                 }
                 auto add = [&](int c, const u32x4_t& vw) __attribute__((always_inline)) {
 #pragma unroll
                     for (int i = 0; i < NP; ++i)
-                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vw), pf[i], o[c], 0, 0, 0);
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vw), __builtin_bit_cast(bf16x8_t, pf[i]),
+                                                                        o[c], 0, 0, 0);
                 };
 #pragma unroll
                 for (int c = 0; c < C; c += 2) {   // columns c and c + 1 of the lane's rows, tokens in pairs
