@@ -24,8 +24,10 @@ struct RopeRows {
     int64_t ld_x, ld_y;
     int n;
 };
+// Turns (not radians) a position of each pair: hi + lo, to about 2^-77 of it.
 struct RopeFreqs {
-    double f[kMaxRotary / 2];   // turns (not radians) a position of each pair
+    double hi[kMaxRotary / 2];
+    float lo[kMaxRotary / 2];
 };
 hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, int rows, int head_dim,
                           int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st);

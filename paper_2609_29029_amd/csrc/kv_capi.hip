@@ -137,10 +137,12 @@ rift_status riftkv_rope(const void* q, int64_t ld_q, int32_t n_q, void* q_out, i
         return RIFT_ERR_SHAPE;
     if (freqs == nullptr) return RIFT_ERR_NULL;
     RopeFreqs f;
-    constexpr double kTwoPi = 6.283185307179586476925286766559;
+    // 2 pi = kTwoPi + kTwoPiRest, to 2^-109 of it
+    constexpr double kTwoPi = 6.283185307179586476925286766559, kTwoPiRest = 2.4492935982947064e-16;
     for (int j = 0; j < rotary_dim / 2; ++j) {
         if (!isfinite(freqs[j])) return RIFT_ERR_NONFINITE;
-        f.f[j] = freqs[j] / kTwoPi;
+        f.hi[j] = freqs[j] / kTwoPi;
+        f.lo[j] = (float)((fma(-f.hi[j], kTwoPi, freqs[j]) - f.hi[j] * kTwoPiRest) * (1.0 / kTwoPi));
     }
     if (!isfinite(magnitude)) return RIFT_ERR_NONFINITE;
     if (rows == 0 || n_q + n_k == 0) return RIFT_OK;

@@ -70,11 +70,13 @@ __device__ __forceinline__ void store_eight(void* p, size_t i, const float (&f)[
 // ---------------------------------------------------------------- positions
 
 // The angle in turns, reduced to [-1/2, 1/2] in float64: float32 holds it and its
-// sine and cosine to their last bits however far the position is.
-__device__ __forceinline__ float2 rope_turn(int position, double turns, float magnitude) {
-    const double t = (double)position * turns;
+// sine and cosine to their last bits however far the position is.  (The turns a position as one
+// float64 are up to 1.3e-7 radians off at 2^31 positions of one radian, 1.2e-6 of 5.6 radians.)
+__device__ __forceinline__ float2 rope_turn(int position, const RopeFreqs& freqs, int j, float magnitude) {
+    const double p = position, whole = rint(p * freqs.hi[j]);
+    const double t = fma(p, freqs.hi[j], -whole) + p * freqs.lo[j];
     float s, c;
-    sincospif((float)(2.0 * (t - rint(t))), &s, &c);
+    sincospif((float)(2.0 * t), &s, &c);
     return make_float2(c * magnitude, s * magnitude);
 }
 
@@ -90,7 +92,7 @@ rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int h
     const size_t x0 = (size_t)row * r.ld_x + hoff, y0 = (size_t)row * r.ld_y + hoff;
     const int half = rotary_dim / 2;
     for (int j = threadIdx.x; j < half; j += 64) {
-        const float2 cs = rope_turn(positions[row], freqs.f[j], magnitude);
+        const float2 cs = rope_turn(positions[row], freqs, j, magnitude);
         const int i1 = interleaved ? 2 * j : j, i2 = interleaved ? 2 * j + 1 : j + half;
         const float2 y = rotate_pair(load_f32<T>(r.x, x0 + i1), load_f32<T>(r.x, x0 + i2), cs);
         store_f32<T>(r.y, y0 + i1, y.x);
@@ -131,7 +133,7 @@ rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int per, 
         if (!INTERLEAVED && v < turned) xb = load_eight<T>(x, from + half + e);
     };
     if (h < end) load();
-    if (threadIdx.x < half) turns[threadIdx.x] = rope_turn(positions[row], freqs.f[threadIdx.x], magnitude);
+    if (threadIdx.x < half) turns[threadIdx.x] = rope_turn(positions[row], freqs, threadIdx.x, magnitude);
     __syncthreads();
     while (h < end) {
         const int v0 = v;
