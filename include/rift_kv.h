@@ -185,8 +185,9 @@ RIFT_API size_t riftkv_attention_workspace_size(const riftkv_cache* cache, int32
  * A length out of range, or a page outside [0, n_pages) among a sequence's tokens,
  * sets the status and makes that sequence's output NaN.
  * What lies in a page past a sequence's length has no effect, whatever its bits.
- * How the keys are dealt out depends on all sequences' lengths: a result may differ in
- * its last bits between batches, never between two calls with the same ones.
+ * How the keys are dealt out depends on n_seq, max_pages and all sequences' lengths: a
+ * result may differ in its last bits where any of these does, never between two calls
+ * with the same.
  * dt bf16 with pages of bf16, fp8 or int8; dt f32 with any.
  * Shape rules: n_heads a multiple of n_kv_heads, at most 4096; 0 <= n_seq <= 65535; max_pages >=
  * 0, max_pages * page_size <= 2^30.  workspace >= riftkv_attention_workspace_size
@@ -223,6 +224,7 @@ RIFT_API size_t riftkv_decode_workspace_size(const rift_model_cfg* cfg, const ri
  *              and its hidden_out row means nothing
  * hidden_out   [n_seq][d] f32 out  residual stream of the new tokens after the last layer
  * status       as for riftkv_write and riftkv_attention; the row of a sequence that sets it is NaN
+ * A sequence's last bits depend on the batch and the table's width as riftkv_attention's do.
  * Shape rules: those of rift_prefill's model and of riftkv_attention; n_seq * d and
  * n_seq * ffn < 2^31.
  * Errors: RIFT_ERR_UNSUPPORTED also for float32 models and pages.
