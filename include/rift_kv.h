@@ -99,7 +99,7 @@ typedef struct {
  * pairs, in float64, and the factor on the rotated pairs that goes with them.
  * freqs [host] out [rotary_dim / 2];  magnitude [host] out (1 except RAMP; may be NULL)
  * Errors: RIFT_ERR_NULL, RIFT_ERR_SHAPE (rotary_dim), RIFT_ERR_UNSUPPORTED (scaling),
- * RIFT_ERR_NONFINITE (a value out of range or not finite).
+ * RIFT_ERR_NONFINITE (a value out of range or not finite, a base that the factor makes so).
  */
 RIFT_API rift_status riftkv_rope_freqs(const riftkv_rope_cfg* cfg, double* freqs, double* magnitude);
 

@@ -101,6 +101,7 @@ rift_status riftkv_rope_freqs(const riftkv_rope_cfg* cfg, double* freqs, double*
     constexpr double kTwoPi = 6.283185307179586476925286766559;
     double base = cfg->base, a = 0.0, b = 0.0;
     if (kind == (int)RIFTKV_ROPE_BASE) base *= pow(cfg->factor, (double)R / (double)(R - 2));
+    if (!isfinite(base)) return RIFT_ERR_NONFINITE;
     if (kind == (int)RIFTKV_ROPE_RAMP) {
         auto pair_of = [&](double turns) { return R * log(cfg->original_len / (kTwoPi * turns)) / (2.0 * log(base)); };
         a = fmax(floor(pair_of(cfg->high)), 0.0);

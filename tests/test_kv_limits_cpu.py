@@ -23,3 +23,13 @@ def test_decode_step_of_rows_past_32_bit_offsets(R, L):  # noqa: F811
         assert size > 0 and status == 5, (d, ffn, most)
         for n in (most + 1, 40000, 65535):
             assert call(d, d // 128, ffn, n) == (0, 2), (d, ffn, n)
+
+
+@pytest.mark.parametrize("base, factor, rotary_dim", [(1e300, 1e10, 64), (10000.0, 1e200, 4), (1.7e308, 2.0, 128)])
+def test_a_base_that_overflows(R, base, factor, rotary_dim):  # noqa: F811
+    """base * factor^(R / (R - 2)) past float64: every frequency but the first would be 0."""
+    with pytest.raises(R.RiftError) as e:
+        R.riftkv_rope_freqs(rotary_dim, base=base, scaling="base", factor=factor)
+    assert e.value.status == 7
+    freqs, _ = R.riftkv_rope_freqs(rotary_dim, base=1e300, scaling="base", factor=1.0)
+    assert (freqs > 0).all()
