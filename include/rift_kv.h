@@ -120,6 +120,7 @@ typedef enum {
  *             same stride); otherwise outputs overlap no input
  * positions   [rows] i32, any value
  * freqs       [host] [rotary_dim / 2], finite; read before the call returns
+ * magnitude   finite in float32
  * Shape rules: rows >= 0, 0 <= n_q, n_k <= 4096, 1 <= head_dim <= 256,
  * rotary_dim even in [2, head_dim], every ld >= its heads * head_dim.
  */

@@ -145,7 +145,7 @@ rift_status riftkv_rope(const void* q, int64_t ld_q, int32_t n_q, void* q_out, i
         f.hi[j] = freqs[j] / kTwoPi;
         f.lo[j] = (float)((fma(-f.hi[j], kTwoPi, freqs[j]) - f.hi[j] * kTwoPiRest) * (1.0 / kTwoPi));
     }
-    if (!isfinite(magnitude)) return RIFT_ERR_NONFINITE;
+    if (!isfinite((float)magnitude)) return RIFT_ERR_NONFINITE;
     if (rows == 0 || n_q + n_k == 0) return RIFT_OK;
     if (positions == nullptr || (n_q > 0 && (q == nullptr || q_out == nullptr)) ||
         (n_k > 0 && (k == nullptr || k_out == nullptr)))

@@ -33,3 +33,16 @@ def test_a_base_that_overflows(R, base, factor, rotary_dim):  # noqa: F811
     assert e.value.status == 7
     freqs, _ = R.riftkv_rope_freqs(rotary_dim, base=1e300, scaling="base", factor=1.0)
     assert (freqs > 0).all()
+
+
+def test_a_magnitude_past_float32(L):  # noqa: F811
+    """The factor on the pairs is applied in float32, where this one is infinite."""
+    import numpy as np
+    f = np.ones(32)
+
+    def call(mag):
+        return L.riftkv_rope(FAKE, 128, 2, FAKE, 128, None, 0, 0, None, 0, 1, FAKE, 0, 64, 64, 0, f.ctypes.data, mag, None)   # no rows
+
+    for mag in (1e39, -3.5e38, float("inf")):
+        assert call(mag) == 7, mag
+    assert call(3.4e38) == 0 and call(0.0) == 0
