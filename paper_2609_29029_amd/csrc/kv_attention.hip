@@ -17,8 +17,11 @@
 // own share of the second product's right operand, O^T = V^T P^T, if its token
 // order is the lanes' (a sum's order is free), and a lane's own rows of V are, with two
 // bytes or halfwords exchanged in registers, its share of the left one.  So nothing
-// passes through LDS, and the softmax is a lane's own but for two swaps.  Unused
-// query columns cost nothing: the bytes of keys and values bound this kernel.
+// passes through LDS, and the softmax is a lane's own but for two swaps.  The bytes of keys
+// and values bound this kernel, so that unused query columns cost nothing, except in 8-bit pages of
+// 64 dimensions: there a tile's vector instructions, the softmax of 16 columns among them whatever the
+// group, take longer than its bytes.  Groups of more than 16 are several head groups, each of which reads
+// the key head's keys and values.
 //
 // Scores, weights and sums are float32: each weight, and each float32 query, goes into the
 // matrix product as three bf16 terms that add up to it.  (Two terms, short by up to 2^-16 of a weight:
@@ -840,24 +843,24 @@ int workgroups(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pa
 // table can hold.  Eight waves (a CU's worth of registers) where every head has a CU and tiles
 // enough for them.  In us, split / whole with 1, 2, 4 and 8 waves, groups of 4 query heads if not
 // said otherwise:
-//   bf16, 128 dims:   8 heads of 256    8.2 / 11.3  7.5  5.4  6.3     8 of 512           8.4 /   -    -   7.5  7.8
-//     8 of 640        8.8 /   -    -   8.6  9.1     8 of 1,024         9.2 / 30.1 22.0 12.2 11.2
-//     96 of 512      12.1 /   -    -   9.8  9.8     96 of 1,024       16.0 /   -    -  16.8 15.6
-//     192 of 768     19.4 /   -    -  15.2 15.0     256 of 768        22.8 /   -    -  18.1 18.8
-//     512 of 64       9.4 /  5.4  5.9  6.0   -      512 of 1,024      45.8 / 50.7 43.2 43.0 45.3
-//     4,096 of 64    28.7 / 24.9 27.8 37.8   -      2,048 of 256      47.4 / 44.3 46.6 46.8   -
-//     3,200 of 50 to 1,024            148 / 153 146 141   -
-//     group 1: 3,200 of 131 to 643    107 / 105 102  97.4 -      512 of 512 to 2,048    59.2 / 90.0 61.4 57.2 57.7
-//              16,384 of 64          91.4 / 84.1 89.4 134 -      32 of 647               9.9 / 22.4 14.6 10.7  9.9
-//   e4m3, 128 dims:   8 of 512          8.5 /   -    -   7.7  7.6     8 of 768           8.9 /   -    -   9.9  9.1
-//     192 of 448     13.4 /   -    -   9.7  9.4     192 of 1,024      18.9 /   -    -  16.5 13.4
-//     256 of 1,024   19.6 /   -    -  17.1 15.3     320 of 1,024      24.4 /   -    -  21.3 25.3
-//     1,024 of 32 to 512  24.6 / 28.0 20.6 22.3 -   2,400 of 1 to 400, int8  39.7 / 40.7 35.7 36.3 -
-//   bf16, 64 dims:    8 of 768          8.3 /   -    -   8.9  7.8     8 of 1,024         8.6 /   -    -  11.6  9.5
-//     32 of 384       8.4 /   -    -   6.2  6.5     256 of 1,024      18.0 /   -    -  15.8 14.0
-//     2,048 of 30 to 200  22.0 / 15.0 14.9 17.3 -
-//   float32, 128 dims:  8 of 256     11.7 / 20.5 12.9 10.7   -        8 of 512          12.5 / 38.8 22.9 16.7   -
-//     128 of 384     21.1 / 35.2 22.3 19.5   -      256 of 512        32.1 / 47.1 29.9 26.9   -
+//   bf16, 128 dims:   8 heads of 256    8.7 / 10.2  7.1  5.8  6.5     8 of 512           9.0 / 17.8 11.1  8.1  8.1
+//     8 of 640        9.1 / 21.6 13.1  9.2  9.6     8 of 1,024         9.4 / 32.7 19.2 12.5 11.3
+//     96 of 512      12.6 / 23.3 14.2 10.2 10.1     96 of 1,024       16.3 / 45.1 26.0 17.3 16.0
+//     192 of 768     19.8 / 35.4 21.0 15.6 15.5     256 of 768        22.9 / 36.2 21.8 18.5 18.7
+//     512 of 64       9.6 /  5.5  6.1  6.0 10.2     512 of 1,024      46.5 / 52.5 43.8 43.6 45.5
+//     4,096 of 64    29.7 / 25.8 29.0 39.5 71.9     2,048 of 256      46.1 / 43.7 45.7 46.1 64.1
+//     3,200 of 50 to 1,024            151 / 155 146 141 162
+//     group 1: 3,200 of 131 to 643    112 / 110 105 102 119             512 of 512 to 2,048    62.3 / 96.9 65.2 59.8 60.2
+//              16,384 of 64          94.3 / 87.0 92.7 137 276           32 of 647              10.5 / 28.7 17.8 12.5 11.2
+//   e4m3, 128 dims:   8 of 512          8.9 / 19.6 12.1  8.7  7.9     8 of 768           9.1 / 28.1 16.6 11.0  9.7
+//     192 of 448     14.1 / 22.6 14.2 10.4 10.3     192 of 1,024      19.7 / 48.1 28.3 17.8 14.0
+//     256 of 1,024   20.3 / 48.4 28.6 18.4 15.9     320 of 1,024      25.4 / 52.1 34.7 22.6 26.0
+//     1,024 of 32 to 512  25.2 / 29.5 21.5 22.6 31.0  2,400 of 1 to 400, int8  41.7 / 42.1 37.2 37.3 66.6
+//   bf16, 64 dims:    8 of 768          8.8 / 21.0 14.0  9.8  8.2     8 of 1,024         8.8 / 27.3 15.6 11.2  9.0
+//     32 of 384       8.9 / 13.4  8.9  6.8  6.8     256 of 1,024      19.0 / 37.7 23.1 16.2 14.3
+//     2,048 of 30 to 200  22.9 / 15.2 14.9 17.1 23.5
+//   float32, 128 dims (no form with eight):  8 of 256  12.2 / 20.7 13.1 10.8     8 of 512     12.5 / 40.1 23.8 17.1
+//     128 of 384     22.3 / 35.1 22.5 19.5          256 of 512        33.0 / 47.3 30.1 27.4
 int whole_waves(const riftkv_cache& c, int64_t heads, int64_t max_pages) {
     const int64_t most = max_pages * c.page_size;
     const bool f32 = c.dt == RIFTKV_F32, wide = c.dt == RIFTKV_BF16 && c.head_dim == 128;
