@@ -6,17 +6,22 @@
  * sequences take from one pool, in 16 or 32 bits or quantised to 8, with one
  * key-value head for each group of query heads:
  *   riftkv_rope       rotary positions of query and key rows
+ *   riftkv_rope_axes  the same with several positions a row (tile, row, column)
  *   riftkv_write      new key and value rows into their sequences' pages,
  *                     quantised as they are written
  *   riftkv_read       rows of the pages back, as dense rows
  *   riftkv_attention  one new token of every sequence over its pages
+ *   riftkv_attention_shared  the same after a prefix that all sequences share,
+ *                     read once for all
+ *   riftkv_page_bounds, riftkv_select_pages, riftkv_attention_pages
+ *                     the same over the pages that promise the largest scores
  *   riftkv_decode_step  a decode step of rift.h's model over them
  *
  * The conventions of rift.h hold: device pointers unless marked [host], buffers
  * and workspace owned by the caller, calls asynchronous and ordered on
  * `stream`, arguments checked on the host before anything is enqueued.
  * Base pointers of rows and pages are 16-byte aligned and row strides a
- * multiple of 16 bytes (RIFT_ERR_SHAPE), except in riftkv_rope, which takes any.
+ * multiple of 16 bytes (RIFT_ERR_SHAPE), except in riftkv_rope and riftkv_rope_axes, which take any.
  * A call runs on the current device, to which `stream` and all memory belong.
  *
  * Pages
@@ -130,6 +135,20 @@ RIFT_API rift_status riftkv_rope(const void* q, int64_t ld_q, int32_t n_q, void*
                                  int32_t rotary_dim, riftkv_rope_layout layout, const double* freqs,
                                  double magnitude, rift_stream stream);
 
+/*
+ * riftkv_rope_axes -- riftkv_rope with a position of every row on each of several axes (a tile's place
+ * in the scene, row and column in the tile): pair j turns by positions[axes[j]][row] * freqs[j].
+ * positions   [n_axes][rows] i32, any value
+ * axes        [host] [rotary_dim / 2] i32 in [0, n_axes); read before the call returns
+ * Everything else as for riftkv_rope, and with all positions of a row the same its results, bit for bit.
+ * Shape rules: 1 <= n_axes <= 8.  Errors: RIFT_ERR_SHAPE also for an axis out of range.
+ */
+RIFT_API rift_status riftkv_rope_axes(const void* q, int64_t ld_q, int32_t n_q, void* q_out, int64_t ld_q_out,
+                                      const void* k, int64_t ld_k, int32_t n_k, void* k_out, int64_t ld_k_out,
+                                      rift_dtype dt, const int32_t* positions, int32_t n_axes, int32_t rows,
+                                      int32_t head_dim, int32_t rotary_dim, riftkv_rope_layout layout,
+                                      const double* freqs, const int32_t* axes, double magnitude, rift_stream stream);
+
 /* ------------------------------------------------------------------ pages */
 
 /*
@@ -198,6 +217,93 @@ RIFT_API rift_status riftkv_attention(const riftkv_cache* cache, const void* q, 
                                       rift_dtype dt, const int32_t* page_table, int32_t n_seq, int32_t max_pages,
                                       const int32_t* lens, float scale, void* out, int64_t ld_out, int32_t* status,
                                       void* workspace, size_t ws_bytes, rift_stream stream);
+
+/* ------------------------------------------------------------------ a shared prefix */
+
+/* Workspace bytes of riftkv_attention_shared (0 for shapes that it refuses).  Not smaller for more
+ * sequences, a longer prefix or wider tables. */
+RIFT_API size_t riftkv_attention_shared_workspace_size(const riftkv_cache* cache, int32_t n_heads, int32_t n_seq,
+                                                       int32_t prefix_len, int32_t max_pages);
+
+/*
+ * riftkv_attention_shared -- riftkv_attention of sequences that all begin with the same prefix_len tokens: each
+ * attends to those and then to the first lens[i] tokens of its own pages, its own row i of page_table.  The prefix'
+ * keys and values are read once for all sequences, not once for each.
+ * prefix_table [ceil(prefix_len / page_size)] i32 pages of the prefix; its last page need not be full
+ * prefix_len   [host] tokens of the prefix, >= 0
+ * lens         [n_seq] i32 in [0, max_pages * page_size], the prefix not counted
+ * A page of the prefix outside [0, n_pages) sets the status and makes every sequence's output NaN; a sequence
+ * without any token gives zeros.  Everything else as for riftkv_attention.
+ * Shape rules: prefix_len <= 2^30.
+ */
+RIFT_API rift_status riftkv_attention_shared(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads,
+                                             rift_dtype dt, const int32_t* prefix_table, int32_t prefix_len,
+                                             const int32_t* page_table, int32_t n_seq, int32_t max_pages,
+                                             const int32_t* lens, float scale, void* out, int64_t ld_out, int32_t* status,
+                                             void* workspace, size_t ws_bytes, rift_stream stream);
+
+/* ------------------------------------------------------------------ some pages of a long context */
+
+/*
+ * riftkv_page_bounds -- the smallest and largest value of every element of the keys of a page's tokens.
+ * bounds      [n_pages][n_kv_heads][2][head_dim], f32 with f32 pages, else bf16: smallest, then largest; by page, as the
+ *             cache is, so that sequences which share a page share its bounds
+ * begins      [n_seq] i32, or NULL: all 0.  The pages of sequence i that hold its tokens begins[i] .. lens[i] - 1 are
+ *             gone through anew, each from its first token on, up to lens[i]; the other bounds stay as they are.
+ *             A decode step that wrote token n passes begins[i] = n, lens[i] = n + 1.  Below 0: as 0
+ * lens        [n_seq] i32 in [0, max_pages * page_size]
+ * The values are exact, 8-bit pages' but for those of rows whose largest magnitude is below 2^-110, which are rounded
+ * to bf16; NaN among an element's values makes both its bounds NaN.
+ * Where sequences share a page that is not full for all of them, its bounds are one of theirs, or parts of several.
+ * A length out of range, or a page outside [0, n_pages), sets the status and is skipped.
+ * Shape rules: n_seq, max_pages >= 0, max_pages * page_size <= 2^30.
+ */
+RIFT_API rift_status riftkv_page_bounds(const riftkv_cache* cache, void* bounds, const int32_t* page_table, int32_t n_seq,
+                                        int32_t max_pages, const int32_t* begins, const int32_t* lens, int32_t* status,
+                                        rift_stream stream);
+
+/* Workspace bytes of riftkv_select_pages (0 for shapes that it refuses).  Not smaller for more sequences or wider
+ * tables. */
+RIFT_API size_t riftkv_select_pages_workspace_size(const riftkv_cache* cache, int32_t n_seq, int32_t max_pages);
+
+/*
+ * riftkv_select_pages -- for every sequence and key head the `top` pages that its new token's queries need most.
+ * A page's score for a query is sum_d (min(q_d, 0) smallest_d + max(q_d, 0) largest_d), in float64: no key of
+ * the page has a larger product with the query.  Its score for the key head is the largest of its group's queries'.
+ * The first keep_first and the last keep_last pages of the sequence's ceil(lens[i] / page_size) are always taken, the
+ * others by (score descending, page ascending) until there are `top`; a page with a score of NaN comes last.
+ * bounds      as riftkv_page_bounds leaves them (of the sequences' pages)
+ * q           [n_seq][n_heads][head_dim] dt, sequences ld_q elements apart
+ * pages       [n_seq][n_kv_heads][top] i32 out: the places in the sequence's row of page_table, ascending; -1 behind the
+ *             last where the sequence has fewer pages.  Overlaps no input
+ * A length out of range sets the status and gives -1 throughout; a page outside [0, n_pages) sets the status and comes last.
+ * Shape rules: those of riftkv_attention; 1 <= top <= 2^20, keep_first, keep_last >= 0, keep_first + keep_last <= top.
+ * dt as for riftkv_attention.  workspace 256-byte aligned; calls that may overlap in time need one each.
+ */
+RIFT_API rift_status riftkv_select_pages(const riftkv_cache* cache, const void* bounds, const void* q, int64_t ld_q,
+                                         int32_t n_heads, rift_dtype dt, const int32_t* page_table, int32_t n_seq,
+                                         int32_t max_pages, const int32_t* lens, int32_t keep_first, int32_t keep_last,
+                                         int32_t* pages, int32_t top, int32_t* status, void* workspace, size_t ws_bytes,
+                                         rift_stream stream);
+
+/* Workspace bytes of riftkv_attention_pages (0 for shapes that it refuses).  Not smaller for more sequences or
+ * longer lists. */
+RIFT_API size_t riftkv_attention_pages_workspace_size(const riftkv_cache* cache, int32_t n_heads, int32_t n_seq, int32_t top);
+
+/*
+ * riftkv_attention_pages -- riftkv_attention over the tokens of some pages only, a list for every sequence and key head.
+ * pages       [n_seq][n_kv_heads][top] i32 places in the sequence's row of page_table, as riftkv_select_pages leaves them or
+ *             in any order; negative ones are skipped.  Of each page the tokens before lens[i] count; a place that is listed
+ *             twice counts twice
+ * A list without tokens gives zeros.  A length out of range, a place >= max_pages or a page outside [0, n_pages) among the
+ * listed tokens sets the status and makes the outputs of that sequence and key head NaN.
+ * Shape rules: those of riftkv_attention; 1 <= top <= 2^20, top * page_size <= 2^30.
+ */
+RIFT_API rift_status riftkv_attention_pages(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads,
+                                            rift_dtype dt, const int32_t* page_table, int32_t n_seq, int32_t max_pages,
+                                            const int32_t* lens, const int32_t* pages, int32_t top, float scale, void* out,
+                                            int64_t ld_out, int32_t* status, void* workspace, size_t ws_bytes,
+                                            rift_stream stream);
 
 /* ------------------------------------------------------------------ decode */
 

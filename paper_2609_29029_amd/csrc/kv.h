@@ -15,6 +15,7 @@ namespace rift {
 rift_status kv_check_cache(const riftkv_cache* c, bool arrays);
 
 constexpr int kMaxRotary = 256;
+constexpr int kMaxAxes = 8;
 constexpr int64_t kMaxTokens = 1 << 30;   // of a table: a tile's end is within 31 bits
 
 // One of the two row sets that a rotation takes: n heads a row.
@@ -31,6 +32,14 @@ struct RopeFreqs {
 };
 hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, int rows, int head_dim,
                           int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st);
+// The same with a position of each axis: positions [n_axes][stride], `of` the axis of each pair.
+struct RopeAxes {
+    int64_t stride;
+    uint8_t of[kMaxRotary / 2];
+};
+hipError_t launch_kv_rope_axes(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, const RopeAxes& axes, int rows,
+                               int head_dim, int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude,
+                               hipStream_t st);
 
 // Where rows go, or come from: the page table and each row's sequence and position.
 struct KvPlaces {
@@ -75,5 +84,32 @@ size_t kv_attention_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq,
 // whether 64-bit counts hold the call's tiles
 bool kv_attention_counts(const riftkv_cache& c, int n_heads, int64_t n_seq, int64_t max_pages);
 hipError_t launch_kv_attention(const riftkv_cache& c, const KvAttention& a, hipStream_t st);
+
+// `a` with each sequence's own pages, after a prefix; or over the pages of lists [n_seq][n_kv_heads][top].
+size_t kv_shared_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, int prefix_len, int64_t max_pages);
+hipError_t launch_kv_attention_shared(const riftkv_cache& c, const KvAttention& a, const int* prefix_table, int prefix_len,
+                                      hipStream_t st);
+size_t kv_listed_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, int top);
+hipError_t launch_kv_attention_pages(const riftkv_cache& c, const KvAttention& a, const int* lists, int top, hipStream_t st);
+
+hipError_t launch_kv_page_bounds(const riftkv_cache& c, void* bounds, const int* table, int n_seq, int max_pages, const int* begins,
+                                 const int* lens, int* status, hipStream_t st);
+
+struct KvSelect {
+    const void* q;
+    const void* bounds;
+    int64_t ld_q;
+    int n_heads;
+    bool bf16;              // type of q
+    const int* table;
+    int n_seq, max_pages;
+    const int* lens;
+    int first, last, top;
+    int* lists;
+    int* status;
+    void* workspace;
+};
+size_t kv_select_workspace(const riftkv_cache& c, int64_t n_seq, int64_t max_pages);
+hipError_t launch_kv_select_pages(const riftkv_cache& c, const KvSelect& s, hipStream_t st);
 
 }  // namespace rift

@@ -30,13 +30,12 @@
 // e4m3, 20.5 and 21.5; bf16 pages within 2%, the large ones 0.3%.)
 #include <type_traits>
 
-#include "kv_device.h"
+#include "kv_tile.h"
 
 namespace rift {
 
 namespace {
 
-constexpr int kTile = 32;                 // tokens of a tile
 constexpr int kBegins = 1, kEnds = 2;     // a part holds a head's first, last tile
 constexpr int kSplitWaves = 4;            // of a workgroup, where heads are split over workgroups
 constexpr int kMaxWgs = 512;              // two workgroups a CU
@@ -71,8 +70,6 @@ __device__ __forceinline__ int length_of(int len, int max_pages, int shift) {
     return len < 0 || (int64_t)len > ((int64_t)max_pages << shift) ? 0 : len;
 }
 
-__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
-
 // a / b; most operands have 32 bits, and 64-bit division is long.
 __device__ __forceinline__ unsigned long long quotient(unsigned long long a, unsigned long long b) {
     return ((a | b) >> 32) == 0 ? (unsigned)a / (unsigned)b : a / b;
@@ -105,69 +102,6 @@ struct Deal {
         return (int)(tile < longer ? quotient(tile, q + 1) : r + quotient(tile - longer, q));
     }
 };
-
-// Maximum and sum over the four lanes that hold a query's tokens (16 lanes apart).
-__device__ __forceinline__ float quad_max(float x) {
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float quad_sum(float x) {
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Two 8-bit codes (half `hi` of w) as two bf16 values, exact.
-template <riftkv_dtype DT, bool HI>
-__device__ __forceinline__ uint32_t widen(uint32_t w) {
-    if constexpr (DT == RIFTKV_FP8)
-        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
-    else {
-        const float a = (float)(int8_t)(w >> (HI ? 16 : 0)), b = (float)(int8_t)(w >> (HI ? 24 : 8));
-        return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-    }
-}
-
-// Pairs of bf16 terms that add up to a and b: each takes the leading 8 of the bits that are left, so that
-// three hold all 24 (of numbers from 2^-110 on; below, to 2^-133, the last bit of the smallest bf16).  Cut off, not
-// rounded: no term can pass the largest number, and what is left is exact.
-template <int N>
-__device__ __forceinline__ void split_bf16(float a, float b, uint32_t (&w)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-        w[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-        a -= __uint_as_float(x & 0xFFFF0000u);
-        b -= __uint_as_float(y & 0xFFFF0000u);
-    }
-}
-
-template <int N>
-struct Words {
-    typedef uint32_t type __attribute__((ext_vector_type(N)));
-};
-template <>
-struct Words<1> {
-    typedef uint32_t type;
-};
-
-// N words from p.
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char* p) {
-    constexpr int C = N < 4 ? N : 4;
-    typedef typename Words<C>::type vec;
-#pragma unroll
-    for (int i = 0; i < N / C; ++i) {
-        const vec x = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p) + i);
-        if constexpr (C == 1) w[0] = x;
-        else
-#pragma unroll
-            for (int j = 0; j < C; ++j) w[C * i + j] = x[j];
-    }
-}
 
 // Output of a sequence without tokens, or of a length out of range: head group hq, or all (-1).
 template <typename T>

@@ -80,6 +80,35 @@ rift_status check_places(const riftkv_cache* cache, const void* k, int64_t ld_k,
 // a grid of this many small workgroups, or of blocks of them
 constexpr int64_t kMostItems = 1ll << 31;
 
+// A rotation's arguments, and its frequencies as the kernels take them.
+rift_status check_rope(const RopeRows& q, const RopeRows& k, const rift_dtype& dt, const int32_t* positions, int32_t rows,
+                       int32_t head_dim, int32_t rotary_dim, const riftkv_rope_layout& layout, const double* freqs,
+                       double magnitude, RopeFreqs& f) {
+    if (!rows_dt_valid(dt)) return RIFT_ERR_DTYPE;
+    const int lay = enum_bits(layout);
+    if (lay != (int)RIFTKV_ROPE_HALF && lay != (int)RIFTKV_ROPE_INTERLEAVED) return RIFT_ERR_UNSUPPORTED;
+    if (rows < 0 || q.n < 0 || q.n > 4096 || k.n < 0 || k.n > 4096 || head_dim < 1 || head_dim > 256 || rotary_dim < 2 ||
+        rotary_dim > head_dim || rotary_dim % 2 != 0)
+        return RIFT_ERR_SHAPE;
+    if (freqs == nullptr) return RIFT_ERR_NULL;
+    // 2 pi = kTwoPi + kTwoPiRest, to 2^-109 of it
+    constexpr double kTwoPi = 6.283185307179586476925286766559, kTwoPiRest = 2.4492935982947064e-16;
+    for (int j = 0; j < rotary_dim / 2; ++j) {
+        if (!isfinite(freqs[j])) return RIFT_ERR_NONFINITE;
+        f.hi[j] = freqs[j] / kTwoPi;
+        f.lo[j] = (float)((fma(-f.hi[j], kTwoPi, freqs[j]) - f.hi[j] * kTwoPiRest) * (1.0 / kTwoPi));
+    }
+    if (!isfinite((float)magnitude)) return RIFT_ERR_NONFINITE;
+    if (rows == 0 || q.n + k.n == 0) return RIFT_OK;
+    for (const RopeRows* r : {&q, &k})
+        if (positions == nullptr || (r->n > 0 && (r->x == nullptr || r->y == nullptr))) return RIFT_ERR_NULL;
+    for (const RopeRows* r : {&q, &k}) {
+        const int64_t width = (int64_t)r->n * head_dim;
+        if (r->n > 0 && (r->ld_x < width || r->ld_y < width || (r->x == r->y && r->ld_x != r->ld_y))) return RIFT_ERR_SHAPE;
+    }
+    return (int64_t)rows * (q.n + k.n) >= kMostItems ? RIFT_ERR_UNSUPPORTED : RIFT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -130,34 +159,36 @@ rift_status riftkv_rope(const void* q, int64_t ld_q, int32_t n_q, void* q_out, i
                         int64_t ld_k, int32_t n_k, void* k_out, int64_t ld_k_out, rift_dtype dt,
                         const int32_t* positions, int32_t rows, int32_t head_dim, int32_t rotary_dim,
                         riftkv_rope_layout layout, const double* freqs, double magnitude, rift_stream stream) {
-    if (!rows_dt_valid(dt)) return RIFT_ERR_DTYPE;
-    const int lay = enum_bits(layout);
-    if (lay != (int)RIFTKV_ROPE_HALF && lay != (int)RIFTKV_ROPE_INTERLEAVED) return RIFT_ERR_UNSUPPORTED;
-    if (rows < 0 || n_q < 0 || n_q > 4096 || n_k < 0 || n_k > 4096 || head_dim < 1 || head_dim > 256 || rotary_dim < 2 ||
-        rotary_dim > head_dim || rotary_dim % 2 != 0)
-        return RIFT_ERR_SHAPE;
-    if (freqs == nullptr) return RIFT_ERR_NULL;
-    RopeFreqs f;
-    // 2 pi = kTwoPi + kTwoPiRest, to 2^-109 of it
-    constexpr double kTwoPi = 6.283185307179586476925286766559, kTwoPiRest = 2.4492935982947064e-16;
-    for (int j = 0; j < rotary_dim / 2; ++j) {
-        if (!isfinite(freqs[j])) return RIFT_ERR_NONFINITE;
-        f.hi[j] = freqs[j] / kTwoPi;
-        f.lo[j] = (float)((fma(-f.hi[j], kTwoPi, freqs[j]) - f.hi[j] * kTwoPiRest) * (1.0 / kTwoPi));
-    }
-    if (!isfinite((float)magnitude)) return RIFT_ERR_NONFINITE;
-    if (rows == 0 || n_q + n_k == 0) return RIFT_OK;
-    if (positions == nullptr || (n_q > 0 && (q == nullptr || q_out == nullptr)) ||
-        (n_k > 0 && (k == nullptr || k_out == nullptr)))
-        return RIFT_ERR_NULL;
-    const int64_t wq = (int64_t)n_q * head_dim, wk = (int64_t)n_k * head_dim;
-    if ((n_q > 0 && (ld_q < wq || ld_q_out < wq)) || (n_k > 0 && (ld_k < wk || ld_k_out < wk))) return RIFT_ERR_SHAPE;
-    if ((n_q > 0 && q == q_out && ld_q != ld_q_out) || (n_k > 0 && k == k_out && ld_k != ld_k_out)) return RIFT_ERR_SHAPE;
-    if ((int64_t)rows * (n_q + n_k) >= kMostItems) return RIFT_ERR_UNSUPPORTED;
     const RopeRows rq{q, q_out, ld_q, ld_q_out, n_q}, rk{k, k_out, ld_k, ld_k_out, n_k};
+    RopeFreqs f;
+    const rift_status cs = check_rope(rq, rk, dt, positions, rows, head_dim, rotary_dim, layout, freqs, magnitude, f);
+    if (cs != RIFT_OK || rows == 0 || n_q + n_k == 0) return cs;
     return hip_status(launch_kv_rope(rq, rk, dt == RIFT_BF16, positions, rows, head_dim, rotary_dim,
-                                     lay == (int)RIFTKV_ROPE_INTERLEAVED, f, (float)magnitude,
+                                     enum_bits(layout) == (int)RIFTKV_ROPE_INTERLEAVED, f, (float)magnitude,
                                      static_cast<hipStream_t>(stream)));
+}
+
+rift_status riftkv_rope_axes(const void* q, int64_t ld_q, int32_t n_q, void* q_out, int64_t ld_q_out, const void* k,
+                             int64_t ld_k, int32_t n_k, void* k_out, int64_t ld_k_out, rift_dtype dt,
+                             const int32_t* positions, int32_t n_axes, int32_t rows, int32_t head_dim, int32_t rotary_dim,
+                             riftkv_rope_layout layout, const double* freqs, const int32_t* axes, double magnitude,
+                             rift_stream stream) {
+    const RopeRows rq{q, q_out, ld_q, ld_q_out, n_q}, rk{k, k_out, ld_k, ld_k_out, n_k};
+    RopeFreqs f;
+    const rift_status cs = check_rope(rq, rk, dt, positions, rows, head_dim, rotary_dim, layout, freqs, magnitude, f);
+    if (cs != RIFT_OK) return cs;
+    if (n_axes < 1 || n_axes > kMaxAxes) return RIFT_ERR_SHAPE;
+    if (axes == nullptr) return RIFT_ERR_NULL;
+    RopeAxes x;
+    x.stride = rows;
+    for (int j = 0; j < rotary_dim / 2; ++j) {
+        if (axes[j] < 0 || axes[j] >= n_axes) return RIFT_ERR_SHAPE;
+        x.of[j] = (uint8_t)axes[j];
+    }
+    if (rows == 0 || n_q + n_k == 0) return RIFT_OK;
+    return hip_status(launch_kv_rope_axes(rq, rk, dt == RIFT_BF16, positions, x, rows, head_dim, rotary_dim,
+                                          enum_bits(layout) == (int)RIFTKV_ROPE_INTERLEAVED, f, (float)magnitude,
+                                          static_cast<hipStream_t>(stream)));
 }
 
 rift_status riftkv_write(const riftkv_cache* cache, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
@@ -215,6 +246,118 @@ rift_status riftkv_attention(const riftkv_cache* cache, const void* q, int64_t l
     if (!check_rows(q, ld_q, width, dt) || !check_rows(out, ld_out, width, dt)) return RIFT_ERR_SHAPE;
     const KvAttention a{q, out, ld_q, ld_out, n_heads, dt == RIFT_BF16, page_table, n_seq, max_pages, lens, scale, status, workspace};
     return hip_status(launch_kv_attention(*cache, a, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+// What the attentions over ranges of pages check alike, but for their workspace; n_seq == 0: no arrays.
+rift_status check_ranges(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads, const rift_dtype& dt,
+                         const int32_t* table, int32_t n_seq, int32_t max_pages, const int32_t* lens, const int32_t* status) {
+    const rift_status cs = kv_check_cache(cache, true);
+    if (cs != RIFT_OK) return cs;
+    if (!rows_dt_valid(dt) || (dt == RIFT_BF16 && cache->dt == RIFTKV_F32)) return RIFT_ERR_DTYPE;
+    if (!attention_shape(*cache, n_heads, n_seq, max_pages)) return RIFT_ERR_SHAPE;
+    if (status == nullptr) return RIFT_ERR_NULL;
+    if (n_seq == 0) return RIFT_OK;
+    if (q == nullptr || lens == nullptr || (table == nullptr && max_pages > 0)) return RIFT_ERR_NULL;
+    return check_rows(q, ld_q, (int64_t)n_heads * cache->head_dim, dt) ? RIFT_OK : RIFT_ERR_SHAPE;
+}
+
+rift_status check_out(const riftkv_cache& c, const void* out, int64_t ld_out, int32_t n_heads, const rift_dtype& dt, float scale) {
+    if (!isfinite(scale * 1.4426950408889634f)) return RIFT_ERR_NONFINITE;   // the base-2 exponent's
+    if (out == nullptr) return RIFT_ERR_NULL;
+    return check_rows(out, ld_out, (int64_t)n_heads * c.head_dim, dt) ? RIFT_OK : RIFT_ERR_SHAPE;
+}
+
+bool shared_shape(const riftkv_cache& c, int32_t n_heads, int32_t n_seq, int32_t prefix_len, int32_t max_pages) {
+    return attention_shape(c, n_heads, n_seq, max_pages) && prefix_len >= 0 && prefix_len <= kMaxTokens;
+}
+
+constexpr int32_t kMostListed = 1 << 20;
+bool listed_shape(const riftkv_cache& c, int32_t n_heads, int32_t n_seq, int32_t top) {
+    return attention_shape(c, n_heads, n_seq, 0) && top >= 1 && top <= kMostListed && (int64_t)top * c.page_size <= kMaxTokens;
+}
+
+rift_status check_workspace(const void* workspace, size_t ws_bytes, size_t needed) {
+    if (workspace == nullptr) return RIFT_ERR_NULL;
+    return misaligned(workspace, 256) || ws_bytes < needed ? RIFT_ERR_WORKSPACE : RIFT_OK;
+}
+}  // namespace
+
+size_t riftkv_attention_shared_workspace_size(const riftkv_cache* cache, int32_t n_heads, int32_t n_seq, int32_t prefix_len,
+                                              int32_t max_pages) {
+    if (kv_check_cache(cache, false) != RIFT_OK || !shared_shape(*cache, n_heads, n_seq, prefix_len, max_pages)) return 0;
+    return kv_shared_workspace(*cache, n_heads, n_seq, prefix_len, max_pages);
+}
+
+rift_status riftkv_attention_shared(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads, rift_dtype dt,
+                                    const int32_t* prefix_table, int32_t prefix_len, const int32_t* page_table, int32_t n_seq,
+                                    int32_t max_pages, const int32_t* lens, float scale, void* out, int64_t ld_out,
+                                    int32_t* status, void* workspace, size_t ws_bytes, rift_stream stream) {
+    rift_status cs = check_ranges(cache, q, ld_q, n_heads, dt, page_table, n_seq, max_pages, lens, status);
+    if (cs != RIFT_OK) return cs;
+    if (!shared_shape(*cache, n_heads, n_seq, prefix_len, max_pages)) return RIFT_ERR_SHAPE;
+    cs = check_workspace(workspace, ws_bytes, kv_shared_workspace(*cache, n_heads, n_seq, prefix_len, max_pages));
+    if (cs != RIFT_OK || n_seq == 0) return cs;
+    if (prefix_table == nullptr && prefix_len > 0) return RIFT_ERR_NULL;
+    cs = check_out(*cache, out, ld_out, n_heads, dt, scale);
+    if (cs != RIFT_OK) return cs;
+    const KvAttention a{q, out, ld_q, ld_out, n_heads, dt == RIFT_BF16, page_table, n_seq, max_pages, lens, scale, status, workspace};
+    return hip_status(launch_kv_attention_shared(*cache, a, prefix_table, prefix_len, static_cast<hipStream_t>(stream)));
+}
+
+rift_status riftkv_page_bounds(const riftkv_cache* cache, void* bounds, const int32_t* page_table, int32_t n_seq, int32_t max_pages,
+                               const int32_t* begins, const int32_t* lens, int32_t* status, rift_stream stream) {
+    const rift_status cs = kv_check_cache(cache, true);
+    if (cs != RIFT_OK) return cs;
+    if (!check_table(*cache, n_seq, max_pages)) return RIFT_ERR_SHAPE;
+    if (status == nullptr) return RIFT_ERR_NULL;
+    if (n_seq == 0) return RIFT_OK;
+    if (bounds == nullptr || lens == nullptr || (page_table == nullptr && max_pages > 0)) return RIFT_ERR_NULL;
+    if (misaligned(bounds, 16)) return RIFT_ERR_SHAPE;
+    return hip_status(launch_kv_page_bounds(*cache, bounds, page_table, n_seq, max_pages, begins, lens, status,
+                                            static_cast<hipStream_t>(stream)));
+}
+
+size_t riftkv_select_pages_workspace_size(const riftkv_cache* cache, int32_t n_seq, int32_t max_pages) {
+    if (kv_check_cache(cache, false) != RIFT_OK || !attention_shape(*cache, cache->n_kv_heads, n_seq, max_pages)) return 0;
+    return kv_select_workspace(*cache, n_seq, max_pages);
+}
+
+rift_status riftkv_select_pages(const riftkv_cache* cache, const void* bounds, const void* q, int64_t ld_q, int32_t n_heads,
+                                rift_dtype dt, const int32_t* page_table, int32_t n_seq, int32_t max_pages, const int32_t* lens,
+                                int32_t keep_first, int32_t keep_last, int32_t* pages, int32_t top, int32_t* status,
+                                void* workspace, size_t ws_bytes, rift_stream stream) {
+    rift_status cs = check_ranges(cache, q, ld_q, n_heads, dt, page_table, n_seq, max_pages, lens, status);
+    if (cs != RIFT_OK) return cs;
+    if (top < 1 || top > kMostListed || keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > top) return RIFT_ERR_SHAPE;
+    cs = check_workspace(workspace, ws_bytes, kv_select_workspace(*cache, n_seq, max_pages));
+    if (cs != RIFT_OK || n_seq == 0) return cs;
+    if (bounds == nullptr || pages == nullptr) return RIFT_ERR_NULL;
+    if (misaligned(bounds, 16)) return RIFT_ERR_SHAPE;
+    const KvSelect s{q, bounds, ld_q, n_heads, dt == RIFT_BF16, page_table, n_seq, max_pages, lens, keep_first, keep_last, top,
+                     pages, status, workspace};
+    return hip_status(launch_kv_select_pages(*cache, s, static_cast<hipStream_t>(stream)));
+}
+
+size_t riftkv_attention_pages_workspace_size(const riftkv_cache* cache, int32_t n_heads, int32_t n_seq, int32_t top) {
+    if (kv_check_cache(cache, false) != RIFT_OK || !listed_shape(*cache, n_heads, n_seq, top)) return 0;
+    return kv_listed_workspace(*cache, n_heads, n_seq, top);
+}
+
+rift_status riftkv_attention_pages(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads, rift_dtype dt,
+                                   const int32_t* page_table, int32_t n_seq, int32_t max_pages, const int32_t* lens,
+                                   const int32_t* pages, int32_t top, float scale, void* out, int64_t ld_out, int32_t* status,
+                                   void* workspace, size_t ws_bytes, rift_stream stream) {
+    rift_status cs = check_ranges(cache, q, ld_q, n_heads, dt, page_table, n_seq, max_pages, lens, status);
+    if (cs != RIFT_OK) return cs;
+    if (!listed_shape(*cache, n_heads, n_seq, top)) return RIFT_ERR_SHAPE;
+    cs = check_workspace(workspace, ws_bytes, kv_listed_workspace(*cache, n_heads, n_seq, top));
+    if (cs != RIFT_OK || n_seq == 0) return cs;
+    if (pages == nullptr) return RIFT_ERR_NULL;
+    cs = check_out(*cache, out, ld_out, n_heads, dt, scale);
+    if (cs != RIFT_OK) return cs;
+    const KvAttention a{q, out, ld_q, ld_out, n_heads, dt == RIFT_BF16, page_table, n_seq, max_pages, lens, scale, status, workspace};
+    return hip_status(launch_kv_attention_pages(*cache, a, pages, top, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

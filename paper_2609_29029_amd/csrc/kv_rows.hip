@@ -80,10 +80,18 @@ __device__ __forceinline__ float2 rope_turn(int position, const RopeFreqs& freqs
     return make_float2(c * magnitude, s * magnitude);
 }
 
+// Whose position turns pair j of a row: the row's one, or its axis'.
+struct OneAxis {
+    __device__ __forceinline__ int position(const int* positions, int row, int) const { return positions[row]; }
+};
+struct SeveralAxes : RopeAxes {
+    __device__ __forceinline__ int position(const int* positions, int row, int j) const { return positions[of[j] * stride + row]; }
+};
+
 // Any sizes, strides and alignment: a wave takes one head of one row.
-template <typename T>
+template <typename T, typename Axes>
 __global__ void __launch_bounds__(64)
-rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int head_dim, int rotary_dim, int interleaved,
+rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, Axes axes, int head_dim, int rotary_dim, int interleaved,
                 RopeFreqs freqs, float magnitude) {
     const int heads = q.n + k.n;
     const int row = blockIdx.x / heads, h = blockIdx.x - row * heads;
@@ -92,7 +100,7 @@ rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int h
     const size_t x0 = (size_t)row * r.ld_x + hoff, y0 = (size_t)row * r.ld_y + hoff;
     const int half = rotary_dim / 2;
     for (int j = threadIdx.x; j < half; j += 64) {
-        const float2 cs = rope_turn(positions[row], freqs, j, magnitude);
+        const float2 cs = rope_turn(axes.position(positions, row, j), freqs, j, magnitude);
         const int i1 = interleaved ? 2 * j : j, i2 = interleaved ? 2 * j + 1 : j + half;
         const float2 y = rotate_pair(load_f32<T>(r.x, x0 + i1), load_f32<T>(r.x, x0 + i2), cs);
         store_f32<T>(r.y, y0 + i1, y.x);
@@ -106,9 +114,9 @@ rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int h
 // half layout, 57.5 us, in twos 60.6, in fours 63.6.)  A head's items are, in the half
 // layout, rotary_dim / 16 pairs of eights, then the eights that are copied; interleaved,
 // head_dim / 8 eights of four pairs each or copied.
-template <typename T, bool INTERLEAVED>
+template <typename T, bool INTERLEAVED, typename Axes>
 __global__ void __launch_bounds__(kThreads)
-rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int per, int head_dim, int rotary_dim,
+rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, Axes axes, int per, int head_dim, int rotary_dim,
             RopeFreqs freqs, float magnitude) {
     __shared__ float2 turns[kMaxRotary / 2];
     const int row = blockIdx.x, heads = q.n + k.n, h0 = blockIdx.y * per;
@@ -133,7 +141,7 @@ rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int per, 
         if (!INTERLEAVED && v < turned) xb = load_eight<T>(x, from + half + e);
     };
     if (h < end) load();
-    if (threadIdx.x < half) turns[threadIdx.x] = rope_turn(positions[row], freqs, threadIdx.x, magnitude);
+    if (threadIdx.x < half) turns[threadIdx.x] = rope_turn(axes.position(positions, row, threadIdx.x), freqs, threadIdx.x, magnitude);
     __syncthreads();
     while (h < end) {
         const int v0 = v;
@@ -484,10 +492,9 @@ hipError_t launch_move(const riftkv_cache& c, const void* k, int64_t ld_k, const
     return hipErrorInvalidValue;
 }
 
-}  // namespace
-
-hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, int rows, int head_dim,
-                          int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st) {
+template <typename Axes>
+hipError_t launch_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, const Axes& axes, int rows, int head_dim,
+                       int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st) {
     const int heads = q.n + k.n;
     // rows from r on
     auto from = [&](const RopeRows& x, int64_t r) {
@@ -513,11 +520,11 @@ hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const
     if (head_dim % 8 != 0 || rotary_dim % 16 != 0 || !aligned(q) || !aligned(k)) {
         auto run = [&](auto kernel) {
             return in_pieces(kMostThreads / 64 / heads, [&](unsigned n, int64_t r) {
-                hipLaunchKernelGGL(kernel, dim3(n * (unsigned)heads), dim3(64), 0, st, from(q, r), from(k, r), positions + r,
+                hipLaunchKernelGGL(kernel, dim3(n * (unsigned)heads), dim3(64), 0, st, from(q, r), from(k, r), positions + r, axes,
                                    head_dim, rotary_dim, interleaved ? 1 : 0, freqs, magnitude);
             });
         };
-        return bf16 ? run(rope_any_kernel<bf16_t>) : run(rope_any_kernel<float>);
+        return bf16 ? run(rope_any_kernel<bf16_t, Axes>) : run(rope_any_kernel<float, Axes>);
     }
     // all heads of a row a workgroup, so that its sines are worked out once, or fewer where that
     // leaves CUs without work (32 rows of 40 heads: 2.6 us, with 512 workgroups 3.4)
@@ -526,11 +533,24 @@ hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const
     auto run = [&](auto kernel) {
         return in_pieces(kMostThreads / kThreads, [&](unsigned n, int64_t r) {
             hipLaunchKernelGGL(kernel, dim3(n, (unsigned)((heads + per - 1) / per)), dim3(kThreads), 0, st, from(q, r), from(k, r),
-                               positions + r, per, head_dim, rotary_dim, freqs, magnitude);
+                               positions + r, axes, per, head_dim, rotary_dim, freqs, magnitude);
         });
     };
-    if (bf16) return interleaved ? run(rope_kernel<bf16_t, true>) : run(rope_kernel<bf16_t, false>);
-    return interleaved ? run(rope_kernel<float, true>) : run(rope_kernel<float, false>);
+    if (bf16) return interleaved ? run(rope_kernel<bf16_t, true, Axes>) : run(rope_kernel<bf16_t, false, Axes>);
+    return interleaved ? run(rope_kernel<float, true, Axes>) : run(rope_kernel<float, false, Axes>);
+}
+
+}  // namespace
+
+hipError_t launch_kv_rope(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, int rows, int head_dim,
+                          int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude, hipStream_t st) {
+    return launch_rope(q, k, bf16, positions, OneAxis{}, rows, head_dim, rotary_dim, interleaved, freqs, magnitude, st);
+}
+
+hipError_t launch_kv_rope_axes(const RopeRows& q, const RopeRows& k, bool bf16, const int* positions, const RopeAxes& axes, int rows,
+                               int head_dim, int rotary_dim, bool interleaved, const RopeFreqs& freqs, float magnitude,
+                               hipStream_t st) {
+    return launch_rope(q, k, bf16, positions, SeveralAxes{axes}, rows, head_dim, rotary_dim, interleaved, freqs, magnitude, st);
 }
 
 hipError_t launch_kv_decode_prep(const int* positions, int n_seq, int64_t capacity, int hd, float rope_base, float2* rope,

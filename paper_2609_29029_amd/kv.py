@@ -15,9 +15,11 @@ from ._lib import RIFT_BF16, RIFT_F32, LayerWeights, ModelCfg, _check, layer_str
 
 RIFTKV_F32, RIFTKV_BF16, RIFTKV_FP8, RIFTKV_INT8 = 0, 1, 2, 3
 # Every symbol include/rift_kv.h declares, in declaration order.
-KV_EXPORTS = ("riftkv_abi_version", "riftkv_rope_freqs", "riftkv_rope", "riftkv_write", "riftkv_read",
-              "riftkv_attention_workspace_size", "riftkv_attention", "riftkv_decode_workspace_size",
-              "riftkv_decode_step")
+KV_EXPORTS = ("riftkv_abi_version", "riftkv_rope_freqs", "riftkv_rope", "riftkv_rope_axes", "riftkv_write", "riftkv_read",
+              "riftkv_attention_workspace_size", "riftkv_attention", "riftkv_attention_shared_workspace_size",
+              "riftkv_attention_shared", "riftkv_page_bounds", "riftkv_select_pages_workspace_size",
+              "riftkv_select_pages", "riftkv_attention_pages_workspace_size", "riftkv_attention_pages",
+              "riftkv_decode_workspace_size", "riftkv_decode_step")
 ROPE_SCALINGS = ("none", "linear", "base", "ramp", "bands")
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 
@@ -54,6 +56,8 @@ def _load() -> ctypes.CDLL:
         L.riftkv_rope_freqs.argtypes = [P, P, P]
         L.riftkv_rope.restype = I32
         L.riftkv_rope.argtypes = [P, I64, I32, P, I64, P, I64, I32, P, I64, I32, P, I32, I32, I32, I32, P, F64, P]
+        L.riftkv_rope_axes.restype = I32
+        L.riftkv_rope_axes.argtypes = [P, I64, I32, P, I64, P, I64, I32, P, I64, I32, P, I32, I32, I32, I32, I32, P, P, F64, P]
         for name in ("riftkv_write", "riftkv_read"):
             getattr(L, name).restype = I32
             getattr(L, name).argtypes = [P, P, I64, P, I64, I32, P, I32, I32, P, P, I32, P, P]
@@ -61,6 +65,20 @@ def _load() -> ctypes.CDLL:
         L.riftkv_attention_workspace_size.argtypes = [P, I32, I32, I32]
         L.riftkv_attention.restype = I32
         L.riftkv_attention.argtypes = [P, P, I64, I32, I32, P, I32, I32, P, F32, P, I64, P, P, SZ, P]
+        L.riftkv_attention_shared_workspace_size.restype = SZ
+        L.riftkv_attention_shared_workspace_size.argtypes = [P, I32, I32, I32, I32]
+        L.riftkv_attention_shared.restype = I32
+        L.riftkv_attention_shared.argtypes = [P, P, I64, I32, I32, P, I32, P, I32, I32, P, F32, P, I64, P, P, SZ, P]
+        L.riftkv_page_bounds.restype = I32
+        L.riftkv_page_bounds.argtypes = [P, P, P, I32, I32, P, P, P, P]
+        L.riftkv_select_pages_workspace_size.restype = SZ
+        L.riftkv_select_pages_workspace_size.argtypes = [P, I32, I32]
+        L.riftkv_select_pages.restype = I32
+        L.riftkv_select_pages.argtypes = [P, P, P, I64, I32, I32, P, I32, I32, P, I32, I32, P, I32, P, P, SZ, P]
+        L.riftkv_attention_pages_workspace_size.restype = SZ
+        L.riftkv_attention_pages_workspace_size.argtypes = [P, I32, I32, I32]
+        L.riftkv_attention_pages.restype = I32
+        L.riftkv_attention_pages.argtypes = [P, P, I64, I32, I32, P, I32, I32, P, P, I32, F32, P, I64, P, P, SZ, P]
         L.riftkv_decode_workspace_size.restype = SZ
         L.riftkv_decode_workspace_size.argtypes = [P, P, I32, I32]
         L.riftkv_decode_step.restype = I32
@@ -186,12 +204,7 @@ def riftkv_rope_freqs(rotary_dim: int, base: float = 10000.0, scaling: str = "no
     return out, float(mag.value)
 
 
-def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "half", magnitude: float = 1.0,
-                stream=None) -> None:
-    """Rotates the rows q and k (either may be None) into q_out and k_out (None: in
-    place) by positions [rows] i32.  freqs: float64 numpy array of rotary_dim / 2
-    angles a position (riftkv_rope_freqs)."""
-    L = _lib or _load()
+def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, stream, axes=None):
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
@@ -222,18 +235,46 @@ def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "h
     lay = ROPE_LAYOUTS.get(layout)
     if lay is None:
         raise ValueError(f"layout: one of {tuple(ROPE_LAYOUTS)}")
-    flags = freqs.flags
-    if freqs.dtype.str != "<f8" or not flags.c_contiguous or freqs.size == 0:
-        raise TypeError("freqs: expected a contiguous float64 array")
-    # (an array's own .ctypes takes three times as long)
-    fp = ctypes.byref(ctypes.c_double.from_buffer(freqs)) if flags.writeable else freqs.ctypes.data
-    if positions.dtype is not _I32 or positions.shape != (rows,) or not positions.is_contiguous() or positions.get_device() != dev:
-        _dense(positions, _I32, (rows,), dev, "positions")
+    fp = _host(freqs, "<f8", ctypes.c_double, "freqs: expected a contiguous float64 array")
+    if axes is None:
+        shape, places, by_axis = (rows,), (rows,), ()
+    else:
+        if axes.shape != freqs.shape:
+            raise ValueError("axes: expected as many as freqs")
+        shape = (positions.shape[0], rows)
+        places = shape
+        by_axis = (_host(axes, "<i4", ctypes.c_int32, "axes: expected a contiguous int32 array"),)
+    if positions.dtype is not _I32 or positions.shape != shape or not positions.is_contiguous() or positions.get_device() != dev:
+        _dense(positions, _I32, shape, dev, "positions")
     st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
-    args = (pq, lq, nq, poq, loq, pk, lk, nk, pok, lok, dt, positions.data_ptr(), rows, hd, 2 * freqs.size, lay, fp, magnitude, st)
-    st = L.riftkv_rope(*args) if dev == _device() else _elsewhere(dev, L.riftkv_rope, *args)
+    args = (pq, lq, nq, poq, loq, pk, lk, nk, pok, lok, dt, positions.data_ptr(), *places, hd, 2 * freqs.size, lay, fp, *by_axis,
+            magnitude, st)
+    st = fn(*args) if dev == _device() else _elsewhere(dev, fn, *args)
     if st:
-        _check(st, "riftkv_rope")
+        _check(st, name)
+
+
+def _host(a, kind, ctype, what):
+    """Address of a numpy array (its own .ctypes takes three times as long)."""
+    flags = a.flags
+    if a.dtype.str != kind or not flags.c_contiguous or a.size == 0:
+        raise TypeError(what)
+    return ctypes.byref(ctype.from_buffer(a)) if flags.writeable else a.ctypes.data
+
+
+def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "half", magnitude: float = 1.0,
+                stream=None) -> None:
+    """Rotates the rows q and k (either may be None) into q_out and k_out (None: in
+    place) by positions [rows] i32.  freqs: float64 numpy array of rotary_dim / 2
+    angles a position (riftkv_rope_freqs)."""
+    _rope("riftkv_rope", (_lib or _load()).riftkv_rope, q, k, positions, freqs, q_out, k_out, layout, magnitude, stream)
+
+
+def riftkv_rope_axes(q, k, positions, freqs, axes, q_out=None, k_out=None, layout: str = "half", magnitude: float = 1.0,
+                     stream=None) -> None:
+    """The same by positions [n_axes][rows] i32 on several axes: pair j turns by
+    positions[axes[j]].  axes: int32 numpy array of rotary_dim / 2."""
+    _rope("riftkv_rope_axes", (_lib or _load()).riftkv_rope_axes, q, k, positions, freqs, q_out, k_out, layout, magnitude, stream, axes)
 
 
 # ----------------------------------------------------------------------------- rows

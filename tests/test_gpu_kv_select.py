@@ -1,0 +1,356 @@
+"""Page bounds and the selection of pages against plain forms, and with the calls that they are used with."""
+import math
+
+import pytest
+import torch
+
+from tests.kv_ranges_testlib import TYPES, attend_lists, bounds_of, check, filled, randn, selection
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def R():
+    import paper_2609_29029_amd as R
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    R.load()
+    return R
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def new_bounds(P, fill=99.0):
+    n_pages, n_kv, _, hd = P.k.shape
+    return torch.full((n_pages, n_kv, 2, hd), fill, dtype=torch.float32 if P.store == torch.float32 else torch.bfloat16, device="cuda")
+
+
+def same(a, b):
+    """Equal, NaN too."""
+    return bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all())
+
+
+# ----------------------------------------------------------------------------- bounds
+@pytest.mark.parametrize("store", ["bf16", "f32", "fp8", "int8"])
+@pytest.mark.parametrize("n_kv, hd, page, lens, begins", [
+    (2, 128, 16, [40, 1, 0, 16, 100], None),
+    (1, 64, 32, [70, 33, 32], [0, 32, 31]),
+    (3, 128, 64, [200, 130, 64, 65], [199, 64, 64, -9]),
+    (5, 64, 16, [17, 500], [17, 77]),
+    (2, 128, 256, [700], [300]),
+])
+def test_bounds(R, store, n_kv, hd, page, lens, begins):
+    """Every page that holds a new token, exactly; no other."""
+    P = filled(R, store, n_kv, hd, page, lens, seed=hd)
+    b = new_bounds(P)
+    want = b.clone()
+    for i, n in enumerate(lens):
+        first = 0 if begins is None else max(0, begins[i])
+        if n > first:
+            for p in range(first // page, -(-n // page)):
+                want[int(P.table[i, p])] = bounds_of(P, i, n, p).to(b.dtype).cuda()
+    R.riftkv_page_bounds(P.cache, b, P.table, i32(lens), P.status, begins=None if begins is None else i32(begins))
+    assert same(b, want) and int(P.status) == 0
+
+
+@pytest.mark.parametrize("store", ["bf16", "f32", "fp8", "int8"])
+def test_bounds_of_what_is_not_a_number(R, store):
+    lens = [60]
+    P = filled(R, store, 2, 64, 16, lens)
+    x = randn(1, 3, 2, 2, 64, dtype=torch.float32 if store == "f32" else torch.bfloat16)
+    x[0, 0, 1, 5], x[1, 0, 0, 7], x[2, 0, 1, 9] = math.nan, math.inf, -math.inf
+    for j, pos in enumerate((3, 20, 59)):
+        P.put(R, 0, x[j:j + 1, 0], x[j:j + 1, 1], first=pos)
+    b = new_bounds(P)
+    R.riftkv_page_bounds(P.cache, b, P.table, i32(lens), P.status)
+    for p in range(4):
+        got, want = b[int(P.table[0, p])].cpu(), bounds_of(P, 0, 60, p).to(b.dtype)
+        assert same(got, want)
+    assert bool(torch.isnan(b[int(P.table[0, 0]), 1, 0, 5]))
+    assert int(P.status) == 0
+
+
+def test_bounds_of_many_uneven_sequences(R):
+    """One long sequence among many short ones, and more sequences than a workgroup has threads."""
+    lens = [(13 * i) % 40 for i in range(700)]
+    lens[411] = 8000
+    P = filled(R, "bf16", 2, 64, 16, [9000])
+    table = torch.full((700, 500), -7, dtype=torch.int32)
+    g = torch.Generator().manual_seed(1)
+    pool = torch.randperm(560, generator=g)
+    at = 0
+    for i, n in enumerate(lens):   # full pages of the pool may be any sequence's; the partial ones are read up to their length
+        h = -(-n // 16)
+        for p in range(h):
+            table[i, p] = int(P.table[0, int(pool[(at + p) % 560])])
+        at += h
+    b = new_bounds(P)
+    # sequence by sequence, the pages of one at a time
+    for i in (0, 1, 5, 411, 699):
+        one = i32([lens[j] if j == i else 0 for j in range(700)])
+        b.fill_(99.0)
+        R.riftkv_page_bounds(P.cache, b, table.cuda(), one, P.status)
+        want = torch.full_like(b, 99.0)
+        for p in range(-(-lens[i] // 16)):
+            k = P.k[int(table[i, p]), :, :min(16, lens[i] - 16 * p)]
+            want[int(table[i, p])] = torch.stack((k.amin(1), k.amax(1)), 1)
+        assert same(b, want), i
+    b.fill_(99.0)
+    whole = i32([16 * (n // 16) for n in lens])              # only full pages: the same whoever computes them
+    R.riftkv_page_bounds(P.cache, b, table.cuda(), whole, P.status)
+    want = torch.full_like(b, 99.0)
+    for i, n in enumerate(lens):
+        for p in range(n // 16):
+            k = P.k[int(table[i, p])]
+            want[int(table[i, p])] = torch.stack((k.amin(1), k.amax(1)), 1)
+    assert same(b, want) and int(P.status) == 0
+
+
+def test_bounds_bad_pages_and_lengths(R):
+    lens = [40, 33, 20]
+    P = filled(R, "bf16", 2, 64, 16, lens)
+    good = new_bounds(P)
+    R.riftkv_page_bounds(P.cache, good, P.table, i32(lens), P.status)
+    for bad in (-1, P.k.shape[0], 2 ** 31 - 1):
+        table = P.table.clone()
+        table[1, 1] = bad
+        b = new_bounds(P)
+        R.riftkv_page_bounds(P.cache, b, table, i32(lens), P.status)
+        assert int(P.status) == 2
+        P.status.zero_()
+        want = good.clone()
+        want[int(P.table[1, 1])] = 99.0
+        assert same(b, want)
+    for n in (-1, P.table.shape[1] * 16 + 1, 2 ** 31 - 1, -2 ** 31):
+        b = new_bounds(P)
+        R.riftkv_page_bounds(P.cache, b, P.table, i32([40, n, 20]), P.status)
+        assert int(P.status) == 2
+        P.status.zero_()
+        want = good.clone()
+        want[P.table[1, :3].long()] = 99.0
+        assert same(b, want)
+
+
+# ----------------------------------------------------------------------------- selection
+def random_bounds(seed, n_pages, n_kv, hd, dtype):
+    a, b = randn(seed, n_pages, n_kv, 1, hd, dtype=dtype), randn(seed + 1, n_pages, n_kv, 1, hd, dtype=dtype)
+    return torch.cat((torch.minimum(a, b), torch.maximum(a, b)), 2).contiguous()
+
+
+def select(R, P, bounds, q, lens, top, first=1, last=1, stream=None):
+    n = q.shape[0]
+    pages = torch.full((n, P.k.shape[1], top), -77, dtype=torch.int32, device="cuda")
+    ws = torch.full((max(256, R.riftkv_select_pages_workspace_size(P.cache, n, P.table.shape[1])),), 255, dtype=torch.uint8, device="cuda")
+    R.riftkv_select_pages(P.cache, bounds, q, P.table, i32(lens), pages, ws, P.status, keep_first=first, keep_last=last, stream=stream)
+    return pages
+
+
+def held(lens, page):
+    return [-(-n // page) for n in lens]
+
+
+@pytest.mark.parametrize("dt, store", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32"), ("bf16", "fp8"), ("f32", "int8")])
+@pytest.mark.parametrize("n_kv, group, hd, page, lens, top, first, last", [
+    (2, 4, 128, 16, [1600, 40, 0, 1, 1601], 10, 1, 2),
+    (1, 1, 64, 16, [500, 480], 3, 0, 0),
+    (3, 5, 64, 32, [3000, 96, 97], 3, 2, 1),
+    (1, 20, 128, 16, [700], 40, 1, 1),
+    (4, 8, 128, 64, [6400, 5000, 64], 1, 0, 1),
+    (2, 2, 64, 16, [900], 57, 0, 4),
+    (2, 2, 64, 16, [900], 56, 0, 4),
+])
+def test_select(R, dt, store, n_kv, group, hd, page, lens, top, first, last):
+    P = filled(R, store, n_kv, hd, page, [0] * len(lens))
+    n_pages = sum(held(lens, page)) + 2
+    P.k = torch.zeros(n_pages, n_kv, page, hd, dtype=P.k.dtype, device="cuda")
+    P.ks = torch.zeros(P.k.shape[:3], dtype=torch.uint8, device="cuda") if P.ks is not None else None
+    P.cache = R.riftkv_cache(P.k, P.k, P.ks, P.ks)
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(5)).int()
+    P.table = torch.full((len(lens), max(held(lens, page)) + 3), -7, dtype=torch.int32)
+    at = 0
+    for i, h in enumerate(held(lens, page)):
+        P.table[i, :h] = order[at:at + h]
+        at += h
+    P.table = P.table.cuda()
+    bounds = random_bounds(3, n_pages, n_kv, hd, torch.float32 if store == "f32" else torch.bfloat16)
+    q = randn(4, len(lens), n_kv * group, hd, dtype=TYPES[dt])
+    got = select(R, P, bounds, q, lens, top, first, last).cpu()
+    assert torch.equal(got, selection(bounds, P.table, q, held(lens, page), n_kv, top, first, last))
+    assert int(P.status) == 0
+
+
+def plain_cache(R, n_kv, hd, page, n_pages, seqs, wide):
+    """A cache whose keys nothing reads, and a table of all its pages in order."""
+    class C:
+        pass
+    P = C()
+    P.k = torch.empty(n_pages, n_kv, page, hd, dtype=torch.bfloat16, device="cuda")
+    P.cache = R.riftkv_cache(P.k, P.k)
+    P.page = page
+    P.table = torch.arange(seqs * wide, dtype=torch.int32, device="cuda").view(seqs, wide) % n_pages
+    P.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    return P
+
+
+def test_select_ties_go_to_the_lowest_page(R):
+    """Pages of a few kinds, so that hundreds share a score; zeros of either sign are one score."""
+    P = plain_cache(R, 2, 64, 16, 600, 2, 300)
+    kinds = random_bounds(7, 3, 2, 64, torch.bfloat16)
+    kinds[2] = 0.0
+    g = torch.Generator().manual_seed(2)
+    bounds = kinds[torch.randint(0, 3, (600,), generator=g).cuda()].contiguous()
+    bounds[:100][bounds[:100] == 0] = -0.0
+    q = randn(4, 2, 4, 64)
+    q[:, :, 32:] = 0
+    lens = [4800, 4790]
+    for top in (2, 20, 150, 280):
+        got = select(R, P, bounds, q, lens, top).cpu()
+        assert torch.equal(got, selection(bounds, P.table, q, [300, 300], 2, top, 1, 1)), top
+
+
+@pytest.mark.parametrize("pages", [1023, 1024, 1025, 5000, 40000])
+def test_select_from_many_pages(R, pages):
+    P = plain_cache(R, 2, 64, 16, pages, 1, pages)
+    bounds = random_bounds(8, pages, 2, 64, torch.bfloat16)
+    q = randn(4, 1, 6, 64)
+    for top, first, last in ((64, 1, 2), (1000, 0, 0)):
+        got = select(R, P, bounds, q, [16 * pages - 5], top, first, last).cpu()
+        assert torch.equal(got, selection(bounds, P.table, q, [pages], 2, top, first, last))
+
+
+def test_select_many_sequences(R):
+    P = plain_cache(R, 1, 64, 16, 900, 300, 60)
+    bounds = random_bounds(9, 900, 1, 64, torch.bfloat16)
+    q = randn(4, 300, 3, 64)
+    lens = [(37 * i) % 961 for i in range(300)]
+    got = select(R, P, bounds, q, lens, 12).cpu()
+    assert torch.equal(got, selection(bounds, P.table, q, held(lens, 16), 1, 12, 1, 1))
+
+
+def test_select_scores_that_float32_confuses(R):
+    """Pages whose scores differ by one part in 2^40: products of 48 bits, added in 64."""
+    P = plain_cache(R, 1, 64, 16, 50, 1, 50)
+    P.k = torch.empty(50, 1, 16, 64, device="cuda")
+    P.cache = R.riftkv_cache(P.k, P.k)
+    bounds = torch.zeros(50, 1, 2, 64, device="cuda")
+    bounds[:, 0, :, 0] = 1.0
+    g = torch.Generator().manual_seed(1)
+    small = torch.randperm(50, generator=g).float().cuda() * 2.0 ** -40
+    bounds[:, 0, :, 1] = small[:, None]
+    q = torch.ones(1, 1, 64, device="cuda")
+    got = select(R, P, bounds, q, [800], 7, 0, 0)
+    want = small.argsort(descending=True)[:7].sort().values.int()
+    assert torch.equal(got[0, 0], want)
+
+
+def test_select_what_is_not_a_number(R):
+    """NaN in a page's bounds, or 0 times infinity: last, the lowest pages of them first; infinite scores in their order."""
+    P = plain_cache(R, 1, 64, 16, 40, 1, 40)
+    bounds = random_bounds(3, 40, 1, 64, torch.bfloat16)
+    bounds[5, 0, :, 3], bounds[7, 0, 1, 4], bounds[9, 0, 0, 5] = math.nan, math.inf, -math.inf
+    q = randn(4, 1, 2, 64)
+    q[0, :, 4] = 1.0
+    q[0, :, 5] = torch.tensor([1.0, 0.0])
+    for top in (4, 36, 38, 39):
+        got = select(R, P, bounds, q, [640], top, 1, 1).cpu()
+        assert torch.equal(got, selection(bounds, P.table, q, [40], 1, top, 1, 1)), top
+    assert 7 in select(R, P, bounds, q, [640], 4)[0, 0].tolist()
+    q[0, 0, 0] = math.nan                                    # every page's
+    got = select(R, P, bounds, q, [640], 4).cpu()
+    assert got[0, 0].tolist() == [0, 1, 2, 39]
+
+
+def test_select_bad_pages_and_lengths(R):
+    P = plain_cache(R, 2, 64, 16, 60, 3, 20)
+    bounds = random_bounds(3, 60, 2, 64, torch.bfloat16)
+    q = randn(4, 3, 4, 64)
+    lens = [320, 300, 77]
+    good = select(R, P, bounds, q, lens, 6)
+    for n in (-1, 321, 2 ** 31 - 1, -2 ** 31):
+        got = select(R, P, bounds, q, [320, n, 77], 6)
+        assert int(P.status) == 2 and bool((got[1] == -1).all()) and torch.equal(got[::2], good[::2])
+        P.status.zero_()
+    middle = [p for p in good[1, 0].tolist() if 0 < p < 18][0]
+    table = P.table.clone()
+    for bad in (-1, 60, 2 ** 31 - 1):
+        P.table = table.clone()
+        P.table[1, middle] = bad
+        got = select(R, P, bounds, q, lens, 6)
+        assert int(P.status) == 2 and middle not in got[1].flatten().tolist() and torch.equal(got[::2], good[::2])
+        P.status.zero_()
+        P.table = table.clone()
+        P.table[2, 1] = bad                                  # of a sequence whose pages are all taken
+        got = select(R, P, bounds, q, lens, 6)
+        assert int(P.status) == 2 and torch.equal(got, good)
+        P.status.zero_()
+
+
+def test_select_strides_streams_and_graphs(R):
+    P = plain_cache(R, 2, 128, 32, 500, 4, 125)
+    bounds = random_bounds(3, 500, 2, 128, torch.bfloat16)
+    wide = randn(4, 4, 10 * 128)
+    q = wide[:, 128:9 * 128].view(4, 8, 128)
+    lens = [4000, 3999, 33, 2000]
+    want = selection(bounds, P.table, q, held(lens, 32), 2, 16, 1, 1)
+    assert torch.equal(select(R, P, bounds, q, lens, 16).cpu(), want)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = select(R, P, bounds, q, lens, 16)
+    side.synchronize()
+    assert torch.equal(got.cpu(), want)
+    n, pages = i32(lens), torch.empty(4, 2, 16, dtype=torch.int32, device="cuda")
+    ws = torch.full((R.riftkv_select_pages_workspace_size(P.cache, 4, 125),), 255, dtype=torch.uint8, device="cuda")
+    P.status.zero_()
+    R.riftkv_select_pages(P.cache, bounds, q, P.table, n, pages, ws, P.status)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        R.riftkv_select_pages(P.cache, bounds, q, P.table, n, pages, ws, P.status)
+    for i in range(3):
+        wide.copy_(randn(40 + i, 4, 10 * 128))
+        n.copy_(i32([4000 - 500 * i, 33, 3999, 1]))
+        pages.zero_()
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(pages.cpu(), selection(bounds, P.table, q, held(n.tolist(), 32), 2, 16, 1, 1))
+    assert int(P.status) == 0
+
+
+# ----------------------------------------------------------------------------- together
+@pytest.mark.parametrize("store", ["bf16", "fp8"])
+def test_decode_over_a_sparse_context(R, store):
+    """As a decoder uses them, over a page's border: positions on three axes, the new row into its page, that page's bounds, the pages
+    that the token needs, its attention; after a prompt whose bounds are made at once."""
+    import numpy as np
+    n_kv, group, hd, page, top = 2, 4, 128, 16, 6
+    lens = [270, 31, 0, 16]
+    P = filled(R, store, n_kv, hd, page, [n + 8 for n in lens], seed=2)
+    freqs, _ = R.riftkv_rope_freqs(hd)
+    axes = (np.arange(hd // 2) % 3).astype(np.int32)
+    b = new_bounds(P)
+    R.riftkv_page_bounds(P.cache, b, P.table, i32(lens), P.status)
+    pages = torch.empty(4, n_kv, top, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(R.riftkv_select_pages_workspace_size(P.cache, 4, P.table.shape[1]), 256,
+                         R.riftkv_attention_pages_workspace_size(P.cache, 4, n_kv * group, top)), dtype=torch.uint8, device="cuda")
+    out = torch.empty(4, n_kv * group, hd, dtype=torch.bfloat16, device="cuda")
+    for step in range(4):
+        qkv = randn(50 + step, 4, (group + 2) * n_kv, hd)
+        q, k, v = qkv[:, :group * n_kv], qkv[:, group * n_kv:(group + 1) * n_kv], qkv[:, (group + 1) * n_kv:]
+        at = i32([n + step for n in lens])
+        places = torch.stack((at, at // 7, at % 7)).int().contiguous()
+        R.riftkv_rope_axes(q, k, places, freqs, axes)
+        R.riftkv_write(P.cache, k, v, P.table, at, P.status)
+        now = at + 1
+        R.riftkv_page_bounds(P.cache, b, P.table, now, P.status, begins=at)
+        R.riftkv_select_pages(P.cache, b, q, P.table, now, pages, ws, P.status)
+        R.riftkv_attention_pages(P.cache, q, P.table, now, pages, out, ws, P.status)
+        n = now.tolist()
+        for i in range(4):
+            for p in range(-(-n[i] // page)):
+                assert same(b[int(P.table[i, p])].cpu(), bounds_of(P, i, n[i], p).to(b.dtype)), (step, i, p)
+        assert torch.equal(pages.cpu(), selection(b, P.table, q, held(n, page), n_kv, top, 1, 1))
+        check(out, *attend_lists(P, q, n, pages.cpu()), q.dtype, f"step {step}")
+    assert int(P.status) == 0
