@@ -9,10 +9,10 @@ namespace rift {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBoundWgs = 2048;
 
-// The smaller and the larger of two numbers; NaN if either is.
+// The smaller of two numbers; NaN if either is.
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
-__device__ __forceinline__ float most(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 // Tokens of a sequence, -1 for a number out of range.
 __device__ __forceinline__ int length_of(int len, int max_pages, int shift) {
@@ -58,65 +58,138 @@ struct Values {
     }
 };
 
-// A workgroup takes a sequence; a wave a page of a key head at a time, 16 bytes of a row a lane.
+// The new pages of a sequence: from the one that holds its first new token.
+struct NewPages {
+    int first, n;
+};
+__device__ __forceinline__ NewPages new_pages(const BoundParams& p, int seq, int& len) {
+    len = length_of(p.lens[seq], p.max_pages, p.shift);
+    const int from = p.begins ? max(p.begins[seq], 0) : 0;
+    return from < len ? NewPages{from >> p.shift, pages_of(len, p.shift) - (from >> p.shift)} : NewPages{0, 0};
+}
+
+// Values joined over the rows of a load: of two lanes each keeps one half of them, the first time the smallest or
+// the negated largest, so that in the end all of a page's are spread over the wave.  at: the place of what this lane keeps.
+template <int D, int HALF, int FIRST, int N>
+__device__ __forceinline__ void join_rows(float (&x)[N], int lane, int& at) {
+    if constexpr (D < 64) {
+        const bool upper = lane & D;
+#pragma unroll
+        for (int e = 0; e < HALF; ++e) {
+            const float give = upper ? x[e] : x[HALF + e], keep = upper ? x[HALF + e] : x[e];
+            x[e] = least(keep, __shfl_xor(give, D));
+        }
+        if (upper) at += FIRST;
+        join_rows<2 * D, HALF / 2, HALF / 2>(x, lane, at);
+    }
+}
+
+// The pages of all sequences and heads, one after the other, are dealt out evenly to the workgroups, however uneven
+// the lengths; a wave takes a page of a head at a time, 16 bytes of a row a lane.
 template <riftkv_dtype DT, int HD>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 bounds_kernel(BoundParams p) {
     constexpr int B = DT == RIFTKV_F32 ? 4 : DT == RIFTKV_BF16 ? 2 : 1, N = 16 / B;
     constexpr int LANES = HD / N, ROWS = 64 / LANES;   // lanes of a row, rows of a load
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane % LANES, sub = lane / LANES;
-    for (int seq = blockIdx.x; seq < p.n_seq; seq += gridDim.x) {
-        const int len = length_of(p.lens[seq], p.max_pages, p.shift);
-        if (len < 0) {
-            if (threadIdx.x == 0) *p.status = RIFT_ERR_SHAPE;
+    constexpr int U = 4;                               // loads in flight
+    __shared__ long long sums[kThreads / 64], found_before;
+    __shared__ int found_seq;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane % LANES, sub = lane / LANES;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // A thread sums a run of sequences, the workgroup scans the sums, and whoever holds the first page looks it up.
+    const int per = (p.n_seq + kThreads - 1) / kThreads;
+    const int s0 = min(tid * per, p.n_seq), s1 = min(s0 + per, p.n_seq);
+    long long mine = 0;
+    int len;
+    for (int s = s0; s < s1; ++s) {
+        mine += new_pages(p, s, len).n;
+        if (len < 0 && blockIdx.x == 0) *p.status = RIFT_ERR_SHAPE;
+    }
+    long long incl = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const long long o = __shfl_up(incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 63) sums[wave] = incl;
+    __syncthreads();
+    long long before = incl - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) {
+        if (w < wave) before += sums[w];
+        total += sums[w];
+    }
+    total *= p.n_kv;
+    // items begin .. end - 1: page of a sequence, head
+    const long long q = total / gridDim.x, r = total - q * gridDim.x, b = blockIdx.x;
+    const long long begin = b * q + (b < r ? b : r), end = begin + q + (b < r);
+    if (begin == end) return;
+    if (mine > 0 && begin >= before * p.n_kv && begin < (before + mine) * p.n_kv) {
+        int s = s0;
+        for (;; ++s) {
+            const int n = new_pages(p, s, len).n;
+            if (begin < (before + n) * p.n_kv) break;
+            before += n;
+        }
+        found_seq = s;
+        found_before = before;
+    }
+    __syncthreads();
+    int seq = __builtin_amdgcn_readfirstlane(found_seq);
+    long long base = found_before * p.n_kv;      // items before this sequence's
+    NewPages pages = new_pages(p, seq, len);
+    for (long long i = begin + wave; i < end; i += kThreads / 64) {
+        while (i >= base + (long long)pages.n * p.n_kv) {
+            base += (long long)pages.n * p.n_kv;
+            pages = new_pages(p, ++seq, len);
+        }
+        const unsigned long long in = i - base;
+        const int nth = (int)((in >> 32) == 0 ? (unsigned)in / (unsigned)p.n_kv : in / p.n_kv);
+        const int head = __builtin_amdgcn_readfirstlane((int)(in - (unsigned long long)nth * p.n_kv));
+        const int place = __builtin_amdgcn_readfirstlane(pages.first + nth);
+        const int page = __builtin_amdgcn_readfirstlane(p.table[(size_t)seq * p.max_pages + place]);
+        if ((unsigned)page >= (unsigned)p.n_pages) {
+            if (lane == 0) *p.status = RIFT_ERR_SHAPE;
             continue;
         }
-        const int from = p.begins ? max(p.begins[seq], 0) : 0;
-        const int first = from >> p.shift, end = from < len ? pages_of(len, p.shift) : 0;
-        for (int64_t i = (int64_t)first * p.n_kv + wave; i < (int64_t)end * p.n_kv; i += kThreads / 64) {
-            const int place = (int)(i / p.n_kv), head = (int)(i - (int64_t)place * p.n_kv);
-            const int page = p.table[(size_t)seq * p.max_pages + place];
-            if ((unsigned)page >= (unsigned)p.n_pages) {
-                if (lane == 0) *p.status = RIFT_ERR_SHAPE;
-                continue;
-            }
-            const int n = (int)min((int64_t)len - ((int64_t)place << p.shift), (int64_t)1 << p.shift);
-            const size_t row = (((size_t)page * p.n_kv) + head) << p.shift;
-            float lo[N], hi[N];
+        const int n = (int)min((int64_t)len - ((int64_t)place << p.shift), (int64_t)1 << p.shift);
+        const size_t row = (((size_t)page * p.n_kv) + head) << p.shift;
+        float x[2 * N];                       // the smallest values, and the smallest of the negated ones
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                lo[e] = INFINITY;
-                hi[e] = -INFINITY;
+        for (int e = 0; e < 2 * N; ++e) x[e] = INFINITY;
+        for (int r0 = 0; r0 < n; r0 += U * ROWS) {
+            u32x4_t w[U];
+            uint32_t scale[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {     // past the last token: its row once more
+                const int at = min(r0 + u * ROWS + sub, n - 1);
+                w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p.k + (row + at) * (HD * B) + col * 16));
+                if constexpr (B == 1) scale[u] = p.ks[row + at];
             }
-            for (int r = sub; r < n; r += ROWS) {
-                const u32x4_t w = *reinterpret_cast<const u32x4_t*>(p.k + (row + r) * (HD * B) + col * 16);
-                const Values<DT> v(w, B == 1 ? scale_of(p.ks[row + r]) : 1.f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const Values<DT> v(w[u], B == 1 ? scale_of(scale[u]) : 1.f);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    lo[e] = least(lo[e], v.x[e]);
-                    hi[e] = most(hi[e], v.x[e]);
+                    x[e] = least(x[e], v.x[e]);
+                    x[N + e] = least(x[N + e], -v.x[e]);
                 }
             }
+        }
+        constexpr int M = 2 * N / ROWS;
+        int to_col = col * N;
+        join_rows<LANES, N, HD>(x, lane, to_col);
+        const size_t to = ((size_t)page * p.n_kv + head) * (2 * HD) + to_col;
+        const float sign = sub & 1 ? -1.f : 1.f;
+        if constexpr (B == 4) {
 #pragma unroll
-            for (int d = LANES; d < 64; d <<= 1)
+            for (int e = 0; e < M; ++e) static_cast<float*>(p.bounds)[to + e] = sign * x[e];
+        } else {
+            uint32_t w[M / 2];
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    lo[e] = least(lo[e], __shfl_xor(lo[e], d));
-                    hi[e] = most(hi[e], __shfl_xor(hi[e], d));
-                }
-            if (sub == 0) {
-                const size_t to = ((size_t)page * p.n_kv + head) * (2 * HD) + col * N;
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    if constexpr (B == 4) {
-                        static_cast<float*>(p.bounds)[to + e] = lo[e];
-                        static_cast<float*>(p.bounds)[to + HD + e] = hi[e];
-                    } else {
-                        static_cast<bf16_t*>(p.bounds)[to + e] = round_bf16(lo[e]);
-                        static_cast<bf16_t*>(p.bounds)[to + HD + e] = round_bf16(hi[e]);
-                    }
-                }
-            }
+            for (int e = 0; e < M / 2; ++e) w[e] = (uint32_t)round_bf16(sign * x[2 * e]) | (uint32_t)round_bf16(sign * x[2 * e + 1]) << 16;
+            if constexpr (M == 4) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.bounds) + to) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t*>(static_cast<bf16_t*>(p.bounds) + to) = w[0];
         }
     }
 }
@@ -270,7 +343,9 @@ hipError_t launch_kv_page_bounds(const riftkv_cache& c, void* bounds, const int*
                                  const int* lens, int* status, hipStream_t st) {
     const BoundParams p{static_cast<const unsigned char*>(c.k), c.k_scale, bounds, table, begins, lens, status, n_seq, max_pages,
                         c.n_pages, c.n_kv_heads, 31 - __builtin_clz(c.page_size)};
-    const unsigned wgs = (unsigned)(n_seq < 4096 ? n_seq : 4096);
+    // a wave an item as far as the table can hold them, and as many as are resident
+    const int64_t items = (int64_t)n_seq * max_pages * c.n_kv_heads, most = (items + 3) / 4;
+    const unsigned wgs = (unsigned)(most < 1 ? 1 : most > kBoundWgs ? kBoundWgs : most);
     auto run = [&](auto dt) {
         if (c.head_dim == 128) hipLaunchKernelGGL((bounds_kernel<dt.value, 128>), dim3(wgs), dim3(kThreads), 0, st, p);
         else hipLaunchKernelGGL((bounds_kernel<dt.value, 64>), dim3(wgs), dim3(kThreads), 0, st, p);
