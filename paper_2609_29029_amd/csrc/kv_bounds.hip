@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBoundWgs = 2048;
+constexpr int kScoreWgs = 8192;
 
 // The smaller of two numbers; NaN if either is.
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
@@ -203,138 +204,304 @@ struct SelectParams {
     int *lists, *status;
     unsigned long long* keys;   // [n_seq][n_kv][max_pages]
     int n_seq, max_pages, n_pages, n_kv, group, shift, first, last, top;
+    int item0, blocks;          // first (sequence, key head) of the launch; workgroups of each
 };
 
-constexpr int kQueries = 4;     // of a pass over the bounds
-constexpr int kSelectThreads = 1024;
-
-// Order of the scores as whole numbers; NaN before every number.
+// Order of the scores as whole numbers; NaN above every number.
+constexpr unsigned long long kNanKey = ~0ull;
 __device__ __forceinline__ unsigned long long key_of(double x) {
-    if (x != x) return 0;
     const long long b = __double_as_longlong(x + 0.0);   // -0 as 0
-    return b < 0 ? ~(unsigned long long)b : (unsigned long long)b | 0x8000000000000000ull;
+    return x != x ? kNanKey : b < 0 ? ~(unsigned long long)b : (unsigned long long)b | 0x8000000000000000ull;
 }
 
-template <typename T>
-__device__ __forceinline__ double load_f64(const void* p, size_t i) {
-    if constexpr (sizeof(T) == 2) return bf16_to_f32(static_cast<const bf16_t*>(p)[i]);
-    else return static_cast<const float*>(p)[i];
+// Eight values
+template <typename BT>
+struct EightOf {
+    u32x4_t w[sizeof(BT) / 2];
+    __device__ __forceinline__ void load(const void* p, size_t i) {
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(BT) / 2; ++j) w[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(static_cast<const BT*>(p) + i) + j);
+    }
+    __device__ __forceinline__ float at(int e) const {
+        if constexpr (sizeof(BT) == 2) return e & 1 ? bf16_hi(w[0][e / 2]) : bf16_lo(w[0][e / 2]);
+        else return __uint_as_float(w[e / 4][e % 4]);
+    }
+};
+
+template <int CTRL>
+__device__ __forceinline__ double dpp(double x) {
+    const long long b = __double_as_longlong(x);
+    const int lo = __builtin_amdgcn_mov_dpp((int)b, CTRL, 0xf, 0xf, false), hi = __builtin_amdgcn_mov_dpp((int)(b >> 32), CTRL, 0xf, 0xf, false);
+    return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
+}
+template <int CTRL>
+__device__ __forceinline__ unsigned long long dpp(unsigned long long x) {
+    const int lo = __builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, false), hi = __builtin_amdgcn_mov_dpp((int)(x >> 32), CTRL, 0xf, 0xf, false);
+    return ((unsigned long long)(unsigned)hi << 32) | (unsigned)lo;
+}
+// Lanes whose numbers differ in one bit only, or that mirror each other: partners of a step of a reduction.
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+
+// One step of a sum over lanes: of two partners each keeps one half of the values, the upper one (bit BIT of its number) the
+// second.
+template <int CTRL, int BIT, int HALF, int N>
+__device__ __forceinline__ void sum_step(double (&x)[N], int lane) {
+    const bool upper = lane & BIT;
+#pragma unroll
+    for (int e = 0; e < HALF; ++e) {
+        const double give = upper ? x[e] : x[HALF + e], keep = upper ? x[HALF + e] : x[e];
+        x[e] = keep + dpp<CTRL>(give);
+    }
 }
 
-// A workgroup takes a key head of a sequence: a page a thread, then the rank of the last page
-// to take, eight bits of it at a time, then the list.
+// Scores.  HD / 8 lanes hold a page's bounds, eight elements each, and the same elements of four queries at a time.  A query's
+// negative and positive values go into two float64 multiply-adds an element, so that no product needs a choice.  A wave
+// takes ITERS loads of pages, so that as many sums as a page has lanes are under way, and adds them up over those lanes by
+// halves: one sum is left to each.
+constexpr int kQueries = 4;
+
 template <typename T, typename BT, int HD>
-__global__ void __launch_bounds__(kSelectThreads)
-select_kernel(SelectParams p) {
-    __shared__ double qs[2][kQueries][HD];      // min(q, 0), max(q, 0)
-    __shared__ int counts[256];
-    __shared__ int waves[kSelectThreads / 64], waves_eq[kSelectThreads / 64];
-    __shared__ int found, above;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int seq = blockIdx.x / p.n_kv, kvh = blockIdx.x - seq * p.n_kv;
-    int* list = p.lists + (size_t)blockIdx.x * p.top;
-    const int given = p.lens[seq], len = length_of(given, p.max_pages, p.shift);
-    if (len < 0 && tid == 0) *p.status = RIFT_ERR_SHAPE;
-    const int held = len < 0 ? 0 : pages_of(len, p.shift);
+__global__ void __launch_bounds__(kThreads, 2)
+scores_kernel(SelectParams p) {
+    constexpr int G = HD / 8, PW = 64 / G;           // lanes of a page, pages of a load
+    constexpr int ITERS = G / kQueries, PAGES = PW * ITERS;
+    constexpr int WAVES = kThreads / 64;
+    const int lane = threadIdx.x & 63, d0 = 8 * (lane % G), sub = lane / G;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = blockIdx.x % p.blocks, item = blockIdx.x / p.blocks + p.item0;
+    const int seq = item / p.n_kv, kvh = item - seq * p.n_kv;
+    const int len = length_of(p.lens[seq], p.max_pages, p.shift);
+    const int held = pages_of(max(len, 0), p.shift);
+    if (held <= p.top) return;                       // all of them
+    const int begin = p.first, end = held - p.last;  // the pages to choose from
     const int* table = p.table + (size_t)seq * p.max_pages;
-    unsigned long long* keys = p.keys + (size_t)blockIdx.x * p.max_pages;
-    for (int i = min(held, p.top) + tid; i < p.top; i += kSelectThreads) list[i] = -1;
+    unsigned long long* keys = p.keys + (size_t)item * p.max_pages;
+    const T* q = static_cast<const T*>(p.q) + (size_t)seq * p.ld_q + (size_t)kvh * p.group * HD + d0;
+    EightOf<T> x[kQueries];
+    auto load_q = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kQueries; ++j) x[j].load(q, (size_t)min(j0 + j, p.group - 1) * HD);   // past the last: it once more
+    };
+    load_q(0);
+    for (int64_t p0 = begin + (int64_t)(block * WAVES + wave) * PAGES; p0 < end; p0 += (int64_t)p.blocks * WAVES * PAGES) {
+        EightOf<BT> lo[ITERS], hi[ITERS];
+        bool there[ITERS];
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {            // past the last: it once more
+            const int page = table[min((int)p0 + i * PW + sub, end - 1)];
+            there[i] = (unsigned)page < (unsigned)p.n_pages;
+            const size_t at = ((size_t)(there[i] ? page : 0) * p.n_kv + kvh) * (2 * HD) + d0;
+            lo[i].load(p.bounds, at);
+            hi[i].load(p.bounds, at + HD);
+        }
+        unsigned long long best = 0;
+        for (int j0 = 0; j0 < p.group; j0 += kQueries) {
+            if (p.group > kQueries) load_q(j0);
+            double s[G];                             // s[kQueries i + j]
+#pragma unroll
+            for (int i = 0; i < G; ++i) s[i] = 0.0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                double a[ITERS], b[ITERS];
+#pragma unroll
+                for (int i = 0; i < ITERS; ++i) {
+                    a[i] = lo[i].at(e);
+                    b[i] = hi[i].at(e);
+                }
+#pragma unroll
+                for (int j = 0; j < kQueries; ++j) {
+                    const float f = x[j].at(e);
+                    const double neg = f > 0.f ? 0.f : f, pos = f < 0.f ? 0.f : f;   // (NaN is in both)
+#pragma unroll
+                    for (int i = 0; i < ITERS; ++i) s[kQueries * i + j] = fma(pos, b[i], fma(neg, a[i], s[kQueries * i + j]));
+                }
+            }
+            // The partners of the first steps mirror each other: what lanes hold differs only by the bits above then.
+            // Bits 0 and 1 of a lane's number are the query in the end, the ones above them the load.
+            if constexpr (G == 16) sum_step<kMirror16, 8, 8>(s, lane);
+            sum_step<kMirror8, 4, 4>(s, lane);
+            sum_step<kXor2, 2, 2>(s, lane);
+            sum_step<kXor1, 1, 1>(s, lane);
+            best = max(best, key_of(s[0]));
+        }
+        best = max(best, dpp<kXor1>(best));
+        best = max(best, dpp<kXor2>(best));
+        const int load = (lane % G) >> 2;
+        bool good = false;
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) good |= load == i && there[i];
+        const int64_t place = p0 + load * PW + sub;
+        if ((lane & 3) == 0 && place < end) {
+            keys[place] = good && best != kNanKey ? best : 0;
+            if (!good) *p.status = RIFT_ERR_SHAPE;
+        }
+    }
+}
+
+// A workgroup takes a key head of a sequence, a thread a run of its pages: the key of the last page to take, eight bits of it at
+// a time from the first that differs between pages, then the list.
+constexpr int kPickThreads = 512, kHeldKeys = 8;   // keys that a thread keeps in registers
+
+__global__ void __launch_bounds__(kPickThreads)
+pick_kernel(SelectParams p) {
+    constexpr int WAVES = kPickThreads / 64;
+    __shared__ int counts[256];
+    __shared__ unsigned long long least_of[WAVES], most_of[WAVES];
+    __shared__ int sums[WAVES][2];
+    __shared__ int found, above, inside;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int item = blockIdx.x + p.item0, seq = item / p.n_kv;
+    int* list = p.lists + (size_t)item * p.top;
+    const int len = length_of(p.lens[seq], p.max_pages, p.shift);
+    if (len < 0 && tid == 0) *p.status = RIFT_ERR_SHAPE;
+    const int held = pages_of(max(len, 0), p.shift);
+    const int* table = p.table + (size_t)seq * p.max_pages;
+    auto check = [&](int place) {
+        if ((unsigned)table[place] >= (unsigned)p.n_pages) *p.status = RIFT_ERR_SHAPE;
+    };
     if (held <= p.top) {
-        for (int i = tid; i < held; i += kSelectThreads) {
-            list[i] = i;
-            if ((unsigned)table[i] >= (unsigned)p.n_pages) *p.status = RIFT_ERR_SHAPE;
+        for (int i = tid; i < p.top; i += kPickThreads) {
+            list[i] = i < held ? i : -1;
+            if (i < held) check(i);
         }
         return;
     }
-    // scores
-    for (int j0 = 0; j0 < p.group; j0 += kQueries) {
-        const int nq = min(kQueries, p.group - j0);
-        __syncthreads();
-        for (int i = tid; i < kQueries * HD; i += kSelectThreads) {
-            const int j = i / HD, d = i % HD;
-            const double x = j < nq ? load_f64<T>(p.q, (size_t)seq * p.ld_q + (size_t)(kvh * p.group + j0 + j) * HD + d) : 0.0;
-            qs[0][j][d] = x < 0.0 ? x : x == x ? 0.0 : x;
-            qs[1][j][d] = x > 0.0 ? x : x == x ? 0.0 : x;
-        }
-        __syncthreads();
-        for (int i = tid; i < held; i += kSelectThreads) {
-            const int page = table[i];
-            unsigned long long best = 0;
-            if ((unsigned)page < (unsigned)p.n_pages) {
-                const size_t at = ((size_t)page * p.n_kv + kvh) * (2 * HD);
-                double s[kQueries] = {};
-                for (int d = 0; d < HD; ++d) {
-                    const double lo = load_f64<BT>(p.bounds, at + d), hi = load_f64<BT>(p.bounds, at + HD + d);
+    for (int i = tid; i < p.first; i += kPickThreads) {
+        list[i] = i;
+        check(i);
+    }
+    for (int i = tid; i < p.last; i += kPickThreads) {
+        list[p.top - p.last + i] = held - p.last + i;
+        check(held - p.last + i);
+    }
+    int need = p.top - p.first - p.last;
+    if (need == 0) {                                                 // no score was worked out
+        for (int i = p.first + tid; i < held - p.last; i += kPickThreads) check(i);
+        return;
+    }
+    const int begin = p.first, n = held - p.first - p.last;          // the pages to choose from, more than need
+    const unsigned long long* keys = p.keys + (size_t)item * p.max_pages + begin;
+    const int per = (n + kPickThreads - 1) / kPickThreads;
+    const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
+    unsigned long long mine[kHeldKeys];
 #pragma unroll
-                    for (int j = 0; j < kQueries; ++j) s[j] = fma(qs[1][j][d], hi, fma(qs[0][j][d], lo, s[j]));
-                }
-                bool nan = j0 > 0 && keys[i] == 0;
-                if (j0 > 0) best = keys[i];
+    for (int i = 0; i < kHeldKeys; ++i) mine[i] = i0 + i < i1 ? keys[i0 + i] : 0;
+    // f(key) of every page of this thread
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        if (per <= kHeldKeys) {
 #pragma unroll
-                for (int j = 0; j < kQueries; ++j)
-                    if (j < nq) {
-                        const unsigned long long k = key_of(s[j]);
-                        nan |= k == 0;
-                        best = max(best, k);
-                    }
-                if (nan) best = 0;
-            } else {
-                *p.status = RIFT_ERR_SHAPE;
-            }
-            keys[i] = best;
+            for (int i = 0; i < kHeldKeys; ++i)
+                if (i0 + i < i1) f(mine[i], i0 + i);
+        } else {
+            for (int i = i0; i < i1; ++i) f(keys[i], i);
         }
+    };
+    unsigned long long lowest = ~0ull, highest = 0;
+    each([&](unsigned long long k, int) {
+        lowest = min(lowest, k);
+        highest = max(highest, k);
+    });
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+        lowest = min(lowest, (unsigned long long)__shfl_xor(lowest, d));
+        highest = max(highest, (unsigned long long)__shfl_xor(highest, d));
+    }
+    if (lane == 0) {
+        least_of[wave] = lowest;
+        most_of[wave] = highest;
     }
     __syncthreads();
-    // the key of the last page to take among those between the ends, and how many of its equals
-    const int begin = p.first, end = held - p.last;
-    int need = p.top - p.first - p.last;
-    unsigned long long prefix = 0;
-    for (int bit = 56; need > 0 && bit >= 0; bit -= 8) {
-        for (int i = tid; i < 256; i += kSelectThreads) counts[i] = 0;
-        __syncthreads();
-        for (int i = begin + tid; i < end; i += kSelectThreads) {
-            const unsigned long long k = keys[i];
-            if (bit == 56 || (k >> (bit + 8)) == (prefix >> (bit + 8))) atomicAdd(&counts[(k >> bit) & 255], 1);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            int sum = 0, b = 255;
-            while (sum + counts[b] < need) sum += counts[b--];
-            found = b;
-            above = sum;
-        }
-        __syncthreads();
-        prefix |= (unsigned long long)found << bit;
-        need -= above;
-        __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        lowest = min(lowest, least_of[w]);
+        highest = max(highest, most_of[w]);
     }
-    // the list, in the pages' order
-    int out = 0, equal = 0;
-    for (int i0 = 0; i0 < held; i0 += kSelectThreads) {
-        const int i = i0 + tid;
-        const bool between = i >= begin && i < end;
-        const unsigned long long k = between ? keys[i] : 0;
-        const bool eq = between && need > 0 && k == prefix;
-        const unsigned long long eqs = __ballot(eq);
-        if (lane == 0) waves_eq[wave] = __popcll(eqs);
-        __syncthreads();
-        int rank = equal + __popcll(eqs & ((1ull << lane) - 1));
-        for (int w = 0; w < kSelectThreads / 64; ++w) {
-            if (w < wave) rank += waves_eq[w];
-            equal += waves_eq[w];
+    // Keys of a bucket share the bits from `bit` on; those of higher buckets are all taken.
+    int bit = lowest == highest ? 0 : max(0, 64 - __clzll(lowest ^ highest) - 8);
+    unsigned long long bucket = highest >> bit;
+    int width = 256;
+    if (lowest == highest) need = min(need, n);
+    else
+        for (;;) {
+            const unsigned long long base = bucket & ~(unsigned long long)(width - 1);   // the first of the buckets looked at
+            if (tid < 256) counts[tid] = 0;
+            __syncthreads();
+            each([&](unsigned long long k, int) {
+                const unsigned long long in = (k >> bit) - base;
+                if (in < (unsigned long long)width) atomicAdd(&counts[in], 1);
+            });
+            __syncthreads();
+            if (wave == 0) {
+                // four buckets a lane, the highest first
+                int c[4], sum = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    c[i] = counts[255 - 4 * lane - i];
+                    sum += c[i];
+                }
+                int incl = sum;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int o = __shfl_up(incl, d);
+                    if (lane >= d) incl += o;
+                }
+                int before = incl - sum;
+                if (before < need && need <= incl) {
+                    int i = 0;
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        if (i == k && before + c[k] < need) {
+                            before += c[k];
+                            ++i;
+                        }
+                    found = 255 - 4 * lane - i;
+                    above = before;
+                    inside = i == 0 ? c[0] : i == 1 ? c[1] : i == 2 ? c[2] : c[3];
+                }
+            }
+            __syncthreads();
+            bucket = base + found;
+            need -= above;
+            if (bit == 0 || inside == need) break;
+            width = bit < 8 ? 1 << bit : 256;
+            const int step = bit < 8 ? bit : 8;
+            bit -= step;
+            bucket <<= step;
+            __syncthreads();
         }
-        const bool take = i < held && (!between || (need > 0 && (k > prefix || (eq && rank < need))));
-        const unsigned long long takes = __ballot(take);
-        if (lane == 0) waves[wave] = __popcll(takes);
-        __syncthreads();
-        int at = out + __popcll(takes & ((1ull << lane) - 1));
-        for (int w = 0; w < kSelectThreads / 64; ++w) {
-            if (w < wave) at += waves[w];
-            out += waves[w];
+    // places in the list: of the pages above, and of the bucket's first ones
+    int higher = 0, equal = 0;
+    each([&](unsigned long long k, int) {
+        higher += (k >> bit) > bucket;
+        equal += (k >> bit) == bucket;
+    });
+    int hi_incl = higher, eq_incl = equal;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int a = __shfl_up(hi_incl, d), b = __shfl_up(eq_incl, d);
+        if (lane >= d) {
+            hi_incl += a;
+            eq_incl += b;
         }
-        if (take) list[at] = i;
-        __syncthreads();
     }
+    if (lane == 63) {
+        sums[wave][0] = hi_incl;
+        sums[wave][1] = eq_incl;
+    }
+    __syncthreads();
+    int hi = hi_incl - higher, eq = eq_incl - equal;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+        if (w < wave) {
+            hi += sums[w][0];
+            eq += sums[w][1];
+        }
+    each([&](unsigned long long k, int i) {
+        const unsigned long long b = k >> bit;
+        if (b > bucket || (b == bucket && eq < need)) list[p.first + hi + min(eq, need)] = begin + i;
+        hi += b > bucket;
+        eq += b == bucket;
+    });
 }
 
 }  // namespace
@@ -366,19 +533,36 @@ size_t kv_select_workspace(const riftkv_cache& c, int64_t n_seq, int64_t max_pag
 }
 
 hipError_t launch_kv_select_pages(const riftkv_cache& c, const KvSelect& s, hipStream_t st) {
-    const SelectParams p{s.q, s.bounds, s.ld_q, s.table, s.lens, s.lists, s.status, static_cast<unsigned long long*>(s.workspace),
-                         s.n_seq, s.max_pages, c.n_pages, c.n_kv_heads, s.n_heads / c.n_kv_heads, 31 - __builtin_clz(c.page_size),
-                         s.first, s.last, s.top};
-    auto run = [&](auto t, auto bt) {
+    SelectParams p{s.q, s.bounds, s.ld_q, s.table, s.lens, s.lists, s.status, static_cast<unsigned long long*>(s.workspace),
+                   s.n_seq, s.max_pages, c.n_pages, c.n_kv_heads, s.n_heads / c.n_kv_heads, 31 - __builtin_clz(c.page_size),
+                   s.first, s.last, s.top, 0, 1};
+    const int64_t items = (int64_t)s.n_seq * c.n_kv_heads;
+    // Workgroups of 64 pages a (sequence, key head), as many as the table can need or as keep all CUs busy.
+    const int64_t most = (s.max_pages + 63) / 64, enough = (kScoreWgs + items - 1) / items;
+    p.blocks = (int)(most < 1 ? 1 : most < enough ? most : enough);
+    auto in_pieces = [&](int64_t wgs_of_item, int threads, auto launch) {
+        const int64_t piece = ((1ll << 32) - 1) / threads / wgs_of_item;
+        for (int64_t i = 0; i < items; i += piece) {
+            p.item0 = (int)i;
+            launch((unsigned)((items - i < piece ? items - i : piece) * wgs_of_item));
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    };
+    auto scores = [&](auto kernel) {
+        return in_pieces(p.blocks, kThreads, [&](unsigned wgs) { hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kThreads), 0, st, p); });
+    };
+    auto types = [&](auto t, auto bt) {
         using T = decltype(t);
         using BT = decltype(bt);
-        const dim3 grid((unsigned)s.n_seq * (unsigned)c.n_kv_heads);
-        if (c.head_dim == 128) hipLaunchKernelGGL((select_kernel<T, BT, 128>), grid, dim3(kSelectThreads), 0, st, p);
-        else hipLaunchKernelGGL((select_kernel<T, BT, 64>), grid, dim3(kSelectThreads), 0, st, p);
-        return hipGetLastError();
+        return c.head_dim == 128 ? scores(scores_kernel<T, BT, 128>) : scores(scores_kernel<T, BT, 64>);
     };
-    if (c.dt == RIFTKV_F32) return run(float{}, float{});
-    return s.bf16 ? run(bf16_t{}, bf16_t{}) : run(float{}, bf16_t{});
+    if (s.max_pages > s.top && s.top > s.first + s.last) {     // something to choose
+        const hipError_t e = c.dt == RIFTKV_F32 ? types(float{}, float{}) : s.bf16 ? types(bf16_t{}, bf16_t{}) : types(float{}, bf16_t{});
+        if (e != hipSuccess) return e;
+    }
+    return in_pieces(1, kPickThreads, [&](unsigned wgs) { hipLaunchKernelGGL(pick_kernel, dim3(wgs), dim3(kPickThreads), 0, st, p); });
 }
 
 }  // namespace rift
