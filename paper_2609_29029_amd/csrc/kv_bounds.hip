@@ -10,7 +10,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBoundWgs = 2048;
-constexpr int kScoreWgs = 8192;
+constexpr int kScoreWgs = 4096;
 
 // The smaller of two numbers; NaN if either is.
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
@@ -204,7 +204,7 @@ struct SelectParams {
     int *lists, *status;
     unsigned long long* keys;   // [n_seq][n_kv][max_pages]
     int n_seq, max_pages, n_pages, n_kv, group, shift, first, last, top;
-    int item0, blocks;          // first (sequence, key head) of the launch; workgroups of each
+    int seq0, blocks;           // first sequence of the launch; workgroups of each of its key heads
 };
 
 // Order of the scores as whole numbers; NaN above every number.
@@ -268,8 +268,9 @@ scores_kernel(SelectParams p) {
     constexpr int WAVES = kThreads / 64;
     const int lane = threadIdx.x & 63, d0 = 8 * (lane % G), sub = lane / G;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block = blockIdx.x % p.blocks, item = blockIdx.x / p.blocks + p.item0;
-    const int seq = item / p.n_kv, kvh = item - seq * p.n_kv;
+    // a block of pages after the other, each with all key heads: what lies together in memory is read together
+    const int of = blockIdx.x / p.n_kv, kvh = blockIdx.x - of * p.n_kv;
+    const int seq = of / p.blocks + p.seq0, block = of % p.blocks, item = seq * p.n_kv + kvh;
     const int len = length_of(p.lens[seq], p.max_pages, p.shift);
     const int held = pages_of(max(len, 0), p.shift);
     if (held <= p.top) return;                       // all of them
@@ -277,20 +278,31 @@ scores_kernel(SelectParams p) {
     const int* table = p.table + (size_t)seq * p.max_pages;
     unsigned long long* keys = p.keys + (size_t)item * p.max_pages;
     const T* q = static_cast<const T*>(p.q) + (size_t)seq * p.ld_q + (size_t)kvh * p.group * HD + d0;
-    EightOf<T> x[kQueries];
+    float neg[kQueries][8], pos[kQueries][8];
     auto load_q = [&](int j0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kQueries; ++j) x[j].load(q, (size_t)min(j0 + j, p.group - 1) * HD);   // past the last: it once more
+        for (int j = 0; j < kQueries; ++j) {         // past the last: it once more
+            EightOf<T> x;
+            x.load(q, (size_t)min(j0 + j, p.group - 1) * HD);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float f = x.at(e);
+                neg[j][e] = f > 0.f ? 0.f : f;       // (NaN is in both)
+                pos[j][e] = f < 0.f ? 0.f : f;
+            }
+        }
     };
     load_q(0);
-    for (int64_t p0 = begin + (int64_t)(block * WAVES + wave) * PAGES; p0 < end; p0 += (int64_t)p.blocks * WAVES * PAGES) {
+    const int64_t step = (int64_t)p.blocks * WAVES * PAGES;
+    for (int64_t p0 = begin + (int64_t)(block * WAVES + wave) * PAGES; p0 < end; p0 += step) {
         EightOf<BT> lo[ITERS], hi[ITERS];
-        bool there[ITERS];
+        unsigned there = 0;                          // loads whose page is there
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {            // past the last: it once more
             const int page = table[min((int)p0 + i * PW + sub, end - 1)];
-            there[i] = (unsigned)page < (unsigned)p.n_pages;
-            const size_t at = ((size_t)(there[i] ? page : 0) * p.n_kv + kvh) * (2 * HD) + d0;
+            const bool is = (unsigned)page < (unsigned)p.n_pages;
+            there |= (unsigned)is << i;
+            const size_t at = ((size_t)(is ? page : 0) * p.n_kv + kvh) * (2 * HD) + d0;
             lo[i].load(p.bounds, at);
             hi[i].load(p.bounds, at + HD);
         }
@@ -310,10 +322,9 @@ scores_kernel(SelectParams p) {
                 }
 #pragma unroll
                 for (int j = 0; j < kQueries; ++j) {
-                    const float f = x[j].at(e);
-                    const double neg = f > 0.f ? 0.f : f, pos = f < 0.f ? 0.f : f;   // (NaN is in both)
+                    const double x = neg[j][e], y = pos[j][e];
 #pragma unroll
-                    for (int i = 0; i < ITERS; ++i) s[kQueries * i + j] = fma(pos, b[i], fma(neg, a[i], s[kQueries * i + j]));
+                    for (int i = 0; i < ITERS; ++i) s[kQueries * i + j] = fma(y, b[i], fma(x, a[i], s[kQueries * i + j]));
                 }
             }
             // The partners of the first steps mirror each other: what lanes hold differs only by the bits above then.
@@ -326,11 +337,9 @@ scores_kernel(SelectParams p) {
         }
         best = max(best, dpp<kXor1>(best));
         best = max(best, dpp<kXor2>(best));
-        const int load = (lane % G) >> 2;
-        bool good = false;
-#pragma unroll
-        for (int i = 0; i < ITERS; ++i) good |= load == i && there[i];
-        const int64_t place = p0 + load * PW + sub;
+        const int nth = (lane % G) >> 2;
+        const bool good = there >> nth & 1;
+        const int64_t place = p0 + nth * PW + sub;
         if ((lane & 3) == 0 && place < end) {
             keys[place] = good && best != kNanKey ? best : 0;
             if (!good) *p.status = RIFT_ERR_SHAPE;
@@ -350,7 +359,7 @@ pick_kernel(SelectParams p) {
     __shared__ int sums[WAVES][2];
     __shared__ int found, above, inside;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int item = blockIdx.x + p.item0, seq = item / p.n_kv;
+    const int item = blockIdx.x + p.seq0 * p.n_kv, seq = item / p.n_kv;
     int* list = p.lists + (size_t)item * p.top;
     const int len = length_of(p.lens[seq], p.max_pages, p.shift);
     if (len < 0 && tid == 0) *p.status = RIFT_ERR_SHAPE;
@@ -540,11 +549,12 @@ hipError_t launch_kv_select_pages(const riftkv_cache& c, const KvSelect& s, hipS
     // Workgroups of 64 pages a (sequence, key head), as many as the table can need or as keep all CUs busy.
     const int64_t most = (s.max_pages + 63) / 64, enough = (kScoreWgs + items - 1) / items;
     p.blocks = (int)(most < 1 ? 1 : most < enough ? most : enough);
-    auto in_pieces = [&](int64_t wgs_of_item, int threads, auto launch) {
-        const int64_t piece = ((1ll << 32) - 1) / threads / wgs_of_item;
-        for (int64_t i = 0; i < items; i += piece) {
-            p.item0 = (int)i;
-            launch((unsigned)((items - i < piece ? items - i : piece) * wgs_of_item));
+    // launch(workgroups), as often as the sequences need
+    auto in_pieces = [&](int64_t wgs_of_head, int threads, auto launch) {
+        const int64_t of_seq = wgs_of_head * c.n_kv_heads, most = ((1ll << 32) - 1) / threads / of_seq;
+        for (int64_t i = 0; i < s.n_seq; i += most) {
+            p.seq0 = (int)i;
+            launch((unsigned)((s.n_seq - i < most ? s.n_seq - i : most) * of_seq));
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
