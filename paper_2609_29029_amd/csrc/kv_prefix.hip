@@ -34,12 +34,29 @@ typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
 // Lane i of each 16-lane group g gets, in component j, the 16-bit element at (address of lane 16 g + 4 j + i / 4) + i % 4.
 __device__ __forceinline__ v4s_t lds_read_tr16(const void* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(p)); }
 
+// Two bf16 terms that add up to a and b but for 2^-17 of them: the first is cut off, what is left rounded.
+__device__ __forceinline__ void round_split(float a, float b, uint32_t (&w)[2]) {
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    w[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    a -= __uint_as_float(x & 0xFFFF0000u);
+    b -= __uint_as_float(y & 0xFFFF0000u);
+    w[1] = (uint32_t)round_bf16(a) | (uint32_t)round_bf16(b) << 16;
+}
+
+// LDS DMA of 16 bytes a lane: from a wave-uniform base and a lane's offset to lds + 16 lane.
+__device__ __forceinline__ void dma16(const unsigned char* base, uint32_t offset, uint32_t lds) {
+    const uint64_t b = (uint64_t)(uintptr_t)base;
+    const uint64_t ub = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b) |
+                        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32);
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(ub) : "memory", "m0");
+}
+
 template <typename T, riftkv_dtype DT, int HD>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1)
 prefix_kernel(PrefixParams p) {
     constexpr int B = DT == RIFTKV_BF16 ? 2 : 1;
     constexpr bool SCALED = B == 1;
-    constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = 3;
+    constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
     constexpr int CHUNKS = HD * B / 16;           // 16-byte chunks of a row in the pages
     constexpr int LOADS = kTokens * CHUNKS / 256; // of a thread, of keys or values
     constexpr int STEP = 256 / CHUNKS;            // rows between them
@@ -55,60 +72,72 @@ prefix_kernel(PrefixParams p) {
     const int tiles = (p.len + kTokens - 1) / kTokens;
     const int t0 = (int)((int64_t)tiles * part / p.parts), t1 = (int)((int64_t)tiles * (part + 1) / p.parts);
     const bool rows_here = r0 < p.rows;
-
-    // this lane's query, 16 kk + 8 h .. of it
-    bf16x8_t qf[NQ][NK];
-    {
-        const int r = min(r0 + n, p.rows - 1), seq = r / p.group;
-        const T* q = static_cast<const T*>(p.q) + (size_t)seq * p.ld_q + (size_t)(kvh * p.group + r - seq * p.group) * HD + 8 * h;
-#pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-            if constexpr (NQ == 1) qf[0][kk] = *reinterpret_cast<const bf16x8_t*>(q + 16 * kk);
-            else {
-                u32x4_t x[NQ];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t w[NQ];
-                    split_bf16<NQ>(q[16 * kk + 2 * e], q[16 * kk + 2 * e + 1], w);
-#pragma unroll
-                    for (int i = 0; i < NQ; ++i) x[i][e] = w[i];
-                }
-#pragma unroll
-                for (int i = 0; i < NQ; ++i) qf[i][kk] = __builtin_bit_cast(bf16x8_t, x[i]);
-            }
-        }
-    }
-    f32x16_t o[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    const int in_mask = (1 << p.shift) - 1;
     bool bad = false;
 
-    // A thread's share of a tile: chunk `chunk` of rows row, row + STEP, ..  All lanes of a wave are in rows of one page.
+    // The pages' numbers, 64 at a time, one a lane.
+    int first = (t0 * kTokens) >> p.shift, mine = 0;
+    auto look = [&]() __attribute__((always_inline)) {
+        const int e = first + lane;
+        if (t0 < t1 && e <= (p.len - 1) >> p.shift) {
+            mine = p.table[e];
+            bad |= (unsigned)mine >= (unsigned)p.n_pages;
+            if (bad) mine = 0;
+        } else mine = 0;
+    };
+    // First row of 16 tokens among the pages' rows; token: the same for the whole wave, before the end.
+    auto row_at = [&](int token) __attribute__((always_inline)) {
+        const int page = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane((token >> p.shift) - first));
+        return ((((size_t)page * p.n_kv) + kvh) << p.shift) + (token & in_mask);
+    };
+    auto reach = [&](int t) __attribute__((always_inline)) {   // the pages of tile t
+        if (((t * kTokens + kTokens - 16) >> p.shift) - first >= 64) {
+            first = (t * kTokens) >> p.shift;
+            look();
+        }
+    };
+    look();
+
+    // A bf16 tile comes by LDS DMA: waves 0 and 1 move 32 rows of keys each, waves 2 and 3 of values, four rows an instruction;
+    // lane i the chunk that belongs at place i mod 16 of row i / 16.
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+    auto dma = [&](int t) __attribute__((always_inline)) {
+        reach(t);
+        const bool v = wave >= 2;
+        const unsigned char* pages = v ? p.pages.v : p.pages.k;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int r = 32 * (wave & 1) + 16 * x;            // the first of 16 rows
+            if (t * kTokens + r >= p.len) continue;
+            const unsigned char* base = pages + row_at(t * kTokens + r) * (HD * B);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 4 * i + (lane >> 4);
+                const int c = (lane & 15) ^ (v ? 4 * (row & 3) : row);
+                if (HD == 128 || c < CHUNKS)
+                    dma16(base, (uint32_t)(row * (HD * B) + c * 16), lds0 + (t & 1) * kStageBytes + (v ? kTileBytes : 0) + (r + 4 * i) * kRowBytes);
+            }
+        }
+    };
+    // An 8-bit tile goes through registers, where it is widened: chunk `chunk` of rows row, row + STEP, .. a thread.  All lanes
+    // of a wave are in 16 rows of one page.
     const int row = tid / CHUNKS, chunk = tid % CHUNKS;
-    u32x4_t kr[LOADS], vr[LOADS];
+    u32x4_t kr[SCALED ? LOADS : 1], vr[SCALED ? LOADS : 1];
     uint32_t sr = 0;
     auto load = [&](int t) __attribute__((always_inline)) {
+        reach(t);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int token = min(t * kTokens + row + i * STEP, p.len - 1);
-            const int page = __builtin_amdgcn_readfirstlane(p.table[token >> p.shift]);
-            const bool there = (unsigned)page < (unsigned)p.n_pages;
-            bad |= !there;
-            const size_t at = (((((size_t)(there ? page : 0) * p.n_kv) + kvh) << p.shift) + (token & ((1 << p.shift) - 1))) * (HD * B) + 16 * chunk;
+            const int r = t * kTokens + __builtin_amdgcn_readfirstlane((row + i * STEP) & ~15);
+            const size_t at = ((r < p.len ? row_at(r) : 0) + ((row + i * STEP) & 15)) * (HD * B) + 16 * chunk;   // (past the end: any)
             kr[i] = *reinterpret_cast<const u32x4_t*>(p.pages.k + at);
             vr[i] = *reinterpret_cast<const u32x4_t*>(p.pages.v + at);
         }
-        if constexpr (SCALED) {
-            if (tid < 2 * kTokens) {
-                const int token = min(t * kTokens + (tid & (kTokens - 1)), p.len - 1);
-                const int page = p.table[token >> p.shift];
-                const size_t at = ((((size_t)((unsigned)page < (unsigned)p.n_pages ? page : 0) * p.n_kv) + kvh) << p.shift) + (token & ((1 << p.shift) - 1));
-                sr = (tid < kTokens ? p.pages.ks : p.pages.vs)[at];
-            }
-        }
+        // the scale of a key (waves 0 and 1) or value of 32 tokens a wave, the upper lanes idle
+        const int r = t * kTokens + 32 * (wave & 1);
+        const size_t a = r < p.len ? row_at(r) : 0, b = r + 16 < p.len ? row_at(r + 16) : 0;
+        sr = 0;
+        if (lane < 32 && r + lane < p.len) sr = (wave < 2 ? p.pages.ks : p.pages.vs)[(lane & 16 ? b : a) + (lane & 15)];
     };
     auto store = [&](int t) __attribute__((always_inline)) {
         unsigned char* K = lds + (t & 1) * kStageBytes;
@@ -117,39 +146,90 @@ prefix_kernel(PrefixParams p) {
         for (int i = 0; i < LOADS; ++i) {
             const int r = row + i * STEP;
             const u32x4_t v = t * kTokens + r < p.len ? vr[i] : u32x4_t{0, 0, 0, 0};   // behind the last token: no part of a sum
-            if constexpr (!SCALED) {
-                *reinterpret_cast<u32x4_t*>(K + r * kRowBytes + ((chunk ^ (r & 15)) << 4)) = kr[i];
-                *reinterpret_cast<u32x4_t*>(V + r * kRowBytes + ((chunk ^ (4 * (r & 3))) << 4)) = v;
-            } else {
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int c = 2 * chunk + y;
-                    *reinterpret_cast<u32x4_t*>(K + r * kRowBytes + ((c ^ (r & 15)) << 4)) =
-                        u32x4_t{widen<DT, false>(kr[i][2 * y]), widen<DT, true>(kr[i][2 * y]), widen<DT, false>(kr[i][2 * y + 1]), widen<DT, true>(kr[i][2 * y + 1])};
-                    *reinterpret_cast<u32x4_t*>(V + r * kRowBytes + ((c ^ (4 * (r & 3))) << 4)) =
-                        u32x4_t{widen<DT, false>(v[2 * y]), widen<DT, true>(v[2 * y]), widen<DT, false>(v[2 * y + 1]), widen<DT, true>(v[2 * y + 1])};
-                }
+            for (int y = 0; y < 2; ++y) {
+                const int c = 2 * chunk + y;
+                *reinterpret_cast<u32x4_t*>(K + r * kRowBytes + ((c ^ (r & 15)) << 4)) =
+                    u32x4_t{widen<DT, false>(kr[i][2 * y]), widen<DT, true>(kr[i][2 * y]), widen<DT, false>(kr[i][2 * y + 1]), widen<DT, true>(kr[i][2 * y + 1])};
+                *reinterpret_cast<u32x4_t*>(V + r * kRowBytes + ((c ^ (4 * (r & 3))) << 4)) =
+                    u32x4_t{widen<DT, false>(v[2 * y]), widen<DT, true>(v[2 * y]), widen<DT, false>(v[2 * y + 1]), widen<DT, true>(v[2 * y + 1])};
             }
         }
-        if constexpr (SCALED)
-            if (tid < 2 * kTokens) scales[(t & 1) * 2 * kTokens + tid] = scale_of(sr);
+        if (lane < 32) scales[(t & 1) * 2 * kTokens + 32 * wave + lane] = scale_of(sr);
     };
+
+    if (t0 < t1) {
+        if constexpr (SCALED) load(t0);
+        else dma(t0);
+    }
+    // this lane's query, 16 kk + 8 h .. of it; negated for a negative scale, so that the largest score is that of the largest product
+    bf16x8_t qf[NQ][NK];
+    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+    const float scale = fabsf(p.scale_log2);
+    {
+        const int r = min(r0 + n, p.rows - 1), seq = r / p.group;
+        const T* q = static_cast<const T*>(p.q) + (size_t)seq * p.ld_q + (size_t)(kvh * p.group + r - seq * p.group) * HD + 8 * h;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            u32x4_t x[NQ];
+            if constexpr (NQ == 1) x[0] = *reinterpret_cast<const u32x4_t*>(q + 16 * kk);
+            else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t w[NQ];
+                    split_bf16<NQ>(q[16 * kk + 2 * e], q[16 * kk + 2 * e + 1], w);
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) x[i][e] = w[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[i][e] ^= flip;
+                qf[i][kk] = __builtin_bit_cast(bf16x8_t, x[i]);
+            }
+        }
+        // (waited for here: the compiler does not count the DMA among what is under way)
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) asm volatile("" : "+v"(qf[i][kk]));
+    }
+    f32x16_t o[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
 
     const int tg = lane >> 4, tj = (lane >> 2) & 3, tu = lane & 3;
     const int v_off = (4 * (tg >> 1) + tj) * kRowBytes + (2 * (tg & 1) + (tu >> 1)) * 16 + 8 * (tu & 1);
-    if (t0 < t1) {
-        load(t0);
-        store(t0);
-        if (t0 + 1 < t1) load(t0 + 1);
+    if constexpr (SCALED) {
+        if (t0 < t1) {
+            store(t0);
+            if (t0 + 1 < t1) load(t0 + 1);
+        }
+        __syncthreads();
     }
-    __syncthreads();
     for (int t = t0; t < t1; ++t) {
-        const unsigned char* K = lds + (t & 1) * kStageBytes;
-        const unsigned char* V = K + kTileBytes;
+        unsigned char* K = lds + (t & 1) * kStageBytes;
+        unsigned char* V = K + kTileBytes;
         const float* ks = scales + (t & 1) * 2 * kTokens;
-        if (t + 1 < t1) {       // into the stage that every wave left at the last barrier
-            store(t + 1);
-            if (t + 2 < t1) load(t + 2);
+        const int there = p.len - t * kTokens;
+        if constexpr (SCALED) {
+            if (t + 1 < t1) {       // into the stage that every wave left at the last barrier
+                store(t + 1);
+                if (t + 2 < t1) load(t + 2);
+            }
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();        // tile t is there, and every wave is done with the one before
+            if (there < kTokens) {  // values behind the last token: no part of a sum, whatever they are
+                for (int i = tid; i < (kTokens - there) * 16; i += 256)
+                    *reinterpret_cast<u32x4_t*>(V + (there + i / 16) * kRowBytes + (i % 16) * 16) = u32x4_t{0, 0, 0, 0};
+                __syncthreads();
+            }
+            if (t + 1 < t1) dma(t + 1);
         }
         if (rows_here) {
             f32x16_t s[2];
@@ -176,11 +256,6 @@ prefix_kernel(PrefixParams p) {
                         for (int e = 0; e < 4; ++e) s[kb][i + e] *= f[e];
                     }
             }
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[kb][i] *= p.scale_log2;
-            const int there = p.len - t * kTokens;
             if (there < kTokens) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
@@ -193,7 +268,7 @@ prefix_kernel(PrefixParams p) {
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb][i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
             // The reference moves only when a score passes it by more than kLazy: weights stay below 2^kLazy, and the sums
             // are rescaled in few tiles.
             const float mn = mx > m + kLazy ? mx : m;
@@ -206,17 +281,33 @@ prefix_kernel(PrefixParams p) {
                     for (int i = 0; i < 16; ++i) o[c][i] *= f;
                 m = mn;
             }
-            const float ref = ref_of(m);
+            const float neg_ref = -ref_of(m);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int ks_ = 0; ks_ < 2; ++ks_) {
+                    // the values first: they arrive while the weights are worked out
+                    const unsigned char* vb = V + (kb * 32 + 16 * ks_) * kRowBytes + v_off;
+                    u32x4_t vv[NT];
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) {
+                        const int at = (c ^ tj) << 6;   // four chunks on, moved by the row's swizzle
+                        const v4s_t lo = lds_read_tr16(vb + at), hi = lds_read_tr16(vb + at + 8 * kRowBytes);
+                        vv[c] = u32x4_t{__builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 0, 1)),
+                                        __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 2, 3)),
+                                        __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 0, 1)),
+                                        __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 2, 3))};
+                    }
                     float w[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        w[j] = __builtin_amdgcn_exp2f(s[kb][8 * ks_ + j] - ref);
-                        l += w[j];
+                    for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(fmaf(s[kb][8 * ks_ + j], scale, neg_ref));
+                    if (there < kTokens) {     // (-infinity times a scale of 0)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (32 * kb + 16 * ks_ + 8 * (j >> 2) + 4 * h + (j & 3) >= there) w[j] = 0.f;
                     }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) l += w[j];
                     if constexpr (SCALED) {
 #pragma unroll
                         for (int j = 0; j < 8; j += 4) {
@@ -224,36 +315,24 @@ prefix_kernel(PrefixParams p) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) w[j + e] *= f[e];
                         }
-                        if (there < kTokens) {   // (a last row's scale may be infinite)
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (32 * kb + 16 * ks_ + 8 * (j >> 2) + 4 * h + (j & 3) >= there) w[j] = 0.f;
-                        }
                     }
                     u32x4_t pf[NP];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t x[NP];
-                        split_bf16<NP>(w[2 * j], w[2 * j + 1], x);
+                        if constexpr (NP == 2) round_split(w[2 * j], w[2 * j + 1], x);
+                        else split_bf16<NP>(w[2 * j], w[2 * j + 1], x);
 #pragma unroll
                         for (int i = 0; i < NP; ++i) pf[i][j] = x[i];
                     }
-                    const unsigned char* vb = V + (kb * 32 + 16 * ks_) * kRowBytes + v_off;
 #pragma unroll
-                    for (int c = 0; c < NT; ++c) {
-                        const int at = (c ^ tj) << 6;   // four chunks on, moved by the row's swizzle
-                        const v4s_t lo = lds_read_tr16(vb + at), hi = lds_read_tr16(vb + at + 8 * kRowBytes);
-                        const u32x4_t vv = {__builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 0, 1)),
-                                            __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 2, 3)),
-                                            __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 0, 1)),
-                                            __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 2, 3))};
+                    for (int i = 0; i < NP; ++i)
 #pragma unroll
-                        for (int i = 0; i < NP; ++i)
-                            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), __builtin_bit_cast(bf16x8_t, pf[i]), o[c], 0, 0, 0);
-                    }
+                        for (int c = 0; c < NT; ++c)
+                            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv[c]), __builtin_bit_cast(bf16x8_t, pf[i]), o[c], 0, 0, 0);
                 }
         }
-        __syncthreads();
+        if constexpr (SCALED) __syncthreads();
     }
     l += __shfl_xor(l, 32);
     if (t0 == t1) l = kNoTokens;
