@@ -25,7 +25,7 @@ constexpr int kRows = 128, kTokens = 64;      // of a workgroup, of a tile
 constexpr int kRowBytes = 256;
 constexpr int kTileBytes = kTokens * kRowBytes;
 constexpr int kStageBytes = 2 * kTileBytes;   // keys, then values
-constexpr int kScaleFloats = 2 * 2 * kTokens; // of keys and values, two stages
+constexpr int kScaleFloats = 4 * 2 * kTokens; // of keys and values, four tiles
 constexpr float kLazy = 8.f;                  // log2 units by which a score may pass the reference
 
 typedef short v4s_t __attribute__((ext_vector_type(4)));
@@ -40,7 +40,9 @@ __device__ __forceinline__ void round_split(float a, float b, uint32_t (&w)[2]) 
     w[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
     a -= __uint_as_float(x & 0xFFFF0000u);
     b -= __uint_as_float(y & 0xFFFF0000u);
-    w[1] = (uint32_t)round_bf16(a) | (uint32_t)round_bf16(b) << 16;
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
 }
 
 // LDS DMA of 16 bytes a lane: from a wave-uniform base and a lane's offset to lds + 16 lane.
@@ -79,93 +81,97 @@ prefix_kernel(PrefixParams p) {
     int first = (t0 * kTokens) >> p.shift, mine = 0;
     auto look = [&]() __attribute__((always_inline)) {
         const int e = first + lane;
-        if (t0 < t1 && e <= (p.len - 1) >> p.shift) {
-            mine = p.table[e];
-            bad |= (unsigned)mine >= (unsigned)p.n_pages;
-            if (bad) mine = 0;
-        } else mine = 0;
+        mine = t0 < t1 && e <= (p.len - 1) >> p.shift ? p.table[e] : 0;
+        if ((unsigned)mine >= (unsigned)p.n_pages) {
+            bad = true;
+            mine = 0;
+        }
     };
     // First row of 16 tokens among the pages' rows; token: the same for the whole wave, before the end.
     auto row_at = [&](int token) __attribute__((always_inline)) {
         const int page = __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane((token >> p.shift) - first));
         return ((((size_t)page * p.n_kv) + kvh) << p.shift) + (token & in_mask);
     };
-    auto reach = [&](int t) __attribute__((always_inline)) {   // the pages of tile t
-        if (((t * kTokens + kTokens - 16) >> p.shift) - first >= 64) {
-            first = (t * kTokens) >> p.shift;
-            look();
-        }
-    };
     look();
 
-    // A bf16 tile comes by LDS DMA: waves 0 and 1 move 32 rows of keys each, waves 2 and 3 of values, four rows an instruction;
-    // lane i the chunk that belongs at place i mod 16 of row i / 16.
+    // A bf16 tile comes by LDS DMA: a wave moves 16 of its rows, four an instruction; lane i the chunk that belongs at place
+    // i mod 16 of row i / 16.
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-    auto dma = [&](int t) __attribute__((always_inline)) {
-        reach(t);
-        const bool v = wave >= 2;
-        const unsigned char* pages = v ? p.pages.v : p.pages.k;
+    auto dma = [&](int t, bool v) __attribute__((always_inline)) {
+        const int r = 16 * wave;
+        if (t * kTokens + r >= p.len) return;
+        const unsigned char* base = (v ? p.pages.v : p.pages.k) + row_at(t * kTokens + r) * (HD * B);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int r = 32 * (wave & 1) + 16 * x;            // the first of 16 rows
-            if (t * kTokens + r >= p.len) continue;
-            const unsigned char* base = pages + row_at(t * kTokens + r) * (HD * B);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 4 * i + (lane >> 4);
-                const int c = (lane & 15) ^ (v ? 4 * (row & 3) : row);
-                if (HD == 128 || c < CHUNKS)
-                    dma16(base, (uint32_t)(row * (HD * B) + c * 16), lds0 + (t & 1) * kStageBytes + (v ? kTileBytes : 0) + (r + 4 * i) * kRowBytes);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int row = 4 * i + (lane >> 4);
+            const int c = (lane & 15) ^ (v ? 4 * (row & 3) : row);
+            if (HD == 128 || c < CHUNKS)
+                dma16(base, (uint32_t)(row * (HD * B) + c * 16), lds0 + (t & 1) * kStageBytes + (v ? kTileBytes : 0) + (r + 4 * i) * kRowBytes);
         }
     };
     // An 8-bit tile goes through registers, where it is widened: chunk `chunk` of rows row, row + STEP, .. a thread.  All lanes
     // of a wave are in 16 rows of one page.
     const int row = tid / CHUNKS, chunk = tid % CHUNKS;
     u32x4_t kr[SCALED ? LOADS : 1], vr[SCALED ? LOADS : 1];
-    uint32_t sr = 0;
-    auto load = [&](int t) __attribute__((always_inline)) {
-        reach(t);
+    uint32_t sr = 0;                               // scale bytes of 16 tokens a wave, of the keys and then of the values
+    auto load = [&](u32x4_t(&x)[SCALED ? LOADS : 1], const unsigned char* pages, int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = t * kTokens + __builtin_amdgcn_readfirstlane((row + i * STEP) & ~15);
             const size_t at = ((r < p.len ? row_at(r) : 0) + ((row + i * STEP) & 15)) * (HD * B) + 16 * chunk;   // (past the end: any)
-            kr[i] = *reinterpret_cast<const u32x4_t*>(p.pages.k + at);
-            vr[i] = *reinterpret_cast<const u32x4_t*>(p.pages.v + at);
+            x[i] = *reinterpret_cast<const u32x4_t*>(pages + at);
         }
-        // the scale of a key (waves 0 and 1) or value of 32 tokens a wave, the upper lanes idle
-        const int r = t * kTokens + 32 * (wave & 1);
-        const size_t a = r < p.len ? row_at(r) : 0, b = r + 16 < p.len ? row_at(r + 16) : 0;
-        sr = 0;
-        if (lane < 32 && r + lane < p.len) sr = (wave < 2 ? p.pages.ks : p.pages.vs)[(lane & 16 ? b : a) + (lane & 15)];
     };
-    auto store = [&](int t) __attribute__((always_inline)) {
-        unsigned char* K = lds + (t & 1) * kStageBytes;
-        unsigned char* V = K + kTileBytes;
+    auto store = [&](const u32x4_t(&x)[SCALED ? LOADS : 1], unsigned char* to, bool v) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = row + i * STEP;
-            const u32x4_t v = t * kTokens + r < p.len ? vr[i] : u32x4_t{0, 0, 0, 0};   // behind the last token: no part of a sum
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const int c = 2 * chunk + y;
-                *reinterpret_cast<u32x4_t*>(K + r * kRowBytes + ((c ^ (r & 15)) << 4)) =
-                    u32x4_t{widen<DT, false>(kr[i][2 * y]), widen<DT, true>(kr[i][2 * y]), widen<DT, false>(kr[i][2 * y + 1]), widen<DT, true>(kr[i][2 * y + 1])};
-                *reinterpret_cast<u32x4_t*>(V + r * kRowBytes + ((c ^ (4 * (r & 3))) << 4)) =
-                    u32x4_t{widen<DT, false>(v[2 * y]), widen<DT, true>(v[2 * y]), widen<DT, false>(v[2 * y + 1]), widen<DT, true>(v[2 * y + 1])};
+                const int c = (2 * chunk + y) ^ (v ? 4 * (r & 3) : r & 15);
+                *reinterpret_cast<u32x4_t*>(to + r * kRowBytes + (c << 4)) =
+                    u32x4_t{widen<DT, false>(x[i][2 * y]), widen<DT, true>(x[i][2 * y]), widen<DT, false>(x[i][2 * y + 1]), widen<DT, true>(x[i][2 * y + 1])};
             }
         }
-        if (lane < 32) scales[(t & 1) * 2 * kTokens + 32 * wave + lane] = scale_of(sr);
+    };
+    // Keys of tile t + 1 (and the scales of its keys and values), and values of tile t, are asked for ..
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+        if (t + 1 < t1) {
+            if ((((t + 1) * kTokens + kTokens - 16) >> p.shift) - first >= 64) {
+                first = (max(t, t0) * kTokens) >> p.shift;
+                look();
+            }
+            if constexpr (SCALED) {
+                load(kr, p.pages.k, t + 1);
+                const int r = (t + 1) * kTokens + 16 * wave;
+                const size_t at = r < p.len ? row_at(r) : 0;
+                sr = lane < 32 && r + (lane & 15) < p.len ? (lane < 16 ? p.pages.ks : p.pages.vs)[at + (lane & 15)] : 127;   // (past the end: 1)
+            } else dma(t + 1, false);
+        }
+        if (t >= t0 && t < t1) {
+            if constexpr (SCALED) load(vr, p.pages.v, t);
+            else dma(t, true);
+        }
+    };
+    // .. and have arrived in LDS, for all waves.
+    auto arrive = [&](int t) __attribute__((always_inline)) {
+        if constexpr (SCALED) {
+            if (t + 1 < t1) {
+                store(kr, lds + ((t + 1) & 1) * kStageBytes, false);
+                if (lane < 32) scales[((t + 1) & 3) * 2 * kTokens + (lane & 16) * (kTokens / 16) + 16 * wave + (lane & 15)] = scale_of(sr);
+            }
+            if (t >= t0) store(vr, lds + (t & 1) * kStageBytes + kTileBytes, true);
+        } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
     };
 
-    if (t0 < t1) {
-        if constexpr (SCALED) load(t0);
-        else dma(t0);
-    }
-    // this lane's query, 16 kk + 8 h .. of it; negated for a negative scale, so that the largest score is that of the largest product
+    if (t0 < t1) fetch(t0 - 1);
+    // this lane's query, 16 kk + 8 h .. of it; negated for a negative scale, so that the largest score is that of the largest
+    // product, and nothing of it for a scale of 0
     bf16x8_t qf[NQ][NK];
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
-    const float scale = fabsf(p.scale_log2);
+    const bool no_scale = p.scale_log2 == 0.f;
+    const float scale = no_scale ? 1.f : fabsf(p.scale_log2);
     {
         const int r = min(r0 + n, p.rows - 1), seq = r / p.group;
         const T* q = static_cast<const T*>(p.q) + (size_t)seq * p.ld_q + (size_t)(kvh * p.group + r - seq * p.group) * HD + 8 * h;
@@ -185,7 +191,11 @@ prefix_kernel(PrefixParams p) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[i][e] ^= flip;
+                for (int e = 0; e < 4; ++e) {
+                    x[i][e] ^= flip;
+                    if (no_scale)    // zeros, but for what is not a number, or infinite
+                        x[i][e] = ((x[i][e] & 0x7F80u) == 0x7F80u ? 0x7FC0u : 0u) | ((x[i][e] & 0x7F800000u) == 0x7F800000u ? 0x7FC00000u : 0u);
+                }
                 qf[i][kk] = __builtin_bit_cast(bf16x8_t, x[i]);
             }
         }
@@ -202,137 +212,169 @@ prefix_kernel(PrefixParams p) {
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -INFINITY, l = 0.f;
 
+    // Half a tile at a time: s[i] is token 32 kb + 8 (i / 4) + 4 h + i % 4 of tile t.  Steps of one product each: `step` kk of
+    // the first, `step` (x, c) of the second.
+    auto key_at = [&](int t, int kb, int kk) __attribute__((always_inline)) {
+        return *reinterpret_cast<const bf16x8_t*>(lds + (t & 1) * kStageBytes + (kb * 32 + n) * kRowBytes + (((2 * kk + h) ^ (n & 15)) << 4));
+    };
+    auto score = [&](const bf16x8_t& kf, int kk, f32x16_t& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i][kk], s, 0, 0, 0);
+    };
     const int tg = lane >> 4, tj = (lane >> 2) & 3, tu = lane & 3;
     const int v_off = (4 * (tg >> 1) + tj) * kRowBytes + (2 * (tg & 1) + (tu >> 1)) * 16 + 8 * (tu & 1);
-    if constexpr (SCALED) {
-        if (t0 < t1) {
-            store(t0);
-            if (t0 + 1 < t1) load(t0 + 1);
-        }
-        __syncthreads();
-    }
-    for (int t = t0; t < t1; ++t) {
-        unsigned char* K = lds + (t & 1) * kStageBytes;
-        unsigned char* V = K + kTileBytes;
-        const float* ks = scales + (t & 1) * 2 * kTokens;
+    auto value_at = [&](int t, int kb, int x, int c) __attribute__((always_inline)) {
+        const unsigned char* at = lds + (t & 1) * kStageBytes + kTileBytes + (kb * 32 + 16 * x) * kRowBytes + v_off +
+                                  ((c ^ tj) << 6);   // four chunks on, moved by the row's swizzle
+        const v4s_t lo = lds_read_tr16(at), hi = lds_read_tr16(at + 8 * kRowBytes);
+        return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 0, 1)), __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 2, 3)),
+                       __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 0, 1)), __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 2, 3))};
+    };
+    auto value = [&](const u32x4_t& vv, int c, const u32x4_t(&pf)[NP]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), __builtin_bit_cast(bf16x8_t, pf[i]), o[c], 0, 0, 0);
+    };
+    auto scores = [&](int t, int kb, f32x16_t& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) score(key_at(t, kb, kk), kk, s);
+    };
+    auto values = [&](int t, int kb, const u32x4_t(&pf)[2][NP]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int c = 0; c < NT; ++c) value(value_at(t, kb, x, c), c, pf[x]);
+    };
+    // No scores for tokens past the end.
+    auto mask = [&](int t, int kb, f32x16_t& s) __attribute__((always_inline)) {
         const int there = p.len - t * kTokens;
+        if (there < kTokens) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (32 * kb + 8 * (i >> 2) + 4 * h + (i & 3) >= there) s[i] = -INFINITY;
+        }
+    };
+    // The reference of half a tile's weights; what is added up so far is to be scaled by f.
+    auto refer = [&](int t, int kb, f32x16_t& s) __attribute__((always_inline)) {
         if constexpr (SCALED) {
-            if (t + 1 < t1) {       // into the stage that every wave left at the last barrier
-                store(t + 1);
-                if (t + 2 < t1) load(t + 2);
+            const float* ks = scales + (t & 3) * 2 * kTokens + 32 * kb + 4 * h;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const f32x4_t f = *reinterpret_cast<const f32x4_t*>(ks + 2 * i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[i + e] *= f[e];
             }
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();        // tile t is there, and every wave is done with the one before
-            if (there < kTokens) {  // values behind the last token: no part of a sum, whatever they are
-                for (int i = tid; i < (kTokens - there) * 16; i += 256)
-                    *reinterpret_cast<u32x4_t*>(V + (there + i / 16) * kRowBytes + (i % 16) * 16) = u32x4_t{0, 0, 0, 0};
-                __syncthreads();
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * scale;
+        // It moves only when a score passes it by more than kLazy: weights stay below 2^kLazy, and the sums are rescaled for
+        // few tiles.
+        const float mn = mx > m + kLazy ? mx : m;
+        const float f = __builtin_amdgcn_exp2f(m - ref_of(mn));
+        m = mn;
+        l *= f;
+        return f;
+    };
+    // Two weights, as a word of each of the second product's operands.
+    auto weigh = [&](int t, int kb, int j, const f32x16_t& s, float neg_ref, u32x4_t(&pf)[2][NP]) __attribute__((always_inline)) {
+        float a = __builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, neg_ref)), b = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, neg_ref));
+        l += a;
+        l += b;
+        if constexpr (SCALED) {
+            const float2 f = *reinterpret_cast<const float2*>(scales + (t & 3) * 2 * kTokens + kTokens + 32 * kb + 4 * h + 8 * (j >> 1) + 2 * (j & 1));
+            a *= f.x;
+            b *= f.y;
+        }
+        uint32_t y[NP];
+        if constexpr (NP == 2) round_split(a, b, y);
+        else split_bf16<NP>(a, b, y);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) pf[j >> 2][i][j & 3] = y[i];
+    };
+    auto weights = [&](int t, int kb, f32x16_t& s, u32x4_t(&pf)[2][NP]) __attribute__((always_inline)) {
+        const float f = refer(t, kb, s), neg_ref = -ref_of(m);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) weigh(t, kb, j, s, neg_ref, pf);
+        return f;
+    };
+    auto rescale = [&](float f) __attribute__((always_inline)) {
+        if (__any(f != 1.f)) {
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[c][i] *= f;
+        }
+    };
+    // scores(tn, kn, sn), values(tv, kv, pv) and weights(ts, ks, s, pf) in eight pieces, so that the vector unit makes two weights
+    // while the matrix cores work on a piece of the products.
+    auto half = [&](int tn, int kn, f32x16_t& sn, int tv, int kv, const u32x4_t(&pv)[2][NP], int ts, int ks, f32x16_t& s, u32x4_t(&pf)[2][NP])
+        __attribute__((always_inline)) {
+        bf16x8_t kf = key_at(tn, kn, 0);
+        u32x4_t vv = value_at(tv, kv, 0, 0);
+        float f = 1.f, neg_ref = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sn[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            constexpr int NV = 2 * NT;
+            const int k0 = j * NK / 8, k1 = (j + 1) * NK / 8, v0 = j * NV / 8, v1 = (j + 1) * NV / 8;   // (a piece has one of each or none)
+            const bf16x8_t kf_now = kf;
+            const u32x4_t vv_now = vv;
+            if (k1 > k0 && k1 < NK) kf = key_at(tn, kn, k1);
+            if (v1 > v0 && v1 < NV) vv = value_at(tv, kv, v1 / NT, v1 % NT);
+            if (k1 > k0) score(kf_now, k0, sn);
+            if (v1 > v0) value(vv_now, v0 % NT, pv[v0 / NT]);
+            if (j == 0) {
+                f = refer(ts, ks, s);
+                neg_ref = -ref_of(m);
             }
-            if (t + 1 < t1) dma(t + 1);
+            weigh(ts, ks, j, s, neg_ref, pf);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return f;
+    };
+    // The halves of the tiles follow each other so that the matrix cores have work while one half's weights are made: the next
+    // half's scores, and the values of the one before.  The keys of tile t + 1 and the values of tile t are needed from the
+    // second half of tile t on: there the waves meet, and the stages that the keys of tile t and the values of
+    // tile t - 1 lay in are filled anew.
+    if (t0 < t1) {
+        f32x16_t sa, sb;
+        u32x4_t pa[2][NP], pb[2][NP];
+        arrive(t0 - 1);
+        fetch(t0);
+        if (rows_here) {
+            scores(t0, 0, sa);
+            scores(t0, 1, sb);
+            mask(t0, 0, sa);
+            weights(t0, 0, sa, pa);
+        }
+        for (int t = t0; t + 1 < t1; ++t) {
+            arrive(t);
+            fetch(t + 1);
+            if (!rows_here) continue;
+            rescale(half(t + 1, 0, sa, t, 0, pa, t, 1, sb, pb));
+            mask(t + 1, 0, sa);
+            rescale(half(t + 1, 1, sb, t, 1, pb, t + 1, 0, sa, pa));
+        }
+        arrive(t1 - 1);
+        const int there = p.len - (t1 - 1) * kTokens;
+        if (there < kTokens) {     // values behind the last token: no part of a sum, whatever they are
+            unsigned char* V = lds + ((t1 - 1) & 1) * kStageBytes + kTileBytes;
+            for (int i = tid; i < (kTokens - there) * 16; i += 256)
+                *reinterpret_cast<u32x4_t*>(V + (there + i / 16) * kRowBytes + (i % 16) * 16) = u32x4_t{0, 0, 0, 0};
+            __syncthreads();
         }
         if (rows_here) {
-            f32x16_t s[2];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < NK; ++kk)
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(K + (kb * 32 + n) * kRowBytes + (((2 * kk + h) ^ (n & 15)) << 4));
-#pragma unroll
-                    for (int i = 0; i < NQ; ++i) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i][kk], s[kb], 0, 0, 0);
-                }
-            // s[kb][i]: token 32 kb + 8 (i / 4) + 4 h + i % 4
-            if constexpr (SCALED) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(ks + 32 * kb + 2 * i + 4 * h);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[kb][i + e] *= f[e];
-                    }
-            }
-            if (there < kTokens) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (32 * kb + 8 * (i >> 2) + 4 * h + (i & 3) >= there) s[kb][i] = -INFINITY;
-            }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb][i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
-            // The reference moves only when a score passes it by more than kLazy: weights stay below 2^kLazy, and the sums
-            // are rescaled in few tiles.
-            const float mn = mx > m + kLazy ? mx : m;
-            if (__any(mn != m)) {
-                const float f = __builtin_amdgcn_exp2f(m - ref_of(mn));
-                l *= f;
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[c][i] *= f;
-                m = mn;
-            }
-            const float neg_ref = -ref_of(m);
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int ks_ = 0; ks_ < 2; ++ks_) {
-                    // the values first: they arrive while the weights are worked out
-                    const unsigned char* vb = V + (kb * 32 + 16 * ks_) * kRowBytes + v_off;
-                    u32x4_t vv[NT];
-#pragma unroll
-                    for (int c = 0; c < NT; ++c) {
-                        const int at = (c ^ tj) << 6;   // four chunks on, moved by the row's swizzle
-                        const v4s_t lo = lds_read_tr16(vb + at), hi = lds_read_tr16(vb + at + 8 * kRowBytes);
-                        vv[c] = u32x4_t{__builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 0, 1)),
-                                        __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 2, 3)),
-                                        __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 0, 1)),
-                                        __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 2, 3))};
-                    }
-                    float w[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(fmaf(s[kb][8 * ks_ + j], scale, neg_ref));
-                    if (there < kTokens) {     // (-infinity times a scale of 0)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (32 * kb + 16 * ks_ + 8 * (j >> 2) + 4 * h + (j & 3) >= there) w[j] = 0.f;
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) l += w[j];
-                    if constexpr (SCALED) {
-#pragma unroll
-                        for (int j = 0; j < 8; j += 4) {
-                            const f32x4_t f = *reinterpret_cast<const f32x4_t*>(ks + kTokens + 32 * kb + 16 * ks_ + 2 * j + 4 * h);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) w[j + e] *= f[e];
-                        }
-                    }
-                    u32x4_t pf[NP];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t x[NP];
-                        if constexpr (NP == 2) round_split(w[2 * j], w[2 * j + 1], x);
-                        else split_bf16<NP>(w[2 * j], w[2 * j + 1], x);
-#pragma unroll
-                        for (int i = 0; i < NP; ++i) pf[i][j] = x[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < NP; ++i)
-#pragma unroll
-                        for (int c = 0; c < NT; ++c)
-                            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv[c]), __builtin_bit_cast(bf16x8_t, pf[i]), o[c], 0, 0, 0);
-                }
+            mask(t1 - 1, 1, sb);
+            values(t1 - 1, 0, pa);
+            rescale(weights(t1 - 1, 1, sb, pb));
+            values(t1 - 1, 1, pb);
         }
-        if constexpr (SCALED) __syncthreads();
     }
     l += __shfl_xor(l, 32);
     if (t0 == t1) l = kNoTokens;
@@ -341,18 +383,21 @@ prefix_kernel(PrefixParams p) {
         l = NAN;
         if (tid == 0) *p.status = RIFT_ERR_SHAPE;
     }
-    if (r0 + n < p.rows) {
-        float* dst = p.slots + (((size_t)kvh * p.parts + part) * p.rows + r0 + n) * RS;
+    // The wave's rows lie together in the workspace: through LDS (all of it: four times 32 rows), so that whole lines are written.
+    if (!rows_here) return;
+    float* out = reinterpret_cast<float*>(lds) + wave * 32 * RS;
+    float* dst = out + n * RS;
 #pragma unroll
-        for (int c = 0; c < NT; ++c)
+    for (int c = 0; c < NT; ++c)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)   // dimensions 32 c + 2 i + 4 h ..
-                *reinterpret_cast<f32x4_t*>(dst + 32 * c + 2 * i + 4 * h) = f32x4_t{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]};
-        if (h == 0) {
-            dst[HD] = m;
-            dst[HD + 1] = l;
-        }
-    }
+        for (int i = 0; i < 16; i += 4)   // dimensions 32 c + 2 i + 4 h ..
+            *reinterpret_cast<f32x4_t*>(dst + 32 * c + 2 * i + 4 * h) = f32x4_t{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]};
+    if (h == 0) *reinterpret_cast<f32x4_t*>(dst + HD) = f32x4_t{m, l, 0.f, 0.f};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    f32x4_t* to = reinterpret_cast<f32x4_t*>(p.slots + (((size_t)kvh * p.parts + part) * p.rows + r0) * RS);
+    const int quads = min(p.rows - r0, 32) * (RS / 4);
+    for (int i = lane; i < quads; i += 64) to[i] = reinterpret_cast<const f32x4_t*>(out)[i];
 }
 
 }  // namespace
@@ -368,6 +413,7 @@ int prefix_parts(int n_kv, int64_t rows, int len) {
 hipError_t launch_prefix(const riftkv_cache& c, bool bf16, PrefixParams p, hipStream_t st) {
     p.row_tiles = (p.rows + kRows - 1) / kRows;
     const size_t lds = 2 * kStageBytes + kScaleFloats * sizeof(float);
+    static_assert(2 * kStageBytes + kScaleFloats * sizeof(float) >= kRows * (128 + 4) * sizeof(float), "the rows of a workgroup");
     auto run = [&](auto kernel) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
