@@ -2,30 +2,42 @@
 // each sequence and query head of the group, stand under each other, so that a tile of keys and values is read
 // once for up to 128 of them.
 //
-//   prefix_kernel   a workgroup takes 128 rows of a key head and a part of the prefix, a wave 32 of the rows.  Tiles of
-//                   64 tokens go through two LDS stages, widened to bf16 on the way; the next tile's loads are in
-//                   flight meanwhile.  Weighted values, largest score and sum of a part go to the workspace,
-//                   where ranges_kernel joins them with the sequences' own.
+// A workgroup takes 128 rows of a key head and a part of the prefix, a wave 32 of the rows.  Tiles of 64 tokens go through two LDS
+// stages, by LDS DMA or, 8-bit ones, through registers where they are widened to bf16; the next tile is under way meanwhile.
+// Weighted values, a reference and the sum of a part go to the workspace.
 //
 // S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds the scores of one query, and its weights are
-// already its share of the second product's right operand, whose left one comes from transposing LDS reads.  Weights,
-// and float32 queries, go into the products as three bf16 terms that add up to them, as in the attention of single sequences.
+// already its share of the second product's right operand, whose left one comes from transposing LDS reads.  Float32 queries and
+// their weights go into the products as three bf16 terms that add up to them; the weights of bf16 queries as two, short by
+// 2^-17 of a weight at most, where the output is rounded to 2^-9.
 //
 // Rows of a tile are 256 bytes (64 dimensions fill half of them); the 16-byte chunks of row r lie at chunk ^ (r & 15) for
 // keys and at chunk ^ 4 (r & 3) for values, so that neither read meets a bank twice.
-#include <type_traits>
+#pragma once
 
-#include "kv_ranges.h"
+#include "kv_tile.h"
 
 namespace rift {
 
-namespace {
+// Rows of queries, one for each sequence and query head of a key head's group, over a prefix.
+struct PrefixParams {
+    const void* q;
+    int64_t ld_q;
+    TilePages pages;
+    const int* table;
+    int* status;
+    float* slots;        // [key head][parts][rows][HD + 4]: weighted values, a reference, sum
+    int len, n_kv, n_pages, shift, group, rows, row_tiles, parts;
+    float scale_log2;
+};
 
 constexpr int kRows = 128, kTokens = 64;      // of a workgroup, of a tile
 constexpr int kRowBytes = 256;
 constexpr int kTileBytes = kTokens * kRowBytes;
 constexpr int kStageBytes = 2 * kTileBytes;   // keys, then values
 constexpr int kScaleFloats = 4 * 2 * kTokens; // of keys and values, four tiles
+constexpr size_t kPrefixLds = 2 * kStageBytes + kScaleFloats * sizeof(float);
+static_assert(kPrefixLds >= kRows * (128 + 4) * sizeof(float), "the rows of a workgroup");
 constexpr float kLazy = 8.f;                  // log2 units by which a score may pass the reference
 
 typedef short v4s_t __attribute__((ext_vector_type(4)));
@@ -45,6 +57,12 @@ __device__ __forceinline__ void round_split(float a, float b, uint32_t (&w)[2]) 
     w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
 }
 
+// A value that has to be there at this point of the program.
+template <typename X>
+__device__ __forceinline__ void hold(X& x) {
+    asm volatile("" : "+v"(x));
+}
+
 // LDS DMA of 16 bytes a lane: from a wave-uniform base and a lane's offset to lds + 16 lane.
 __device__ __forceinline__ void dma16(const unsigned char* base, uint32_t offset, uint32_t lds) {
     const uint64_t b = (uint64_t)(uintptr_t)base;
@@ -53,9 +71,9 @@ __device__ __forceinline__ void dma16(const unsigned char* base, uint32_t offset
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(ub) : "memory", "m0");
 }
 
+// Workgroup `block` of n_kv * row_tiles * parts; lds: kPrefixLds bytes, two stages, then their scales.
 template <typename T, riftkv_dtype DT, int HD>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1)
-prefix_kernel(PrefixParams p) {
+__device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, unsigned char* lds) {
     constexpr int B = DT == RIFTKV_BF16 ? 2 : 1;
     constexpr bool SCALED = B == 1;
     constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
@@ -64,12 +82,11 @@ prefix_kernel(PrefixParams p) {
     constexpr int STEP = 256 / CHUNKS;            // rows between them
     constexpr int NK = HD / 16, NT = HD / 32;     // steps of the first product, 32-dimension blocks of the second
     constexpr int RS = HD + 4;
-    extern __shared__ __align__(16) unsigned char lds[];   // two stages, then their scales
     float* scales = reinterpret_cast<float*>(lds + 2 * kStageBytes);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, n = lane & 31;
-    const int part = blockIdx.x % p.parts, rest = blockIdx.x / p.parts;
+    const int part = block % p.parts, rest = block / p.parts;
     const int kvh = rest / p.row_tiles, r0 = (rest - kvh * p.row_tiles) * kRows + 32 * wave;
     const int tiles = (p.len + kTokens - 1) / kTokens;
     const int t0 = (int)((int64_t)tiles * part / p.parts), t1 = (int)((int64_t)tiles * (part + 1) / p.parts);
@@ -230,10 +247,8 @@ prefix_kernel(PrefixParams p) {
         return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 0, 1)), __builtin_bit_cast(uint32_t, __builtin_shufflevector(lo, lo, 2, 3)),
                        __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 0, 1)), __builtin_bit_cast(uint32_t, __builtin_shufflevector(hi, hi, 2, 3))};
     };
-    auto value = [&](const u32x4_t& vv, int c, const u32x4_t(&pf)[NP]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), __builtin_bit_cast(bf16x8_t, pf[i]), o[c], 0, 0, 0);
+    auto value_term = [&](const u32x4_t& vv, int c, const u32x4_t& pf) __attribute__((always_inline)) {
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), __builtin_bit_cast(bf16x8_t, pf), o[c], 0, 0, 0);
     };
     auto scores = [&](int t, int kb, f32x16_t& s) __attribute__((always_inline)) {
 #pragma unroll
@@ -245,7 +260,11 @@ prefix_kernel(PrefixParams p) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int c = 0; c < NT; ++c) value(value_at(t, kb, x, c), c, pf[x]);
+            for (int c = 0; c < NT; ++c) {
+                const u32x4_t vv = value_at(t, kb, x, c);
+#pragma unroll
+                for (int i = 0; i < NP; ++i) value_term(vv, c, pf[x][i]);
+            }
     };
     // No scores for tokens past the end.
     auto mask = [&](int t, int kb, f32x16_t& s) __attribute__((always_inline)) {
@@ -280,9 +299,9 @@ prefix_kernel(PrefixParams p) {
         l *= f;
         return f;
     };
-    // Two weights, as a word of each of the second product's operands.
-    auto weigh = [&](int t, int kb, int j, const f32x16_t& s, float neg_ref, u32x4_t(&pf)[2][NP]) __attribute__((always_inline)) {
-        float a = __builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, neg_ref)), b = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, neg_ref));
+    auto weight = [&](float s, float neg_ref) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(fmaf(s, scale, neg_ref)); };
+    // The j-th two weights, as a word of each of the second product's operands.
+    auto split_pair = [&](int t, int kb, int j, float a, float b, uint32_t(&y)[NP]) __attribute__((always_inline)) {
         l += a;
         l += b;
         if constexpr (SCALED) {
@@ -290,16 +309,18 @@ prefix_kernel(PrefixParams p) {
             a *= f.x;
             b *= f.y;
         }
-        uint32_t y[NP];
         if constexpr (NP == 2) round_split(a, b, y);
         else split_bf16<NP>(a, b, y);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) pf[j >> 2][i][j & 3] = y[i];
     };
     auto weights = [&](int t, int kb, f32x16_t& s, u32x4_t(&pf)[2][NP]) __attribute__((always_inline)) {
         const float f = refer(t, kb, s), neg_ref = -ref_of(m);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) weigh(t, kb, j, s, neg_ref, pf);
+        for (int j = 0; j < 8; ++j) {
+            uint32_t y[NP];
+            split_pair(t, kb, j, weight(s[2 * j], neg_ref), weight(s[2 * j + 1], neg_ref), y);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) pf[j >> 2][i][j & 3] = y[i];
+        }
         return f;
     };
     auto rescale = [&](float f) __attribute__((always_inline)) {
@@ -323,18 +344,37 @@ prefix_kernel(PrefixParams p) {
         for (int j = 0; j < 8; ++j) {
             constexpr int NV = 2 * NT;
             const int k0 = j * NK / 8, k1 = (j + 1) * NK / 8, v0 = j * NV / 8, v1 = (j + 1) * NV / 8;   // (a piece has one of each or none)
-            const bf16x8_t kf_now = kf;
-            const u32x4_t vv_now = vv;
+            // A product of the matrix cores holds the next one up: between two of them stands what the vector unit can do, and the
+            // empty asm keeps it there.
+            bf16x8_t kf_now = kf;
+            u32x4_t vv_now = vv;
             if (k1 > k0 && k1 < NK) kf = key_at(tn, kn, k1);
             if (v1 > v0 && v1 < NV) vv = value_at(tv, kv, v1 / NT, v1 % NT);
+            hold(kf_now);
             if (k1 > k0) score(kf_now, k0, sn);
-            if (v1 > v0) value(vv_now, v0 % NT, pv[v0 / NT]);
             if (j == 0) {
                 f = refer(ts, ks, s);
                 neg_ref = -ref_of(m);
             }
-            weigh(ts, ks, j, s, neg_ref, pf);
-            __builtin_amdgcn_sched_barrier(0);
+            float w0 = s[2 * j], w1 = s[2 * j + 1];
+            hold(w0);
+            hold(w1);
+            w0 = weight(w0, neg_ref);
+            w1 = weight(w1, neg_ref);
+            hold(w0);
+            hold(w1);
+            hold(vv_now);
+            if (v1 > v0) value_term(vv_now, v0 % NT, pv[v0 / NT][0]);
+            uint32_t y[NP];
+            split_pair(ts, ks, j, w0, w1, y);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                hold(y[i]);
+                pf[j >> 2][i][j & 3] = y[i];
+            }
+#pragma unroll
+            for (int i = 1; i < NP; ++i)
+                if (v1 > v0) value_term(vv_now, v0 % NT, pv[v0 / NT][i]);
         }
         return f;
     };
@@ -398,38 +438,6 @@ prefix_kernel(PrefixParams p) {
     f32x4_t* to = reinterpret_cast<f32x4_t*>(p.slots + (((size_t)kvh * p.parts + part) * p.rows + r0) * RS);
     const int quads = min(p.rows - r0, 32) * (RS / 4);
     for (int i = lane; i < quads; i += 64) to[i] = reinterpret_cast<const f32x4_t*>(out)[i];
-}
-
-}  // namespace
-
-// a part has two tiles at least; two workgroups a CU
-int prefix_parts(int n_kv, int64_t rows, int len) {
-    const int64_t wgs = n_kv * ((rows + kRows - 1) / kRows), tiles = (len + kTokens - 1) / kTokens;
-    int64_t parts = 512 / wgs;
-    if (parts > tiles / 2) parts = tiles / 2;
-    return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : (int)parts;
-}
-
-hipError_t launch_prefix(const riftkv_cache& c, bool bf16, PrefixParams p, hipStream_t st) {
-    p.row_tiles = (p.rows + kRows - 1) / kRows;
-    const size_t lds = 2 * kStageBytes + kScaleFloats * sizeof(float);
-    static_assert(2 * kStageBytes + kScaleFloats * sizeof(float) >= kRows * (128 + 4) * sizeof(float), "the rows of a workgroup");
-    auto run = [&](auto kernel) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)p.n_kv * p.row_tiles * p.parts)), dim3(256), lds, st, p);
-        return hipGetLastError();
-    };
-    auto types = [&](auto dt) {
-        if (c.head_dim == 128) return bf16 ? run(prefix_kernel<bf16_t, dt.value, 128>) : run(prefix_kernel<float, dt.value, 128>);
-        return bf16 ? run(prefix_kernel<bf16_t, dt.value, 64>) : run(prefix_kernel<float, dt.value, 64>);
-    };
-    switch (c.dt) {
-        case RIFTKV_BF16: return types(std::integral_constant<riftkv_dtype, RIFTKV_BF16>{});
-        case RIFTKV_FP8: return types(std::integral_constant<riftkv_dtype, RIFTKV_FP8>{});
-        case RIFTKV_INT8: return types(std::integral_constant<riftkv_dtype, RIFTKV_INT8>{});
-        default: return hipErrorInvalidValue;
-    }
 }
 
 }  // namespace rift

@@ -1,20 +1,22 @@
 // One query token of every sequence over ranges of paged keys and values: the pages of a list
 // (riftkv_attention_pages), or a prefix that all sequences share and then their own (riftkv_attention_shared).
 //
-//   ranges_kernel   a workgroup takes a part of the tokens of up to 16 query rows of one key head; its waves
-//                   share the part's tiles and join in LDS.  Where the tokens are one part, it joins them with the
-//                   prefix' parts, if there is one, and writes the output.
-//   parts_kernel    otherwise: the sum of the parts.
-// A shared prefix comes first, by prefix_kernel (kv_prefix.hip) or, for few rows and float32 pages, by ranges_kernel.
+//   listed_kernel   a workgroup takes a part of the tokens of up to 16 query heads of one key head; its waves share the
+//                   part's tiles and join in LDS.  Where the tokens are one part, the output is written here.
+//   shared_kernel   the same for a sequence's own tokens, and beside them, in the same launch, workgroups for the prefix:
+//                   prefix_body (kv_prefix.h), or for few rows and float32 pages as above, 16 rows of a key head whatever
+//                   their sequences.  A short prefix is walked by every sequence itself.
+//   parts_kernel    the sum of the parts.
 #include <type_traits>
 
-#include "kv_ranges.h"
+#include "kv_prefix.h"
 
 namespace rift {
 
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kMaxParts = 64;   // of an item's tokens: a lane each where they are joined
 
 struct RangeParams {
     const void* q;
@@ -23,9 +25,11 @@ struct RangeParams {
     TilePages pages;
     int* status;
     float* slots;            // [sequence][head group][parts][rows][HD + 4]: weighted values, largest score, sum
-    const float* front;      // parts of a prefix, [key head][front_parts][n_seq * group][HD + 4]
-    int n_kv, group, q_tiles, rows, parts, n_pages, shift, front_parts, item0;
+    float* front;            // parts of a prefix, [key head][front_parts][front_rows][HD + 4]
     int64_t front_rows;      // n_seq * group
+    int n_kv, group, q_tiles, rows, parts, n_pages, shift, front_parts;
+    int front_wgs;           // workgroups for the prefix, the first of the launch
+    int item0;               // first item of the others
     float scale_log2;
 };
 
@@ -63,14 +67,18 @@ struct Item {
     int len, n, tiles;
 };
 
+// Where 16 tokens are: in an entry, at a row of its page, and how many of them there can be.
+struct Place {
+    int entry, in_page, most;
+};
+
 // The listed pages, in the list's order.
 struct ListedPages {
     OwnPages own;
     const int* lists;        // [n_seq][n_kv][top]
     int top;
-    static constexpr bool kFront = false;
     __device__ __forceinline__ const int* list(const RangeParams& p, int seq, int kvh) const { return lists + ((size_t)seq * p.n_kv + kvh) * top; }
-    __device__ __forceinline__ Item item(const RangeParams& p, int seq, int kvh, int lane, bool& bad) const {
+    __device__ __forceinline__ Item item(const RangeParams& p, int seq, int kvh, bool, int lane, bool& bad) const {
         Item it;
         it.len = own.length(seq, p.shift, bad);
         it.n = top;
@@ -87,52 +95,53 @@ struct ListedPages {
         it.tiles = ((it.n << p.shift) + kTile - 1) / kTile;
         return it;
     }
-    __device__ __forceinline__ Entry entry(const RangeParams& p, const Item& it, int seq, int kvh, int e) const {
+    __device__ __forceinline__ Entry entry(const RangeParams& p, const Item& it, int seq, int kvh, bool, int e) const {
         return own.at(p, seq, e < it.n ? list(p, seq, kvh)[e] : -1, it.len);
     }
-};
-
-// A sequence's own pages.
-struct WholePages {
-    OwnPages own;
-    static constexpr bool kFront = false;
-    __device__ __forceinline__ Item item(const RangeParams& p, int seq, int, int, bool& bad) const {
-        Item it;
-        it.len = own.length(seq, p.shift, bad);
-        it.n = it.len > 0 ? ((it.len - 1) >> p.shift) + 1 : 0;
-        it.tiles = (it.len + kTile - 1) / kTile;
-        return it;
-    }
-    __device__ __forceinline__ Entry entry(const RangeParams& p, const Item& it, int seq, int, int e) const {
-        return own.at(p, seq, e < it.n ? e : -1, it.len);
+    __device__ __forceinline__ Place place(const RangeParams& p, bool, int tile, int half) const {
+        const int v = tile * kTile + 16 * half;
+        return Place{v >> p.shift, v & ((1 << p.shift) - 1), 16};
     }
 };
 
-// A prefix' pages; its items are 16 rows of a key head, of whatever sequences, and write their parts for the others to join.
-struct PrefixPages {
-    OwnPages own;            // the prefix as sequence 0
-    int len;
-    static constexpr bool kFront = true;
-    __device__ __forceinline__ Item item(const RangeParams& p, int, int, int, bool& bad) const {
+// The prefix (front items); a sequence's own pages, after the first `walked` tokens of the prefix: all or none.
+struct SharedPages {
+    OwnPages own, prefix;    // (the prefix as sequence 0)
+    int prefix_len, walked;
+    __device__ __forceinline__ int walked_pages(int shift) const { return walked > 0 ? prefix.max_pages : 0; }
+    __device__ __forceinline__ Item item(const RangeParams& p, int seq, int, bool front, int, bool& bad) const {
         bad = false;
-        return Item{len, own.max_pages, (len + kTile - 1) / kTile};
+        if (front) return Item{prefix_len, prefix.max_pages, (prefix_len + kTile - 1) / kTile};
+        const int len = own.length(seq, p.shift, bad);
+        return Item{len, walked_pages(p.shift) + (len > 0 ? ((len - 1) >> p.shift) + 1 : 0), (walked + kTile - 1) / kTile + (len + kTile - 1) / kTile};
     }
-    __device__ __forceinline__ Entry entry(const RangeParams& p, const Item& it, int, int, int e) const {
-        return own.at(p, 0, e < it.n ? e : -1, it.len);
+    __device__ __forceinline__ Entry entry(const RangeParams& p, const Item& it, int seq, int, bool front, int e) const {
+        const int before = walked_pages(p.shift);
+        if (front || e < before) return prefix.at(p, 0, e < (front ? it.n : before) ? e : -1, prefix_len);
+        return own.at(p, seq, e < it.n ? e - before : -1, it.len);
+    }
+    __device__ __forceinline__ Place place(const RangeParams& p, bool front, int tile, int half) const {
+        const int before = front ? 0 : (walked + kTile - 1) / kTile, mask = (1 << p.shift) - 1;
+        if (tile < before) {
+            const int v = tile * kTile + 16 * half;
+            return v < walked ? Place{v >> p.shift, v & mask, 16} : Place{0, 0, 0};
+        }
+        const int v = (tile - before) * kTile + 16 * half;
+        return Place{(front ? 0 : walked_pages(p.shift)) + (v >> p.shift), v & mask, 16};
     }
 };
 
+// Workgroup `block` of the items' or, front, of the prefix'.
 template <typename T, riftkv_dtype DT, int HD, typename Where>
-__global__ void __launch_bounds__(64 * kWaves, 2)
-ranges_kernel(RangeParams p, Where where) {
+__device__ __forceinline__ void ranges_body(const RangeParams& p, const Where& where, bool front, int block, float* records) {
     constexpr int RS = HD + 4;
-    extern __shared__ __align__(16) float records[];   // [kWaves][rows][RS]
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // blocks: item by item, each with its parts
-    const int part = blockIdx.x % p.parts, item = blockIdx.x / p.parts + p.item0;
+    // item by item, each with its parts
+    const int n_parts = front ? p.front_parts : p.parts;
+    const int part = block % n_parts, item = block / n_parts + (front ? 0 : p.item0);
     int seq, kvh, r0, rows;                    // sequence, key head, first of its group's rows (of all rows) and how many
-    if constexpr (Where::kFront) {
+    if (front) {
         const int tiles = (int)((p.front_rows + 15) / 16);
         seq = 0;
         kvh = item / tiles;
@@ -148,15 +157,15 @@ ranges_kernel(RangeParams p, Where where) {
     }
 
     bool bad;
-    const Item it = where.item(p, seq, kvh, lane, bad);
-    const int share = part * kWaves + wave, shares = p.parts * kWaves;
+    const Item it = where.item(p, seq, kvh, front, lane, bad);
+    const int share = part * kWaves + wave, shares = n_parts * kWaves;
     int tile = (int)((int64_t)it.tiles * share / shares);
     int left = __builtin_amdgcn_readfirstlane((int)((int64_t)it.tiles * (share + 1) / shares) - tile);
 
     TilePass<T, DT, HD> pass(lane);
     {
         int of = seq, r = r0 + min(pass.n, rows - 1);
-        if constexpr (Where::kFront) {
+        if (front) {
             of = r / p.group;
             r -= of * p.group;
         }
@@ -166,25 +175,24 @@ ranges_kernel(RangeParams p, Where where) {
     if (left > 0) {
         // 64 entries at a time, one a lane: what a tile needs of them is read from its lane, without a load to wait for
         // behind those of keys and values.
-        const int in_mask = (1 << p.shift) - 1;
-        int first = (tile * kTile) >> p.shift;
+        int first = where.place(p, front, tile, 0).entry;
         Entry mine;
         auto look = [&]() __attribute__((always_inline)) {
-            mine = where.entry(p, it, seq, kvh, first + lane);
+            mine = where.entry(p, it, seq, kvh, front, first + lane);
             bad |= __any(mine.bad);
         };
         auto find = [&](int t, Half (&half)[2]) __attribute__((always_inline)) {
-            if (((t * kTile + 16) >> p.shift) - first >= 64) {
-                first = (t * kTile) >> p.shift;
+            const Place at[2] = {where.place(p, front, t, 0), where.place(p, front, t, 1)};
+            if (max(at[0].entry, at[1].entry) - first >= 64) {
+                first = at[0].entry;
                 look();
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int v = t * kTile + 16 * h, in_page = v & in_mask;
-                const int of = __builtin_amdgcn_readfirstlane((v >> p.shift) - first);
+                const int of = __builtin_amdgcn_readfirstlane(max(at[h].entry - first, 0));
                 const int page = __builtin_amdgcn_readlane(mine.page, of), count = __builtin_amdgcn_readlane(mine.count, of);
-                half[h].row = ((((size_t)page * p.n_kv) + kvh) << p.shift) + in_page;
-                half[h].n = max(0, min(count - in_page, 16));
+                half[h].row = ((((size_t)page * p.n_kv) + kvh) << p.shift) + at[h].in_page;
+                half[h].n = max(0, min(count - at[h].in_page, at[h].most));
             }
         };
         look();
@@ -216,9 +224,12 @@ ranges_kernel(RangeParams p, Where where) {
         sum = NAN;
         if (lane == 0) *p.status = RIFT_ERR_SHAPE;
     }
-    const int record = p.rows * RS;
+    const int record = (p.front_wgs > 0 ? 16 : p.rows) * RS;
     pass.put(records + wave * record, rows, sum);
     __syncthreads();
+    const bool direct = !front && p.parts == 1 && p.front_parts == 0;
+    float* slots = front ? p.front + (((size_t)kvh * n_parts + part) * p.front_rows + r0) * RS
+                         : p.slots + ((size_t)item * n_parts + part) * p.rows * RS;
     for (int i = tid; i < rows * (HD / 4); i += 64 * kWaves) {
         const int row = i / (HD / 4), col = 4 * (i % (HD / 4));
         const float* src = records + row * RS;
@@ -232,53 +243,45 @@ ranges_kernel(RangeParams p, Where where) {
             L = fmaf(f, src[w * record + HD + 1], L);
             acc += f * *reinterpret_cast<const f32x4_t*>(src + w * record + col);
         }
-        if constexpr (Where::kFront) {
-            float* slot = p.slots + (((size_t)kvh * p.parts + part) * p.front_rows + r0 + row) * RS;
-            *reinterpret_cast<f32x4_t*>(slot + col) = acc;
-            if (col == 0) *reinterpret_cast<float2*>(slot + HD) = make_float2(mx, L);
-        } else if (p.parts == 1) {
-            if (p.front_parts > 0) {
-                const size_t next = (size_t)p.front_rows * RS;
-                const float* src = p.front + (size_t)kvh * p.front_parts * next + ((size_t)seq * p.group + r0 + row) * RS;
-                constexpr int U = 4;   // parts in flight
-                for (int k0 = 0; k0 < p.front_parts; k0 += U) {
-                    float2 ml[U];
-                    f32x4_t x[U];
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {   // past the last: its values, not used
-                        const float* at = src + min(k0 + u, p.front_parts - 1) * next;
-                        ml[u] = *reinterpret_cast<const float2*>(at + HD);
-                        x[u] = *reinterpret_cast<const f32x4_t*>(at + col);
-                    }
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if (k0 + u >= p.front_parts) continue;
-                        const float mn = fmaxf(mx, ml[u].x);
-                        const float f = __builtin_amdgcn_exp2f(mx - ref_of(mn)), fk = __builtin_amdgcn_exp2f(ml[u].x - ref_of(mn));
-                        acc = acc * f + x[u] * fk;
-                        L = fmaf(fk, ml[u].y, L * f);
-                        mx = mn;
-                    }
-                }
-            }
+        if (direct) {
             acc *= weight_of(L);
             store_four<T>(p.out, (size_t)seq * p.ld_out + (size_t)(kvh * p.group + r0 + row) * HD + col, acc[0], acc[1], acc[2], acc[3]);
         } else {
-            float* slot = p.slots + (((size_t)item * p.parts + part) * p.rows + row) * RS;
-            *reinterpret_cast<f32x4_t*>(slot + col) = acc;
-            if (col == 0) *reinterpret_cast<float2*>(slot + HD) = make_float2(mx, L);
+            *reinterpret_cast<f32x4_t*>(slots + row * RS + col) = acc;
+            if (col == 0) *reinterpret_cast<float2*>(slots + row * RS + HD) = make_float2(mx, L);
         }
     }
+}
+
+template <typename T, riftkv_dtype DT, int HD>
+__global__ void __launch_bounds__(64 * kWaves, 2)
+listed_kernel(RangeParams p, ListedPages where) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    ranges_body<T, DT, HD>(p, where, false, blockIdx.x, reinterpret_cast<float*>(lds));
+}
+
+// BY_ROWS: the prefix by prefix_body.
+template <typename T, riftkv_dtype DT, int HD, bool BY_ROWS>
+__global__ void __launch_bounds__(64 * kWaves, BY_ROWS && sizeof(T) == 4 ? 1 : 2)
+shared_kernel(RangeParams p, SharedPages where, PrefixParams f) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    const bool front = (int)blockIdx.x < p.front_wgs;
+    if constexpr (BY_ROWS)
+        if (front) {
+            prefix_body<T, DT, HD>(f, blockIdx.x, lds);
+            return;
+        }
+    ranges_body<T, DT, HD>(p, where, !BY_ROWS && front, front ? blockIdx.x : blockIdx.x - p.front_wgs, reinterpret_cast<float*>(lds));
 }
 
 // A query head a wave: lane k finds the weight of part k, then the parts' values are added up, PG of them side by side, as
 // many loads in flight as there are parts.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256)
-parts_kernel(RangeParams p, int64_t n) {
+parts_kernel(RangeParams p, int64_t first, int64_t n) {
     constexpr int RS = HD + 4, CV = HD / 4, PG = 64 / CV, U = 8;
     const int lane = threadIdx.x & 63;
-    const int64_t of = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // sequence and head
+    const int64_t of = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // sequence and head
     if (of >= n) return;
     const int heads = p.n_kv * p.group;
     const int64_t seq = of / heads;
@@ -340,6 +343,7 @@ RangeParams params_of(const riftkv_cache& c, const KvAttention& a) {
     p.pages = TilePages{static_cast<const unsigned char*>(c.k), static_cast<const unsigned char*>(c.v), c.k_scale, c.v_scale};
     p.status = a.status;
     p.slots = static_cast<float*>(a.workspace);
+    p.parts = 1;
     p.n_kv = c.n_kv_heads;
     p.group = a.n_heads / c.n_kv_heads;
     p.q_tiles = (p.group + 15) / 16;
@@ -350,33 +354,20 @@ RangeParams params_of(const riftkv_cache& c, const KvAttention& a) {
     return p;
 }
 
-constexpr int64_t kMostWorkgroups = ((1ll << 32) - 1) / 256;   // of a launch; more take several
+constexpr int64_t kMostWorkgroups = ((1ll << 32) - 1) / (64 * kWaves);   // of a launch; more take several
+constexpr int kMostSplit = 512;                                        // items times parts, where items are split
+constexpr int kPrefixWgs = 256;
 
-template <typename Where>
-hipError_t launch_ranges(const riftkv_cache& c, const KvAttention& a, RangeParams p, int64_t items, const Where& where, hipStream_t st) {
-    const size_t lds = (size_t)kWaves * p.rows * (c.head_dim + 4) * sizeof(float);
-    auto run = [&](auto t, auto dt, auto hd) {
-        using T = decltype(t);
-        const int64_t most = kMostWorkgroups / p.parts;
-        for (int64_t i = 0; i < items; i += most) {
-            p.item0 = (int)i;
-            hipLaunchKernelGGL((ranges_kernel<T, dt.value, hd.value, Where>), dim3((unsigned)((items - i < most ? items - i : most) * p.parts)),
-                               dim3(64 * kWaves), lds, st, p, where);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
-        if (Where::kFront || p.parts == 1) return hipSuccess;
-        const int64_t n = (int64_t)a.n_seq * a.n_heads;
-        hipLaunchKernelGGL((parts_kernel<T, hd.value>), dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, p, n);
-        return hipGetLastError();
-    };
+// run(row type, page type, head_dim)
+template <typename Run>
+hipError_t by_types(const riftkv_cache& c, bool bf16, Run run) {
     auto heads = [&](auto t, auto dt) {
         if (c.head_dim == 128) return run(t, dt, std::integral_constant<int, 128>{});
         return run(t, dt, std::integral_constant<int, 64>{});
     };
     auto types = [&](auto dt) {
         if constexpr (dt.value != RIFTKV_F32)
-            if (a.bf16) return heads(bf16_t{}, dt);
+            if (bf16) return heads(bf16_t{}, dt);
         return heads(float{}, dt);
     };
     switch (c.dt) {
@@ -388,49 +379,77 @@ hipError_t launch_ranges(const riftkv_cache& c, const KvAttention& a, RangeParam
     return hipErrorInvalidValue;
 }
 
-constexpr int kMostSplit = 512;   // items times parts, where items are split
+// launch(workgroups) for the items, as often as they need; the first time with the prefix' workgroups.
+template <typename Launch>
+hipError_t by_items(RangeParams& p, int64_t items, Launch launch) {
+    const int64_t most = (kMostWorkgroups - p.front_wgs) / p.parts;
+    for (int64_t i = 0; i < items; i += most) {
+        p.item0 = (int)i;
+        const hipError_t e = launch((unsigned)((items - i < most ? items - i : most) * p.parts + p.front_wgs));
+        if (e != hipSuccess) return e;
+        p.front_wgs = 0;
+    }
+    return hipSuccess;
+}
 
-// Parts of an item of at most `tiles` tiles: a split costs a launch, which pays for long items that are few.
+template <typename T, int HD>
+hipError_t join_parts(const KvAttention& a, const RangeParams& p, hipStream_t st) {
+    const int64_t n = (int64_t)a.n_seq * a.n_heads, most = kMostWorkgroups * 4;   // a wave each
+    for (int64_t i = 0; i < n; i += most) {
+        const int64_t m = n - i < most ? n - i : most;
+        hipLaunchKernelGGL((parts_kernel<T, HD>), dim3((unsigned)((m + 3) / 4)), dim3(256), 0, st, p, i, n);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// Parts of an item of at most `tiles` tiles, four of them at least a part.
 int parts_of(int64_t items, int64_t tiles) {
-    if (items > 128 || tiles < 24) return 1;
     const int64_t parts = kMostSplit / items < tiles / 4 ? kMostSplit / items : tiles / 4;
-    return parts > kMaxParts ? kMaxParts : (int)parts;
+    return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : (int)parts;
 }
 
 size_t part_bytes(const riftkv_cache& c) { return (size_t)(c.head_dim + 4) * sizeof(float); }
 
-// How the call of a prefix is made: its parts and those of the sequences' own tokens.
+// How the call of a prefix is made.
 struct SharedPlan {
-    bool by_rows;            // prefix_kernel
     int64_t rows, items;     // rows of a key head; items of the sequences' own tokens
-    int front_parts, parts;
+    bool walk, by_rows;      // the prefix by every sequence itself; by prefix_body
+    int front_parts, front_wgs, row_tiles, parts;
     SharedPlan(const riftkv_cache& c, int n_heads, int64_t n_seq, int prefix_len, int64_t max_pages) {
         const int group = n_heads / c.n_kv_heads;
+        const int64_t own = (max_pages * c.page_size + kTile - 1) / kTile;
         rows = n_seq * group;
         items = n_seq * c.n_kv_heads * ((group + 15) / 16);
-        by_rows = c.dt != RIFTKV_F32 && rows > 32;
-        front_parts = 0;
-        if (prefix_len > 0 && rows > 0) {
-            const int64_t tiles = (prefix_len + kTile - 1) / kTile;
-            if (by_rows) front_parts = prefix_parts(c.n_kv_heads, rows, prefix_len);
-            else {
-                const int64_t wgs = c.n_kv_heads * ((rows + 15) / 16);
-                const int64_t n = kMostSplit / wgs < tiles / 4 ? kMostSplit / wgs : tiles / 4;
-                front_parts = n < 1 ? 1 : n > kMaxParts ? kMaxParts : (int)n;
-            }
-        }
-        parts = items > 0 ? parts_of(items, (max_pages * c.page_size + kTile - 1) / kTile) : 1;
+        walk = prefix_len <= kWalked;
+        by_rows = !walk && c.dt != RIFTKV_F32 && rows > 32;
+        front_parts = front_wgs = 0;
+        row_tiles = (int)((rows + kRows - 1) / kRows);
+        parts = items > 128 || own < 24 ? 1 : parts_of(items, own);   // a split alone costs a launch, which pays for long items that are few
+        if (walk) return;
+        parts = parts_of(items, own);
+        const int64_t wgs = c.n_kv_heads * (by_rows ? row_tiles : (rows + 15) / 16);
+        if (by_rows) {
+            const int64_t tiles = (prefix_len + kTokens - 1) / kTokens;
+            int64_t n = kPrefixWgs / wgs;
+            if (n > tiles / 2) n = tiles / 2;
+            front_parts = n < 1 ? 1 : n > kMaxParts ? kMaxParts : (int)n;
+        } else front_parts = parts_of(wgs, (prefix_len + kTile - 1) / kTile);
+        front_wgs = (int)(wgs * front_parts);
     }
+    static constexpr int kWalked = 64;
 };
 
 }  // namespace
 
 size_t kv_shared_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, int prefix_len, int64_t) {
-    // The prefix' parts: rows of 128 for each of 512 workgroups, or one part of every row; fewer where rows and their parts
-    // are few.  Then those of the sequences' own tokens.
+    // The prefix' parts: 128 rows for each of its workgroups, or one part of every row; fewer where rows and their parts are
+    // few.  Those of the sequences' own tokens: one of every row (groups of more than 16 may leave some unused), or as many
+    // as where they are split.
     const int64_t group = n_heads / c.n_kv_heads, rows = n_seq * n_heads;
-    const int64_t split = rows * kMaxParts < 512 * 128 ? rows * kMaxParts : 512 * 128;
-    return ((prefix_len > 0 ? split + rows : 0) + kMostSplit * (group < 16 ? group : 16)) * part_bytes(c);
+    const int64_t split = rows * kMaxParts < kPrefixWgs * kRows ? rows * kMaxParts : kPrefixWgs * kRows;
+    return ((prefix_len > 0 ? split + 3 * rows : 0) + kMostSplit * (group < 16 ? group : 16)) * part_bytes(c);
 }
 
 size_t kv_listed_workspace(const riftkv_cache& c, int n_heads, int64_t, int) {
@@ -441,36 +460,55 @@ size_t kv_listed_workspace(const riftkv_cache& c, int n_heads, int64_t, int) {
 hipError_t launch_kv_attention_shared(const riftkv_cache& c, const KvAttention& a, const int* prefix_table, int prefix_len, hipStream_t st) {
     const SharedPlan plan(c, a.n_heads, a.n_seq, prefix_len, a.max_pages);
     RangeParams p = params_of(c, a);
-    p.front_rows = plan.rows;
-    if (plan.front_parts > 0) {
-        float* front = static_cast<float*>(a.workspace);
-        hipError_t e;
-        if (plan.by_rows) {
-            const PrefixParams f{a.q, a.ld_q, p.pages, prefix_table, a.status, front, prefix_len, p.n_kv, p.n_pages, p.shift, p.group,
-                                 (int)plan.rows, 0, plan.front_parts, p.scale_log2};
-            e = launch_prefix(c, a.bf16, f, st);
-        } else {
-            RangeParams f = p;
-            f.slots = front;
-            f.parts = plan.front_parts;
-            f.rows = plan.rows < 16 ? (int)plan.rows : 16;
-            const int pages = (int)(((int64_t)prefix_len + c.page_size - 1) / c.page_size);
-            e = launch_ranges(c, a, f, p.n_kv * ((plan.rows + 15) / 16), PrefixPages{OwnPages{prefix_table, nullptr, pages}, prefix_len}, st);
-        }
-        if (e != hipSuccess) return e;
-        p.front = front;
-        p.front_parts = plan.front_parts;
-        p.slots = front + (size_t)p.n_kv * plan.front_parts * plan.rows * (c.head_dim + 4);
-    }
     p.parts = plan.parts;
-    return launch_ranges(c, a, p, plan.items, WholePages{OwnPages{a.table, a.lens, a.max_pages}}, st);
+    p.front_rows = plan.rows;
+    p.front_parts = plan.front_parts;
+    p.front_wgs = plan.front_wgs;
+    p.front = static_cast<float*>(a.workspace);
+    p.slots = p.front + (size_t)p.n_kv * plan.front_parts * plan.rows * (c.head_dim + 4);
+    const int pages = (int)(((int64_t)prefix_len + c.page_size - 1) / c.page_size);
+    const SharedPages where{OwnPages{a.table, a.lens, a.max_pages}, OwnPages{prefix_table, nullptr, pages}, prefix_len, plan.walk ? prefix_len : 0};
+    const PrefixParams f{a.q, a.ld_q, p.pages, prefix_table, a.status, p.front, prefix_len, p.n_kv, p.n_pages, p.shift, p.group,
+                         (int)plan.rows, plan.row_tiles, plan.front_parts, p.scale_log2};
+    return by_types(c, a.bf16, [&](auto t, auto dt, auto hd) {
+        using T = decltype(t);
+        auto launch = [&](auto kernel, size_t lds) {
+            if (lds > 64 * 1024) {   // the attribute is the current device's
+                const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                if (e != hipSuccess) return e;
+            }
+            return by_items(p, plan.items, [&](unsigned wgs) {
+                hipLaunchKernelGGL(kernel, dim3(wgs), dim3(64 * kWaves), lds, st, p, where, f);
+                return hipGetLastError();
+            });
+        };
+        hipError_t e;
+        bool done = false;
+        if constexpr (dt.value != RIFTKV_F32)
+            if (plan.by_rows) {
+                e = launch(shared_kernel<T, dt.value, hd.value, true>, kPrefixLds);
+                done = true;
+            }
+        if (!done) e = launch(shared_kernel<T, dt.value, hd.value, false>, (size_t)kWaves * (plan.front_wgs > 0 ? 16 : p.rows) * (hd.value + 4) * sizeof(float));
+        if (e != hipSuccess || (plan.walk && p.parts == 1)) return e;
+        return join_parts<T, hd.value>(a, p, st);
+    });
 }
 
 hipError_t launch_kv_attention_pages(const riftkv_cache& c, const KvAttention& a, const int* lists, int top, hipStream_t st) {
     RangeParams p = params_of(c, a);
-    const int64_t items = (int64_t)a.n_seq * p.n_kv * p.q_tiles;
-    p.parts = parts_of(items, ((int64_t)top * c.page_size + kTile - 1) / kTile);
-    return launch_ranges(c, a, p, items, ListedPages{OwnPages{a.table, a.lens, a.max_pages}, lists, top}, st);
+    const int64_t items = (int64_t)a.n_seq * p.n_kv * p.q_tiles, tiles = ((int64_t)top * c.page_size + kTile - 1) / kTile;
+    if (items <= 128 && tiles >= 24) p.parts = parts_of(items, tiles);   // a split costs a launch, which pays for long items that are few
+    const ListedPages where{OwnPages{a.table, a.lens, a.max_pages}, lists, top};
+    const size_t lds = (size_t)kWaves * p.rows * (c.head_dim + 4) * sizeof(float);
+    return by_types(c, a.bf16, [&](auto t, auto dt, auto hd) {
+        using T = decltype(t);
+        const hipError_t e = by_items(p, items, [&](unsigned wgs) {
+            hipLaunchKernelGGL((listed_kernel<T, dt.value, hd.value>), dim3(wgs), dim3(64 * kWaves), lds, st, p, where);
+            return hipGetLastError();
+        });
+        return e != hipSuccess || p.parts == 1 ? e : join_parts<T, hd.value>(a, p, st);
+    });
 }
 
 }  // namespace rift
