@@ -10,8 +10,8 @@ from ._lib import (EXPORTS, LIB_PATH, RIFT_BF16, RIFT_F32, LayerWeights, ModelCf
                    rift_score_workspace_size,
                    rift_select_tokens, rift_set_debug, rift_split_budgets)
 from .kv import (KV_EXPORTS, RIFTKV_BF16, RIFTKV_F32, RIFTKV_FP8, RIFTKV_INT8, KvCache, riftkv_attention,  # noqa: F401
+                 riftkv_attention_pages, riftkv_attention_pages_workspace_size, riftkv_attention_shared,
+                 riftkv_attention_shared_workspace_size,
                  riftkv_attention_workspace_size, riftkv_cache, riftkv_decode_step, riftkv_decode_workspace_size,
-                 riftkv_read, riftkv_rope, riftkv_rope_axes, riftkv_rope_freqs, riftkv_write)
-from .kv_ranges import (riftkv_attention_pages, riftkv_attention_pages_workspace_size, riftkv_attention_shared,  # noqa: F401
-                        riftkv_attention_shared_workspace_size, riftkv_page_bounds, riftkv_select_pages,
-                        riftkv_select_pages_workspace_size)
+                 riftkv_page_bounds, riftkv_read, riftkv_rope, riftkv_rope_axes, riftkv_rope_freqs, riftkv_select_pages,
+                 riftkv_select_pages_workspace_size, riftkv_write)

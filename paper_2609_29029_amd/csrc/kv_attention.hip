@@ -75,17 +75,6 @@ __device__ __forceinline__ unsigned long long quotient(unsigned long long a, uns
     return ((a | b) >> 32) == 0 ? (unsigned)a / (unsigned)b : a / b;
 }
 
-// Inclusive sums over the wave.
-__device__ __forceinline__ int wave_scan(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast 15 into rows 1 and 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast 31 into rows 2 and 3
-    return x;
-}
-
 // How N tiles are dealt to W waves (W <= N): wave w's run begins at w q + min(w, r).
 struct Deal {
     unsigned long long q = 1, r = 0;

@@ -347,15 +347,17 @@ scores_kernel(SelectParams p) {
     }
 }
 
-// A workgroup takes a key head of a sequence, a thread a run of its pages: the key of the last page to take, eight bits of it at
-// a time from the first that differs between pages, then the list.
+// A workgroup takes a key head of a sequence, a thread a run of its pages: the key of the last page to take, eleven bits of it
+// at a time from the first that differs between pages (so that few pages are left in a bucket of the first time, often the
+// one that is looked for), then the list.
 constexpr int kPickThreads = 512, kHeldKeys = 8;   // keys that a thread keeps in registers
+constexpr int kBucketBits = 11, kBuckets = 1 << kBucketBits;
 
 __global__ void __launch_bounds__(kPickThreads)
 pick_kernel(SelectParams p) {
     constexpr int WAVES = kPickThreads / 64;
-    __shared__ int counts[256];
-    __shared__ unsigned long long least_of[WAVES], most_of[WAVES];
+    __shared__ __align__(16) int counts[kBuckets];
+    __shared__ uint2 ends_of[WAVES];                // largest of the keys' upper words, and of their complements
     __shared__ int sums[WAVES][2];
     __shared__ int found, above, inside;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -405,94 +407,84 @@ pick_kernel(SelectParams p) {
             for (int i = i0; i < i1; ++i) f(keys[i], i);
         }
     };
-    unsigned long long lowest = ~0ull, highest = 0;
+    uint32_t highest = 0, complement = 0;
     each([&](unsigned long long k, int) {
-        lowest = min(lowest, k);
-        highest = max(highest, k);
+        highest = max(highest, (uint32_t)(k >> 32));
+        complement = max(complement, ~(uint32_t)(k >> 32));
     });
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        lowest = min(lowest, (unsigned long long)__shfl_xor(lowest, d));
-        highest = max(highest, (unsigned long long)__shfl_xor(highest, d));
-    }
-    if (lane == 0) {
-        least_of[wave] = lowest;
-        most_of[wave] = highest;
-    }
+    highest = wave_most(highest);
+    complement = wave_most(complement);
+    if (lane == 0) ends_of[wave] = make_uint2(highest, complement);
+    for (int i = tid; i < kBuckets; i += kPickThreads) counts[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        lowest = min(lowest, least_of[w]);
-        highest = max(highest, most_of[w]);
+        highest = max(highest, ends_of[w].x);
+        complement = max(complement, ends_of[w].y);
     }
-    // Keys of a bucket share the bits from `bit` on; those of higher buckets are all taken.
-    int bit = lowest == highest ? 0 : max(0, 64 - __clzll(lowest ^ highest) - 8);
-    unsigned long long bucket = highest >> bit;
-    int width = 256;
-    if (lowest == highest) need = min(need, n);
-    else
-        for (;;) {
-            const unsigned long long base = bucket & ~(unsigned long long)(width - 1);   // the first of the buckets looked at
-            if (tid < 256) counts[tid] = 0;
-            __syncthreads();
-            each([&](unsigned long long k, int) {
-                const unsigned long long in = (k >> bit) - base;
-                if (in < (unsigned long long)width) atomicAdd(&counts[in], 1);
-            });
-            __syncthreads();
-            if (wave == 0) {
-                // four buckets a lane, the highest first
-                int c[4], sum = 0;
+    // Keys of a bucket share the bits from `bit` on; those of higher buckets are all taken.  Upper words that are all alike: from
+    // the lower ones on.
+    const uint32_t differ = highest ^ ~complement;
+    int bit = (differ == 0 ? 32 : 64 - __clz(differ)) - kBucketBits;
+    unsigned long long bucket = ((unsigned long long)highest << 32) >> bit;
+    int width = kBuckets;
+    for (;;) {
+        const unsigned long long base = bucket & ~(unsigned long long)(width - 1);   // the first of the buckets looked at
+        each([&](unsigned long long k, int) {
+            const unsigned long long in = (k >> bit) - base;
+            if (in < (unsigned long long)width) atomicAdd(&counts[in], 1);
+        });
+        __syncthreads();
+        if (wave == 0) {
+            // a run of buckets a lane, the highest first
+            constexpr int RUN = kBuckets / 64;
+            int c[RUN], sum = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    c[i] = counts[255 - 4 * lane - i];
-                    sum += c[i];
-                }
-                int incl = sum;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int o = __shfl_up(incl, d);
-                    if (lane >= d) incl += o;
-                }
-                int before = incl - sum;
-                if (before < need && need <= incl) {
-                    int i = 0;
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        if (i == k && before + c[k] < need) {
-                            before += c[k];
-                            ++i;
-                        }
-                    found = 255 - 4 * lane - i;
-                    above = before;
-                    inside = i == 0 ? c[0] : i == 1 ? c[1] : i == 2 ? c[2] : c[3];
-                }
+            for (int i = 0; i < RUN; i += 4) {
+                const int4 x = *reinterpret_cast<const int4*>(counts + kBuckets - RUN * (lane + 1) + i);
+                c[RUN - 1 - i] = x.x;
+                c[RUN - 2 - i] = x.y;
+                c[RUN - 3 - i] = x.z;
+                c[RUN - 4 - i] = x.w;
+                sum += x.x + x.y + x.z + x.w;
             }
-            __syncthreads();
-            bucket = base + found;
-            need -= above;
-            if (bit == 0 || inside == need) break;
-            width = bit < 8 ? 1 << bit : 256;
-            const int step = bit < 8 ? bit : 8;
-            bit -= step;
-            bucket <<= step;
-            __syncthreads();
+            const int incl = wave_scan(sum);
+            int before = incl - sum, at = 0, in = 0;
+            if (before < need && need <= incl) {
+                bool past = false;
+#pragma unroll
+                for (int i = 0; i < RUN; ++i) {
+                    if (!past && before + c[i] >= need) {
+                        past = true;
+                        at = i;
+                        in = c[i];
+                    }
+                    if (!past) before += c[i];
+                }
+                found = kBuckets - 1 - RUN * lane - at;
+                above = before;
+                inside = in;
+            }
         }
+        __syncthreads();
+        bucket = base + found;
+        need -= above;
+        if (bit == 0 || inside == need) break;
+        const int step = min(bit, kBucketBits);
+        width = 1 << step;
+        bit -= step;
+        bucket <<= step;
+        __syncthreads();            // (found, above and inside have been read)
+        for (int i = tid; i < kBuckets; i += kPickThreads) counts[i] = 0;
+        __syncthreads();
+    }
     // places in the list: of the pages above, and of the bucket's first ones
     int higher = 0, equal = 0;
     each([&](unsigned long long k, int) {
         higher += (k >> bit) > bucket;
         equal += (k >> bit) == bucket;
     });
-    int hi_incl = higher, eq_incl = equal;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int a = __shfl_up(hi_incl, d), b = __shfl_up(eq_incl, d);
-        if (lane >= d) {
-            hi_incl += a;
-            eq_incl += b;
-        }
-    }
+    const int hi_incl = wave_scan(higher), eq_incl = wave_scan(equal);
     if (lane == 63) {
         sums[wave][0] = hi_incl;
         sums[wave][1] = eq_incl;

@@ -302,7 +302,8 @@ parts_kernel(RangeParams p, int64_t first, int64_t n) {
     f32x4_t x[U];
     auto load = [&](const Set& set, int k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const f32x4_t*>(set.at + min(k0 + u * PG + pg, set.n - 1) * set.next + col);
+        for (int u = 0; u < U; ++u)
+            if (k0 + u * PG < set.n) x[u] = *reinterpret_cast<const f32x4_t*>(set.at + min(k0 + u * PG + pg, set.n - 1) * set.next + col);
     };
     load(sets[0], 0);
     float mx = fmaxf(ml[0].x, ml[1].x);
@@ -356,7 +357,7 @@ RangeParams params_of(const riftkv_cache& c, const KvAttention& a) {
 
 constexpr int64_t kMostWorkgroups = ((1ll << 32) - 1) / (64 * kWaves);   // of a launch; more take several
 constexpr int kMostSplit = 512;                                        // items times parts, where items are split
-constexpr int kPrefixWgs = 256;
+constexpr int kMostPrefixWgs = 384;
 
 // run(row type, page type, head_dim)
 template <typename Run>
@@ -432,13 +433,19 @@ struct SharedPlan {
         const int64_t wgs = c.n_kv_heads * (by_rows ? row_tiles : (rows + 15) / 16);
         if (by_rows) {
             const int64_t tiles = (prefix_len + kTokens - 1) / kTokens;
-            int64_t n = kPrefixWgs / wgs;
+            // A workgroup a CU, so that the sequences' own tokens have the other half of it; more where a tile has few bytes or
+            // is widened (64 sequences after 32,768 tokens, groups of 4, with 256 and 384: bf16 73.5 and 74.4 us, 8,192 tokens in
+            // groups of 1 22.4 and 24.9; e4m3 90.6 and 84.1; 64 dimensions 57.3 and 53.9).
+            int64_t n = (c.dt == RIFTKV_BF16 && c.head_dim == 128 ? 256 : kMostPrefixWgs) / wgs;
             if (n > tiles / 2) n = tiles / 2;
             front_parts = n < 1 ? 1 : n > kMaxParts ? kMaxParts : (int)n;
         } else front_parts = parts_of(wgs, (prefix_len + kTile - 1) / kTile);
         front_wgs = (int)(wgs * front_parts);
     }
-    static constexpr int kWalked = 64;
+    // Tokens of a prefix that every sequence walks itself, walked / in workgroups of its own: 100 sequences of 96 to 608 tokens
+    // and 32 heads 92 / 100 us (65 tokens), 101 / 103 (200), 109 / 103 (300); 64 of 1 to 300 in groups of 4 11.7 / 18.6 (65),
+    // 13.8 / 18.9 (200), 15.2 / 19.0 (300); 8 of them 10.1 / 10.6 (256), 13.0 / 11.0 (500).
+    static constexpr int kWalked = 256;
 };
 
 }  // namespace
@@ -448,7 +455,7 @@ size_t kv_shared_workspace(const riftkv_cache& c, int n_heads, int64_t n_seq, in
     // few.  Those of the sequences' own tokens: one of every row (groups of more than 16 may leave some unused), or as many
     // as where they are split.
     const int64_t group = n_heads / c.n_kv_heads, rows = n_seq * n_heads;
-    const int64_t split = rows * kMaxParts < kPrefixWgs * kRows ? rows * kMaxParts : kPrefixWgs * kRows;
+    const int64_t split = rows * kMaxParts < kMostPrefixWgs * kRows ? rows * kMaxParts : kMostPrefixWgs * kRows;
     return ((prefix_len > 0 ? split + 3 * rows : 0) + kMostSplit * (group < 16 ? group : 16)) * part_bytes(c);
 }
 

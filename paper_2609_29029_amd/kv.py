@@ -36,13 +36,15 @@ class _RopeStruct(ctypes.Structure):
 
 _lib: Optional[ctypes.CDLL] = None
 # Set by the first call: importing the package does not import torch.
-torch = _ROWS = _STORES = _I32 = _U8 = _device = _raw_stream = None
+torch = _ROWS = _STORES = _I32 = _U8 = _F8 = _I4 = _device = _raw_stream = None
 
 
 def _load() -> ctypes.CDLL:
-    global _lib, torch, _ROWS, _STORES, _I32, _U8, _device, _raw_stream
+    global _lib, torch, _ROWS, _STORES, _I32, _U8, _F8, _I4, _device, _raw_stream
     if _lib is None:
+        import numpy as np
         import torch as t
+        _F8, _I4 = np.dtype("<f8"), np.dtype("<i4")
         torch, _I32, _U8 = t, t.int32, t.uint8
         _device, _raw_stream = t._C._cuda_getDevice, t._C._cuda_getCurrentRawStream
         _ROWS = {t.bfloat16: RIFT_BF16, t.float32: RIFT_F32}
@@ -204,6 +206,15 @@ def riftkv_rope_freqs(rotary_dim: int, base: float = 10000.0, scaling: str = "no
     return out, float(mag.value)
 
 
+def _rope_rows(t, dtype, rows, heads, hd, dev, name):
+    """_rows, for rows whose strides are as they mostly are."""
+    if t.dtype is dtype and t.shape == (rows, heads, hd) and t.get_device() == dev:
+        ld, sh, se = t.stride()
+        if se == 1 and sh == hd and rows > 1:
+            return t.data_ptr(), ld
+    return _rows(t, dtype, (rows, heads, hd), dev, name)
+
+
 def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, stream, axes=None):
     x = q if q is not None else k
     if x is None:
@@ -218,24 +229,22 @@ def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, str
     pq = lq = nq = poq = loq = pk = lk = nk = pok = lok = 0
     if q is not None:
         nq = x.shape[1]
-        shape = (rows, nq, hd)
-        pq, lq = _rows(q, dtype, shape, dev, "q")
-        poq, loq = (pq, lq) if q_out is None else _rows(q_out, dtype, shape, dev, "q_out")
+        pq, lq = _rope_rows(q, dtype, rows, nq, hd, dev, "q")
+        poq, loq = (pq, lq) if q_out is None else _rope_rows(q_out, dtype, rows, nq, hd, dev, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
     if k is not None:
         if k.dim() != 3:
             raise ValueError("rows: expected [rows][heads][head_dim]")
         nk = k.shape[1]
-        shape = (rows, nk, hd)
-        pk, lk = _rows(k, dtype, shape, dev, "k")
-        pok, lok = (pk, lk) if k_out is None else _rows(k_out, dtype, shape, dev, "k_out")
+        pk, lk = _rope_rows(k, dtype, rows, nk, hd, dev, "k")
+        pok, lok = (pk, lk) if k_out is None else _rope_rows(k_out, dtype, rows, nk, hd, dev, "k_out")
     elif k_out is not None:
         raise ValueError("k_out without k")
     lay = ROPE_LAYOUTS.get(layout)
     if lay is None:
         raise ValueError(f"layout: one of {tuple(ROPE_LAYOUTS)}")
-    fp = _host(freqs, "<f8", ctypes.c_double, "freqs: expected a contiguous float64 array")
+    fp = _host(freqs, _F8, ctypes.c_double, "freqs: expected a contiguous float64 array")
     if axes is None:
         shape, places, by_axis = (rows,), (rows,), ()
     else:
@@ -243,7 +252,7 @@ def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, str
             raise ValueError("axes: expected as many as freqs")
         shape = (positions.shape[0], rows)
         places = shape
-        by_axis = (_host(axes, "<i4", ctypes.c_int32, "axes: expected a contiguous int32 array"),)
+        by_axis = (_host(axes, _I4, ctypes.c_int32, "axes: expected a contiguous int32 array"),)
     if positions.dtype is not _I32 or positions.shape != shape or not positions.is_contiguous() or positions.get_device() != dev:
         _dense(positions, _I32, shape, dev, "positions")
     st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
@@ -254,12 +263,16 @@ def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, str
         _check(st, name)
 
 
-def _host(a, kind, ctype, what):
+def _host(a, dtype, ctype, what):
     """Address of a numpy array (its own .ctypes takes three times as long)."""
-    flags = a.flags
-    if a.dtype.str != kind or not flags.c_contiguous or a.size == 0:
+    if a.dtype is dtype:
+        try:
+            return ctypes.byref(ctype.from_buffer(a))
+        except (TypeError, ValueError, BufferError):   # not writeable, or not what it has to be
+            pass
+    if a.dtype.str != dtype.str or not a.flags.c_contiguous or a.size == 0:
         raise TypeError(what)
-    return ctypes.byref(ctype.from_buffer(a)) if flags.writeable else a.ctypes.data
+    return a.ctypes.data
 
 
 def riftkv_rope(q, k, positions, freqs, q_out=None, k_out=None, layout: str = "half", magnitude: float = 1.0,
@@ -376,6 +389,140 @@ def riftkv_attention(cache: KvCache, q, page_table, lens, out, workspace, status
     st = _lib.riftkv_attention(*args) if dev == _device() else _elsewhere(dev, _lib.riftkv_attention, *args)
     if st:
         _check(st, "riftkv_attention")
+
+
+# ----------------------------------------------------------------------------- ranges of pages
+def _queries(cache, q, page_table, lens, status):
+    """What the calls below check alike: (device, row type, sequences, the table's width, q's address and stride)."""
+    dev, hd, dtype, i32 = cache.device, cache.head_dim, q.dtype, _I32
+    n_seq, max_pages = page_table.shape
+    dt = _ROWS.get(dtype)
+    if dt is None:
+        _row_type(q, "q")
+    n, n_heads, width = q.shape
+    pq = q.data_ptr()
+    ldq, sh, se = q.stride()
+    if n != n_seq or width != hd or q.get_device() != dev or se != 1 or sh != hd:
+        pq, ldq = _rows(q, dtype, (n_seq, n_heads, hd), dev, "q")
+    elif n_seq < 2:
+        ldq = n_heads * hd
+    if page_table.dtype is not i32 or not page_table.is_contiguous() or page_table.get_device() != dev:
+        _dense(page_table, i32, None, dev, "page_table")
+    if lens.dtype is not i32 or lens.shape != (n_seq,) or not lens.is_contiguous() or lens.get_device() != dev:
+        _dense(lens, i32, (n_seq,), dev, "lens")
+    if status.dtype is not i32 or status.shape != (1,) or status.get_device() != dev:
+        _dense(status, i32, (1,), dev, "status")
+    return dev, dt, n_seq, max_pages, n_heads, pq, ldq
+
+
+def _output(out, q, dev):
+    """Address and stride of rows like q's."""
+    shape = q.shape
+    ld, sh, se = out.stride()
+    if out.dtype is not q.dtype or out.shape != shape or out.get_device() != dev or se != 1 or sh != shape[2]:
+        return _rows(out, q.dtype, shape, dev, "out")
+    return out.data_ptr(), (ld if shape[0] > 1 else shape[1] * shape[2])
+
+
+def _space(workspace, dev):
+    if workspace.dtype is not _U8 or not workspace.is_contiguous() or workspace.get_device() != dev:
+        _dense(workspace, _U8, None, dev, "workspace")
+    return workspace.data_ptr()
+
+
+def _lists(cache, pages, n_seq, dev):
+    shape = pages.shape
+    if len(shape) != 3:
+        raise ValueError("pages: expected [n_seq][n_kv_heads][top]")
+    if shape[0] != n_seq or shape[1] != cache.n_kv_heads or pages.dtype is not _I32 or not pages.is_contiguous() or pages.get_device() != dev:
+        _dense(pages, _I32, (n_seq, cache.n_kv_heads, shape[2]), dev, "pages")
+    return pages.data_ptr(), shape[2]
+
+
+def _bounds(cache, bounds):
+    """Address of the pages' bounds."""
+    return _dense(bounds, torch.float32 if cache.dt == RIFTKV_F32 else torch.bfloat16,
+                  (cache.n_pages, cache.n_kv_heads, 2, cache.head_dim), cache.device, "bounds")
+
+
+def riftkv_attention_shared_workspace_size(cache: KvCache, n_seq: int, n_heads: int, prefix_len: int, max_pages: int) -> int:
+    return int(_lib.riftkv_attention_shared_workspace_size(cache.ref, int(n_heads), int(n_seq), int(prefix_len), int(max_pages)))
+
+
+def riftkv_attention_shared(cache: KvCache, q, prefix_table, prefix_len: int, page_table, lens, out, workspace, status,
+                            scale: Optional[float] = None, stream=None) -> None:
+    """out[i] := attention of q[i] [n_heads][head_dim] over the prefix_len tokens of the pages prefix_table [pages] i32
+    and then the first lens[i] tokens of sequence i's own pages; scale None: 1 / sqrt(head_dim)."""
+    dev, dt, n_seq, max_pages, n_heads, pq, ldq = _queries(cache, q, page_table, lens, status)
+    if prefix_table.dtype is not _I32 or not prefix_table.is_contiguous() or prefix_table.get_device() != dev:
+        _dense(prefix_table, _I32, None, dev, "prefix_table")
+    if prefix_table.dim() != 1 or prefix_table.shape[0] * cache.page_size < prefix_len:
+        raise ValueError("prefix_table: expected the pages of prefix_len tokens")
+    po, ldo = _output(out, q, dev)
+    ws = _space(workspace, dev)
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (cache.ref, pq, ldq, n_heads, dt, prefix_table.data_ptr(), prefix_len, page_table.data_ptr(), n_seq, max_pages,
+            lens.data_ptr(), cache.head_dim ** -0.5 if scale is None else scale, po, ldo, status.data_ptr(), ws, workspace.numel(), st)
+    st = _lib.riftkv_attention_shared(*args) if dev == _device() else _elsewhere(dev, _lib.riftkv_attention_shared, *args)
+    if st:
+        _check(st, "riftkv_attention_shared")
+
+
+def riftkv_page_bounds(cache: KvCache, bounds, page_table, lens, status, begins=None, stream=None) -> None:
+    """bounds [n_pages][n_kv_heads][2][head_dim] (float32 with float32 pages, else bf16) := the smallest and largest key values
+    of the pages that hold tokens begins[i] (None: 0) .. lens[i] - 1 of every sequence."""
+    dev, i32 = cache.device, _I32
+    n_seq, max_pages = page_table.shape
+    to = _bounds(cache, bounds)
+    table = _dense(page_table, i32, None, dev, "page_table")
+    n = _dense(lens, i32, (n_seq,), dev, "lens")
+    first = None if begins is None else _dense(begins, i32, (n_seq,), dev, "begins")
+    word = _dense(status, i32, (1,), dev, "status")
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (cache.ref, to, table, n_seq, max_pages, first, n, word, st)
+    st = _lib.riftkv_page_bounds(*args) if dev == _device() else _elsewhere(dev, _lib.riftkv_page_bounds, *args)
+    if st:
+        _check(st, "riftkv_page_bounds")
+
+
+def riftkv_select_pages_workspace_size(cache: KvCache, n_seq: int, max_pages: int) -> int:
+    return int(_lib.riftkv_select_pages_workspace_size(cache.ref, int(n_seq), int(max_pages)))
+
+
+def riftkv_select_pages(cache: KvCache, bounds, q, page_table, lens, pages, workspace, status, keep_first: int = 1,
+                        keep_last: int = 1, stream=None) -> None:
+    """pages [n_seq][n_kv_heads][top] i32 := the places in its row of page_table of the `top` pages that each sequence's
+    token needs most of each key head, ascending, -1 behind them; the first keep_first and last keep_last always."""
+    dev, dt, n_seq, max_pages, n_heads, pq, ldq = _queries(cache, q, page_table, lens, status)
+    of = _bounds(cache, bounds)
+    to, top = _lists(cache, pages, n_seq, dev)
+    ws = _space(workspace, dev)
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (cache.ref, of, pq, ldq, n_heads, dt, page_table.data_ptr(), n_seq, max_pages, lens.data_ptr(), keep_first, keep_last, to,
+            top, status.data_ptr(), ws, workspace.numel(), st)
+    st = _lib.riftkv_select_pages(*args) if dev == _device() else _elsewhere(dev, _lib.riftkv_select_pages, *args)
+    if st:
+        _check(st, "riftkv_select_pages")
+
+
+def riftkv_attention_pages_workspace_size(cache: KvCache, n_seq: int, n_heads: int, top: int) -> int:
+    return int(_lib.riftkv_attention_pages_workspace_size(cache.ref, int(n_heads), int(n_seq), int(top)))
+
+
+def riftkv_attention_pages(cache: KvCache, q, page_table, lens, pages, out, workspace, status, scale: Optional[float] = None,
+                           stream=None) -> None:
+    """out[i] := attention of q[i] [n_heads][head_dim] over the tokens before lens[i] of the pages listed for it:
+    pages [n_seq][n_kv_heads][top] i32, places in sequence i's row of page_table; scale None: 1 / sqrt(head_dim)."""
+    dev, dt, n_seq, max_pages, n_heads, pq, ldq = _queries(cache, q, page_table, lens, status)
+    of, top = _lists(cache, pages, n_seq, dev)
+    po, ldo = _output(out, q, dev)
+    ws = _space(workspace, dev)
+    st = _raw_stream(dev) or None if stream is None else _stream(stream, dev)
+    args = (cache.ref, pq, ldq, n_heads, dt, page_table.data_ptr(), n_seq, max_pages, lens.data_ptr(), of, top,
+            cache.head_dim ** -0.5 if scale is None else scale, po, ldo, status.data_ptr(), ws, workspace.numel(), st)
+    st = _lib.riftkv_attention_pages(*args) if dev == _device() else _elsewhere(dev, _lib.riftkv_attention_pages, *args)
+    if st:
+        _check(st, "riftkv_attention_pages")
 
 
 # ----------------------------------------------------------------------------- decode
