@@ -233,8 +233,9 @@ RIFT_API size_t riftkv_attention_shared_workspace_size(const riftkv_cache* cache
  * prefix_len   [host] tokens of the prefix, >= 0
  * lens         [n_seq] i32 in [0, max_pages * page_size], the prefix not counted
  * A page of the prefix outside [0, n_pages) sets the status and makes every sequence's output NaN; a sequence
- * without any token gives zeros.  Everything else as for riftkv_attention.
- * Shape rules: prefix_len <= 2^30.
+ * without any token gives zeros.  With bf16 queries a weight of the prefix goes into the product with the values short
+ * by up to 2^-17 of it.  Everything else as for riftkv_attention.
+ * Shape rules: prefix_len <= 2^30, n_seq * n_heads <= 2^26.
  */
 RIFT_API rift_status riftkv_attention_shared(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads,
                                              rift_dtype dt, const int32_t* prefix_table, int32_t prefix_len,
@@ -256,7 +257,7 @@ RIFT_API rift_status riftkv_attention_shared(const riftkv_cache* cache, const vo
  * to bf16; NaN among an element's values makes both its bounds NaN.
  * Where sequences share a page that is not full for all of them, its bounds are one of theirs, or parts of several.
  * A length out of range, or a page outside [0, n_pages), sets the status and is skipped.
- * Shape rules: n_seq, max_pages >= 0, max_pages * page_size <= 2^30.
+ * Shape rules: 0 <= n_seq <= 65535, max_pages >= 0, max_pages * page_size <= 2^30.
  */
 RIFT_API rift_status riftkv_page_bounds(const riftkv_cache* cache, void* bounds, const int32_t* page_table, int32_t n_seq,
                                         int32_t max_pages, const int32_t* begins, const int32_t* lens, int32_t* status,

@@ -268,8 +268,10 @@ rift_status check_out(const riftkv_cache& c, const void* out, int64_t ld_out, in
     return check_rows(out, ld_out, (int64_t)n_heads * c.head_dim, dt) ? RIFT_OK : RIFT_ERR_SHAPE;
 }
 
+constexpr int64_t kMostRows = 1 << 26;   // of a prefix: their workgroups fit a launch
 bool shared_shape(const riftkv_cache& c, int32_t n_heads, int32_t n_seq, int32_t prefix_len, int32_t max_pages) {
-    return attention_shape(c, n_heads, n_seq, max_pages) && prefix_len >= 0 && prefix_len <= kMaxTokens;
+    return attention_shape(c, n_heads, n_seq, max_pages) && prefix_len >= 0 && prefix_len <= kMaxTokens &&
+           (int64_t)n_seq * n_heads <= kMostRows;
 }
 
 constexpr int32_t kMostListed = 1 << 20;
@@ -309,7 +311,7 @@ rift_status riftkv_page_bounds(const riftkv_cache* cache, void* bounds, const in
                                const int32_t* begins, const int32_t* lens, int32_t* status, rift_stream stream) {
     const rift_status cs = kv_check_cache(cache, true);
     if (cs != RIFT_OK) return cs;
-    if (!check_table(*cache, n_seq, max_pages)) return RIFT_ERR_SHAPE;
+    if (!check_table(*cache, n_seq, max_pages) || n_seq > 65535) return RIFT_ERR_SHAPE;
     if (status == nullptr) return RIFT_ERR_NULL;
     if (n_seq == 0) return RIFT_OK;
     if (bounds == nullptr || lens == nullptr || (page_table == nullptr && max_pages > 0)) return RIFT_ERR_NULL;

@@ -335,21 +335,30 @@ __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, un
     // while the matrix cores work on a piece of the products.
     auto half = [&](int tn, int kn, f32x16_t& sn, int tv, int kv, const u32x4_t(&pv)[2][NP], int ts, int ks, f32x16_t& s, u32x4_t(&pf)[2][NP])
         __attribute__((always_inline)) {
-        bf16x8_t kf = key_at(tn, kn, 0);
-        u32x4_t vv = value_at(tv, kv, 0, 0);
+        constexpr int NV = 2 * NT;
+        bf16x8_t kf[NK];
+        u32x4_t vv[NV];
         float f = 1.f, neg_ref = 0.f;
+        // The operands of piece j, a piece ahead (two ahead: the same, and 8-bit pages run out of registers): the scores' k0, the
+        // values' v0, where it has one.
+        auto ask = [&](int j) __attribute__((always_inline)) {
+            const int k0 = j * NK / 8, k1 = (j + 1) * NK / 8, v0 = j * NV / 8, v1 = (j + 1) * NV / 8;
+            if (k1 > k0) kf[k0] = key_at(tn, kn, k0);
+            if (v1 > v0) vv[v0] = value_at(tv, kv, v0 / NT, v0 % NT);
+        };
 #pragma unroll
         for (int i = 0; i < 16; ++i) sn[i] = 0.f;
+        ask(0);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            constexpr int NV = 2 * NT;
-            const int k0 = j * NK / 8, k1 = (j + 1) * NK / 8, v0 = j * NV / 8, v1 = (j + 1) * NV / 8;   // (a piece has one of each or none)
+            const int k0 = j * NK / 8, k1 = (j + 1) * NK / 8, v0 = j * NV / 8, v1 = (j + 1) * NV / 8;
             // A product of the matrix cores holds the next one up: between two of them stands what the vector unit can do, and the
             // empty asm keeps it there.
-            bf16x8_t kf_now = kf;
-            u32x4_t vv_now = vv;
-            if (k1 > k0 && k1 < NK) kf = key_at(tn, kn, k1);
-            if (v1 > v0 && v1 < NV) vv = value_at(tv, kv, v1 / NT, v1 % NT);
+            if (j < 7) ask(j + 1);
+            bf16x8_t kf_now{};
+            u32x4_t vv_now{};
+            if (k1 > k0) kf_now = kf[k0];
+            if (v1 > v0) vv_now = vv[v0];
             hold(kf_now);
             if (k1 > k0) score(kf_now, k0, sn);
             if (j == 0) {

@@ -39,10 +39,15 @@ def shared(R, P, q, prefix_len, lens, out=None, scale=None, stream=None, ws=None
 
 
 def check_shared(P, q, prefix_len, lens, out, scale=None):
+    """Of bf16 queries the prefix' weights are short by up to 2^-17: of each of their values' magnitudes."""
     kp, vp = P.rows(0, prefix_len)
     for i, n in enumerate(lens):
         k, v = P.rows(1 + i, n)
-        o, e = attend(q[i].double().cpu(), torch.cat((kp, k)), torch.cat((vp, v)), q.shape[2] ** -0.5 if scale is None else scale)
+        keys, values, qd = torch.cat((kp, k)), torch.cat((vp, v)), q[i].double().cpu()
+        scaled = q.shape[2] ** -0.5 if scale is None else scale
+        o, e = attend(qd, keys, values, scaled)
+        if q.dtype == torch.bfloat16:
+            e = e + 2.0 ** -17 * attend(qd, keys, values.abs(), scaled)[0]
         check(out[i], o, e, q.dtype, f"sequence {i}")
 
 
@@ -330,6 +335,33 @@ def test_values_that_are_not_numbers(R, value):
         for j in range(2):
             assert bool(torch.isnan(again[1, j]).all()) == bool(nan[j])
         assert torch.equal(again[0], out[0]) and torch.equal(again[2], out[2])
+
+
+@pytest.mark.parametrize("store", ["fp8", "int8"])
+@pytest.mark.parametrize("prefix, seqs, group", [(60, 3, 2), (700, 3, 2), (700, 40, 2)])
+def test_rows_of_8_bits_that_hold_nan(R, store, prefix, seqs, group):
+    """Written as NaN: a key's makes its key head's outputs NaN, a value's too; the other key head keeps its bits."""
+    lens = [(5 * i) % 30 for i in range(seqs)]
+    P = filled(R, store, 2, 128, 16, [prefix] + lens, seed=9)
+    q = randn(4, seqs, 2 * group, 128)
+    good = shared(R, P, q, prefix, lens)
+    check_shared(P, q, prefix, lens, good)
+    lists = torch.arange(3, dtype=torch.int32).repeat(1, 2, 1)
+    one = filled(R, store, 2, 128, 16, [40], seed=3)
+    fine = listed(R, one, q[:1], [40], lists)
+    for which in (0, 1):
+        for pages, seq, n in ((P, 0, prefix), (one, 0, 40)):
+            kv = randn(6, 1, 2, 2, 128)
+            kv[0, which, 1, 77] = math.nan
+            saved = [None if x is None else x.clone() for x in (pages.k.view(torch.uint8), pages.v.view(torch.uint8), pages.ks, pages.vs)]
+            keep_k, keep_v = pages.rows(seq, n)
+            kv[0, 0, 0], kv[0, 1, 0] = keep_k[n - 9, 0].cuda(), keep_v[n - 9, 0].cuda()      # key head 0 as it was
+            pages.put(R, seq, kv[:, 0], kv[:, 1], first=n - 9)
+            out = shared(R, P, q, prefix, lens) if pages is P else listed(R, one, q[:1], [40], lists)
+            want = good if pages is P else fine
+            assert bool(torch.isnan(out[:, group:]).all()) and torch.equal(out[:, :group], want[:, :group])
+            for x, y in zip((pages.k.view(torch.uint8), pages.v.view(torch.uint8), pages.ks, pages.vs), saved):
+                x.copy_(y)
 
 
 def test_keys_of_minus_infinity(R):

@@ -27,6 +27,7 @@ def test_attention_shared_is_checked(L):  # noqa: F811
     for over in (dict(heads=6), dict(heads=0), dict(heads=4100), dict(n_seq=-1), dict(n_seq=65536), dict(pages=-1), dict(pages=(1 << 26) + 1),
                  dict(ldq=1016), dict(ldo=1028), dict(out=FAKE + 8), dict(q=FAKE + 4), dict(prefix=-1), dict(prefix=(1 << 30) + 1)):
         assert call(**over) == 2, over
+    assert call(heads=4096, ldq=1 << 20, ldo=1 << 20, n_seq=(1 << 14) + 1) == 2      # more rows than the prefix' workgroups take
     assert call(dt=3) == 3 and call(cache(dt=0, ks=None, vs=None)) == 3
     assert call(scale=float("nan")) == 7 and call(scale=float("inf")) == 7 and call(scale=3e38) == 7
     assert call(ws=FAKE + 16) == 5 and call(wsb=16) == 5
@@ -60,7 +61,7 @@ def test_page_bounds_is_checked(L):  # noqa: F811
     assert L.riftkv_page_bounds(None, *base.values(), None) == 1
     for over in (dict(bounds=None), dict(table=None), dict(lens=None), dict(status=None)):
         assert call(**over) == 1, over
-    for over in (dict(n_seq=-1), dict(pages=-1), dict(pages=(1 << 26) + 1), dict(bounds=FAKE + 8)):
+    for over in (dict(n_seq=-1), dict(n_seq=65536), dict(pages=-1), dict(pages=(1 << 26) + 1), dict(bounds=FAKE + 8)):
         assert call(**over) == 2, over
     assert call(n_seq=0, bounds=None, table=None, begins=None, lens=None) == 0
 
@@ -114,7 +115,7 @@ def test_workspaces_never_shrink(L):  # noqa: F811
                      lambda n, p: L.riftkv_attention_pages_workspace_size(r, heads, n, p + 1),
                      lambda n, p: L.riftkv_select_pages_workspace_size(r, n, p))
             for size in sizes:
-                for p in (0, 1, 7, 100, 20000):
+                for p in (0, 1, 7, 100, 255, 256, 257, 20000):
                     by_seq = [size(n, p) for n in (0, 1, 2, 3, 5, 7, 8, 9, 16, 31, 33, 50, 64, 65, 100, 127, 128, 129, 300, 5000, 65535)]
                     assert by_seq == sorted(by_seq) and by_seq[0] >= 256
                 for n in (1, 3, 20, 64, 1000):
