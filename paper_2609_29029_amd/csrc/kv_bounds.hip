@@ -216,13 +216,13 @@ __device__ __forceinline__ unsigned long long key_of(double x) {
     return x != x ? kNanKey : b < 0 ? ~(unsigned long long)b : (unsigned long long)b | 0x8000000000000000ull;
 }
 
-// Eight values
+// Eight values; of float32 four, and four `apart` elements on.
 template <typename BT>
 struct EightOf {
     u32x4_t w[sizeof(BT) / 2];
-    __device__ __forceinline__ void load(const void* p, size_t i) {
+    __device__ __forceinline__ void load(const void* p, size_t i, int apart) {
 #pragma unroll
-        for (int j = 0; j < (int)sizeof(BT) / 2; ++j) w[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(static_cast<const BT*>(p) + i) + j);
+        for (int j = 0; j < (int)sizeof(BT) / 2; ++j) w[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(static_cast<const BT*>(p) + i + j * apart));
     }
     __device__ __forceinline__ float at(int e) const {
         if constexpr (sizeof(BT) == 2) return e & 1 ? bf16_hi(w[0][e / 2]) : bf16_lo(w[0][e / 2]);
@@ -241,39 +241,37 @@ __device__ __forceinline__ unsigned long long dpp(unsigned long long x) {
     const int lo = __builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, false), hi = __builtin_amdgcn_mov_dpp((int)(x >> 32), CTRL, 0xf, 0xf, false);
     return ((unsigned long long)(unsigned)hi << 32) | (unsigned)lo;
 }
-// Lanes whose numbers differ in one bit only, or that mirror each other: partners of a step of a reduction.
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+// Lanes whose numbers differ in one bit; the lane eight or four on, among sixteen in a ring.
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kTurn8 = 0x128, kTurn4 = 0x124;
 
-// One step of a sum over lanes: of two partners each keeps one half of the values, the upper one (bit BIT of its number) the
-// second.
-template <int CTRL, int BIT, int HALF, int N>
-__device__ __forceinline__ void sum_step(double (&x)[N], int lane) {
-    const bool upper = lane & BIT;
-#pragma unroll
-    for (int e = 0; e < HALF; ++e) {
-        const double give = upper ? x[e] : x[HALF + e], keep = upper ? x[HALF + e] : x[e];
-        x[e] = keep + dpp<CTRL>(give);
-    }
-}
-
-// Scores.  HD / 8 lanes hold a page's bounds, eight elements each, and the same elements of four queries at a time.  A query's
-// negative and positive values go into two float64 multiply-adds an element, so that no product needs a choice.  A wave
-// takes ITERS loads of pages, so that as many sums as a page has lanes are under way, and adds them up over those lanes by
-// halves: one sum is left to each.  Float64, because float32 sums would order pages otherwise than the definition does.
+// Scores, on v_mfma_f64_4x4x4: four products of 4 pages x 4 elements and 4 elements x 4 queries.  In lane 16 k + 4 b + i (of the
+// right operand: 4 b + j) of product b is page i's (query j's) element k, in lane 16 i + 4 b + j of the result page i's sum for
+// query j.  A lane holds eight elements of a page's bounds, one for each of eight steps, which are the element k of product b:
+// the order of a sum is free.  128 dimensions take the four products for one group of four pages, 64 two products for each of
+// two.  Negative and positive query values are operands of their own, with the smallest and the largest keys, so that no
+// product needs a choice.  Float64, because float32 sums would order pages otherwise than the definition does.
+// NS: sets of four queries that share the bounds' conversions (groups of 8: 74.6 us with two, 80.8 with one).
 //
-// Between the bounds' bytes and the vector unit: of a wave's 16 pages of 128 dimensions 256 multiply-adds (5.1 cycles each,
-// measured) and 128 conversions (8.3).  48 contexts of 17 to 65,001 tokens, 32 heads in groups of 4, pages of 32: 200 MB in 59 us,
-// 3.4 TB/s.  The next loads ahead of the products, three waves a SIMD with half the loads, and 256 to 8,192 workgroups made no
-// difference; a page's key heads in workgroups next to each other 3 to 5%.
+// Between the bounds' bytes and the float64 unit, which has the products and the conversions: of a wave's 16 pages of 128
+// dimensions 64 products (18.7 cycles each, measured, the rate of as many multiply-adds) and 64 conversions (8.3).  48 contexts of 17
+// to 65,001 tokens, 32 heads in groups of 4, pages of 32: 200 MB, with the selection 52.4 us; 40 of loads alone.  Multiply-adds
+// with queries in registers of float32 took 66.7: their conversions, 15 exchanges of a sum's parts, and two waves a SIMD
+// instead of five.  256 to 8,192 workgroups: within 8%; a page's key heads in workgroups next to each other 3 to 5%; loads that
+// stay in the caches 58 (float32 bounds too, 32 bytes a lane, until each load took whole pieces of 64: 114 us, 94 now).
 constexpr int kQueries = 4;
 
-template <typename T, typename BT, int HD>
-__global__ void __launch_bounds__(kThreads, 2)
+template <typename T, typename BT, int HD, int NS>
+__global__ void __launch_bounds__(kThreads, NS == 1 ? 4 : 3)
 scores_kernel(SelectParams p) {
     constexpr int G = HD / 8, PW = 64 / G;           // lanes of a page, pages of a load
-    constexpr int ITERS = G / kQueries, PAGES = PW * ITERS;
+    constexpr int ITERS = G / 4, PAGES = PW * ITERS; // loads of a wave's turn: as many as products of a page
     constexpr int WAVES = kThreads / 64;
-    const int lane = threadIdx.x & 63, d0 = 8 * (lane % G), sub = lane / G;
+    const int lane = threadIdx.x & 63, k = lane >> 4, b = (lane >> 2) & 3;
+    // product of the page that this lane's bounds belong to, and first page of its group of four
+    const int part = HD == 128 ? b : b >> 1, group4 = HD == 128 ? 0 : 4 * (b & 1);
+    constexpr int APART = sizeof(BT) == 2 ? 4 : HD / 2;
+    const int d0 = (HD / 4 * k + 8 * part) / (sizeof(BT) / 2), sub = group4 + (lane & 3);   // its first element; its page of a load
+    const int got = group4 + k;                      // the page, of load `part`, whose sum it has in the end
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // a block of pages after the other, each with all key heads: what lies together in memory is read together
     const int of = blockIdx.x / p.n_kv, kvh = blockIdx.x - of * p.n_kv;
@@ -285,17 +283,17 @@ scores_kernel(SelectParams p) {
     const int* table = p.table + (size_t)seq * p.max_pages;
     unsigned long long* keys = p.keys + (size_t)item * p.max_pages;
     const T* q = static_cast<const T*>(p.q) + (size_t)seq * p.ld_q + (size_t)kvh * p.group * HD + d0;
-    float neg[kQueries][8], pos[kQueries][8];
+    double neg[NS][8], pos[NS][8];
     auto load_q = [&](int j0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kQueries; ++j) {         // past the last: it once more
+        for (int n = 0; n < NS; ++n) {               // past the last: it once more
             EightOf<T> x;
-            x.load(q, (size_t)min(j0 + j, p.group - 1) * HD);
+            x.load(q, (size_t)min(j0 + kQueries * n + (lane & 3), p.group - 1) * HD, APART);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float f = x.at(e);
-                neg[j][e] = f > 0.f ? 0.f : f;       // (NaN is in both)
-                pos[j][e] = f < 0.f ? 0.f : f;
+                neg[n][e] = f > 0.f ? 0.f : f;       // (NaN is in both)
+                pos[n][e] = f < 0.f ? 0.f : f;
             }
         }
     };
@@ -303,50 +301,60 @@ scores_kernel(SelectParams p) {
     const int64_t step = (int64_t)p.blocks * WAVES * PAGES;
     for (int64_t p0 = begin + (int64_t)(block * WAVES + wave) * PAGES; p0 < end; p0 += step) {
         EightOf<BT> lo[ITERS], hi[ITERS];
-        unsigned there = 0;                          // loads whose page is there
+        bool good = true;
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {            // past the last: it once more
             const int page = table[min((int)p0 + i * PW + sub, end - 1)];
             const bool is = (unsigned)page < (unsigned)p.n_pages;
-            there |= (unsigned)is << i;
+            const unsigned long long there = __ballot(is);
+            if (part == i) good = there >> got & 1;
             const size_t at = ((size_t)(is ? page : 0) * p.n_kv + kvh) * (2 * HD) + d0;
-            lo[i].load(p.bounds, at);
-            hi[i].load(p.bounds, at + HD);
+            lo[i].load(p.bounds, at, APART);
+            hi[i].load(p.bounds, at + HD, APART);
         }
         unsigned long long best = 0;
-        for (int j0 = 0; j0 < p.group; j0 += kQueries) {
-            if (p.group > kQueries) load_q(j0);
-            double s[G];                             // s[kQueries i + j]
+        for (int j0 = 0; j0 < p.group; j0 += kQueries * NS) {
+            if (p.group > kQueries * NS) load_q(j0);
 #pragma unroll
-            for (int i = 0; i < G; ++i) s[i] = 0.0;
+            for (int i = 0; i < ITERS; ++i)          // converted where a step needs them, not for all steps before the loop
+#pragma unroll
+                for (int j = 0; j < (int)sizeof(BT) / 2; ++j) asm volatile("" : "+v"(lo[i].w[j]), "+v"(hi[i].w[j]));
+            double s[NS][ITERS];
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < ITERS; ++i) s[n][i] = 0.0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                double a[ITERS], b[ITERS];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < ITERS; ++i)
+#pragma unroll
+                    for (int n = 0; n < NS; ++n) s[n][i] = __builtin_amdgcn_mfma_f64_4x4x4f64(lo[i].at(e), neg[n][e], s[n][i], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < ITERS; ++i)
+#pragma unroll
+                    for (int n = 0; n < NS; ++n) s[n][i] = __builtin_amdgcn_mfma_f64_4x4x4f64(hi[i].at(e), pos[n][e], s[n][i], 0, 0, 0);
+            }
+            // Over the products of a page, whose numbers differ by two, then by one, in turn: all its lanes have its sum then, and
+            // each takes that of one load.
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
 #pragma unroll
                 for (int i = 0; i < ITERS; ++i) {
-                    a[i] = lo[i].at(e);
-                    b[i] = hi[i].at(e);
+                    s[n][i] += dpp<kTurn8>(s[n][i]);
+                    if constexpr (HD == 128) s[n][i] += dpp<kTurn4>(s[n][i]);
                 }
+                double mine = s[n][0];
 #pragma unroll
-                for (int j = 0; j < kQueries; ++j) {
-                    const double x = neg[j][e], y = pos[j][e];
-#pragma unroll
-                    for (int i = 0; i < ITERS; ++i) s[kQueries * i + j] = fma(y, b[i], fma(x, a[i], s[kQueries * i + j]));
-                }
+                for (int i = 1; i < ITERS; ++i)
+                    if (part == i) mine = s[n][i];
+                best = max(best, key_of(mine));
             }
-            // The partners of the first steps mirror each other: what lanes hold differs only by the bits above then.
-            // Bits 0 and 1 of a lane's number are the query in the end, the ones above them the load.
-            if constexpr (G == 16) sum_step<kMirror16, 8, 8>(s, lane);
-            sum_step<kMirror8, 4, 4>(s, lane);
-            sum_step<kXor2, 2, 2>(s, lane);
-            sum_step<kXor1, 1, 1>(s, lane);
-            best = max(best, key_of(s[0]));
         }
-        best = max(best, dpp<kXor1>(best));
+        best = max(best, dpp<kXor1>(best));          // over the queries
         best = max(best, dpp<kXor2>(best));
-        const int nth = (lane % G) >> 2;
-        const bool good = there >> nth & 1;
-        const int64_t place = p0 + nth * PW + sub;
+        const int64_t place = p0 + part * PW + got;
         if ((lane & 3) == 0 && place < end) {
             keys[place] = good && best != kNanKey ? best : 0;
             if (!good) *p.status = RIFT_ERR_SHAPE;
@@ -565,7 +573,10 @@ hipError_t launch_kv_select_pages(const riftkv_cache& c, const KvSelect& s, hipS
     auto types = [&](auto t, auto bt) {
         using T = decltype(t);
         using BT = decltype(bt);
-        return c.head_dim == 128 ? scores(scores_kernel<T, BT, 128>) : scores(scores_kernel<T, BT, 64>);
+        auto sets = [&](auto n) {
+            return c.head_dim == 128 ? scores(scores_kernel<T, BT, 128, n.value>) : scores(scores_kernel<T, BT, 64, n.value>);
+        };
+        return p.group > kQueries ? sets(std::integral_constant<int, 2>{}) : sets(std::integral_constant<int, 1>{});
     };
     if (s.max_pages > s.top && s.top > s.first + s.last) {     // something to choose
         const hipError_t e = c.dt == RIFTKV_F32 ? types(float{}, float{}) : s.bf16 ? types(bf16_t{}, bf16_t{}) : types(float{}, bf16_t{});
