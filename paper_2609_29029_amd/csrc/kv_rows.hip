@@ -110,23 +110,27 @@ rope_any_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, Axes 
     for (int j = rotary_dim + threadIdx.x; j < head_dim; j += 64) store_f32<T>(r.y, y0 + j, load_f32<T>(r.x, x0 + j));
 }
 
-// Eights of elements: a workgroup takes `per` heads of a row.  (Several rows a workgroup
-// save launches of workgroups and lose more in the wait for the first sines: 16,384 rows of 40 heads,
-// half layout, 57.5 us, in twos 60.6, in fours 63.6.)  A head's items are, in the half
+// Eights of elements: a workgroup takes `per` heads of a row, or of several rows side by side whose threads have something to do
+// at once.  (Rows that its threads take one after the other save launches of workgroups and lose more in the wait for the
+// first sines: 16,384 rows of 40 heads, half layout, 57.5 us, in twos 60.6, in fours 63.6.)  A head's items are, in the half
 // layout, rotary_dim / 16 pairs of eights, then the eights that are copied; interleaved,
 // head_dim / 8 eights of four pairs each or copied.
-template <typename T, bool INTERLEAVED, typename Axes>
+template <typename T, bool INTERLEAVED, bool SIDE, typename Axes>
 __global__ void __launch_bounds__(kThreads)
-rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, Axes axes, int per, int head_dim, int rotary_dim,
-            RopeFreqs freqs, float magnitude) {
-    __shared__ float2 turns[kMaxRotary / 2];
-    const int row = blockIdx.x, heads = q.n + k.n, h0 = blockIdx.y * per;
+rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, int rows, Axes axes, int per, int threads_log2, int head_dim,
+            int rotary_dim, RopeFreqs freqs, float magnitude) {
+    __shared__ float2 turns_of[kThreads];
+    static_assert(kThreads >= kMaxRotary / 2, "a row's pairs");
+    const int threads = SIDE ? 1 << threads_log2 : kThreads, tid = SIDE ? threadIdx.x & (threads - 1) : threadIdx.x;
+    const int nth = SIDE ? threadIdx.x >> threads_log2 : 0, row = SIDE ? blockIdx.x * (kThreads >> threads_log2) + nth : blockIdx.x;
+    const int heads = q.n + k.n, h0 = blockIdx.y * per;
     const int half = rotary_dim / 2;
+    float2* turns = turns_of + nth * half;
     const int turned = INTERLEAVED ? rotary_dim / 8 : rotary_dim / 16, items = turned + (head_dim - rotary_dim) / 8;
     // item v of head h; its values are asked for before they are needed, the first before
     // the sines
-    int v = threadIdx.x % items, h = h0 + threadIdx.x / items;
-    const int dv = kThreads % items, dh = kThreads / items, end = min(h0 + per, heads);
+    int v = tid % items, h = h0 + tid / items;
+    const int dv = threads % items, dh = threads / items, end = !SIDE || row < rows ? min(h0 + per, heads) : 0;
     Eight<T> xa, xb;
     void* y;
     size_t at;
@@ -142,7 +146,7 @@ rope_kernel(RopeRows q, RopeRows k, const int* __restrict__ positions, Axes axes
         if (!INTERLEAVED && v < turned) xb = load_eight<T>(x, from + half + e);
     };
     if (h < end) load();
-    if (threadIdx.x < half) turns[threadIdx.x] = rope_turn(axes.position(positions, row, threadIdx.x), freqs, threadIdx.x, magnitude);
+    if (tid < half && (!SIDE || row < rows)) turns[tid] = rope_turn(axes.position(positions, row, tid), freqs, tid, magnitude);
     __syncthreads();
     while (h < end) {
         const int v0 = v;
@@ -531,14 +535,27 @@ hipError_t launch_rope(const RopeRows& q, const RopeRows& k, bool bf16, const in
     // leaves CUs without work (32 rows of 40 heads: 2.6 us, with 512 workgroups 3.4)
     int per = heads;
     while (per > 4 && (int64_t)rows * ((heads + per - 1) / per) < 256) per = (per + 1) / 2;
+    // Threads of a row: as few as take each no more than one item and one pair's sines, while workgroups stay for all CUs
+    // (a workgroup a row and several side by side, us: 14,898 rows of 6 heads of 64, bf16 15.5 and 7.6, f32 19.5 and 12.7; 60,000
+    // of 2 49 and 16; 20,000 of 10 of 128 28.2 and 23.7; 2,100 of 8 of 64 3.8 and 3.5; 1,000 of them 2.9 and 3.0).
+    const int items = heads * ((interleaved ? rotary_dim / 8 : rotary_dim / 16) + (head_dim - rotary_dim) / 8);
+    const int needed = items > rotary_dim / 2 ? items : rotary_dim / 2;
+    int threads_log2 = 8;
+    static_assert(kThreads == 1 << 8, "the threads of a workgroup");
+    while (threads_log2 > 3 && 1 << (threads_log2 - 1) >= needed && rows >> (9 - threads_log2) >= 512) --threads_log2;
+    const int side = kThreads >> threads_log2;
     auto run = [&](auto kernel) {
-        return in_pieces(kMostThreads / kThreads, [&](unsigned n, int64_t r) {
-            hipLaunchKernelGGL(kernel, dim3(n, (unsigned)((heads + per - 1) / per)), dim3(kThreads), 0, st, from(q, r), from(k, r),
-                               positions + r, axes, per, head_dim, rotary_dim, freqs, magnitude);
+        return in_pieces(kMostThreads / kThreads * side, [&](unsigned n, int64_t r) {
+            hipLaunchKernelGGL(kernel, dim3((n + side - 1) / side, (unsigned)((heads + per - 1) / per)), dim3(kThreads), 0, st, from(q, r),
+                               from(k, r), positions + r, (int)n, axes, per, threads_log2, head_dim, rotary_dim, freqs, magnitude);
         });
     };
-    if (bf16) return interleaved ? run(rope_kernel<bf16_t, true, Axes>) : run(rope_kernel<bf16_t, false, Axes>);
-    return interleaved ? run(rope_kernel<float, true, Axes>) : run(rope_kernel<float, false, Axes>);
+    auto types = [&](auto wide) {
+        constexpr bool SIDE = decltype(wide)::value;
+        if (bf16) return interleaved ? run(rope_kernel<bf16_t, true, SIDE, Axes>) : run(rope_kernel<bf16_t, false, SIDE, Axes>);
+        return interleaved ? run(rope_kernel<float, true, SIDE, Axes>) : run(rope_kernel<float, false, SIDE, Axes>);
+    };
+    return side > 1 ? types(std::true_type{}) : types(std::false_type{});
 }
 
 }  // namespace

@@ -151,3 +151,45 @@ def test_rows_of_no_length(R):
     freqs, _ = R.riftkv_rope_freqs(64)
     x = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
     R.riftkv_rope_axes(x, None, torch.empty(2, 0, dtype=torch.int32, device="cuda"), freqs, by_turns(32, 2))
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows, nq, nk, hd, rot", [
+    (1025, 1, 0, 16, 16), (16389, 1, 0, 16, 16), (4099, 0, 1, 64, 32), (2051, 2, 1, 64, 64), (20001, 1, 1, 64, 64), (1030, 3, 1, 128, 128),
+    (2100, 8, 2, 128, 128), (2049, 1, 1, 256, 256), (4100, 1, 2, 128, 16), (1100, 16, 16, 64, 64)])
+def test_many_rows_of_few_heads(R, layout, dt, rows, nq, nk, hd, rot):
+    """Many rows of few heads share workgroups, few do not: the same bits either way, on one axis and on several, in place
+    and not, with the row behind the last left as it was."""
+    dtype = TYPES[dt]
+    wide = randn(rows + nq, rows + 1, (nq + nk) * hd, dtype=dtype)
+    g = torch.Generator().manual_seed(hd)
+    pos = torch.randint(-(1 << 31), (1 << 31) - 1, (3, rows), generator=g, dtype=torch.int64).int().cuda()
+    freqs, _ = R.riftkv_rope_freqs(rot)
+    axes = by_turns(rot // 2, 3)
+
+    def parts(t, n):
+        return (t[:n, :nq * hd].view(n, nq, hd) if nq else None, t[:n, nq * hd:].view(n, nk, hd) if nk else None)
+
+    for several in (True, False):
+        def call(t, n, places):
+            q, k = parts(t, n)
+            if several:
+                R.riftkv_rope_axes(q, k, places.contiguous(), freqs, axes, layout=layout)
+            else:
+                R.riftkv_rope(q, k, places[0].contiguous(), freqs, layout=layout)
+
+        want, got, out = wide.clone(), wide.clone(), wide.clone()
+        for r in range(0, rows, 300):
+            n = min(300, rows - r)
+            call(want[r:r + n], n, pos[:, r:r + n])
+        call(got, rows, pos)
+        assert torch.equal(got, want) and torch.equal(got[rows], wide[rows]) and not torch.equal(got, wide)
+        out.fill_(7.0)
+        args = (*parts(wide, rows), pos if several else pos[0], freqs)
+        outs = parts(out, rows)
+        if several:
+            R.riftkv_rope_axes(*args, axes, *outs, layout=layout)
+        else:
+            R.riftkv_rope(*args, *outs, layout=layout)
+        assert torch.equal(out[:rows], want[:rows]) and bool((out[rows] == 7.0).all())
