@@ -4,8 +4,8 @@
 //   listed_kernel   a workgroup takes a part of the tokens of up to 16 query heads of one key head; its waves share the
 //                   part's tiles and join in LDS.  Where the tokens are one part, the output is written here.
 //   shared_kernel   the same for a sequence's own tokens, and beside them, in the same launch, workgroups for the prefix:
-//                   prefix_body (kv_prefix.h), or for few rows and float32 pages as above, 16 rows of a key head whatever
-//                   their sequences.  A short prefix is walked by every sequence itself.
+//                   prefix_body (kv_prefix.h), or where there is little to do, and for float32 pages, as above, 16 rows of a
+//                   key head whatever their sequences.  A short prefix is walked by every sequence itself.
 //   parts_kernel    the sum of the parts.
 //
 // The items' tokens are bound by their bytes (64 sequences, 64 heads in groups of 8, 128 e4m3 pages of 32 a key head: 504 MB in 84 us,
@@ -424,13 +424,19 @@ struct SharedPlan {
     int64_t rows, items;     // rows of a key head; items of the sequences' own tokens
     bool walk, by_rows;      // the prefix by every sequence itself; by prefix_body
     int front_parts, front_wgs, row_tiles, parts;
-    SharedPlan(const riftkv_cache& c, int n_heads, int64_t n_seq, int prefix_len, int64_t max_pages) {
+    SharedPlan(const riftkv_cache& c, int n_heads, bool bf16, int64_t n_seq, int prefix_len, int64_t max_pages) {
         const int group = n_heads / c.n_kv_heads;
         const int64_t own = (max_pages * c.page_size + kTile - 1) / kTile;
         rows = n_seq * group;
         items = n_seq * c.n_kv_heads * ((group + 15) / 16);
         walk = prefix_len <= kWalked;
-        by_rows = !walk && c.dt != RIFTKV_F32 && rows > 32;
+        // 16 rows at a time keep more CUs busy and wait less; 128 read less and use larger products, which pays from so many (16
+        // rows, token) pairs on.  In us, 16 and 128 rows at a time (bf16 queries, 128 dimensions): bf16 pages, 48,000 pairs 13.1
+        // and 13.3, 64,000 19.5 and 17.2, 128,000 17.5 and 18.4 or 20.0 and 17.0, 384,000 36 and 21; 8 bits, 192,000 21.2 and 23.7,
+        // 384,000 29.3 and 26.5, 512,000 30.3 and 27.6, 4.2 million 160 and 86.  Float32 queries: bf16 pages alike; 8 bits, two times three
+        // terms of widened rows, 29 and 45, 57 and 66, 170 and 180.
+        const int64_t pairs = (int64_t)c.n_kv_heads * ((rows + 15) / 16) * prefix_len;
+        by_rows = !walk && rows_kernel(c.dt, bf16) && pairs > (c.dt == RIFTKV_BF16 ? 56 : 400) * 1000;
         front_parts = front_wgs = 0;
         row_tiles = (int)((rows + kRows - 1) / kRows);
         parts = items > 128 || own < 24 ? 1 : parts_of(items, own);   // a split alone costs a launch, which pays for long items that are few
@@ -448,6 +454,7 @@ struct SharedPlan {
         } else front_parts = parts_of(wgs, (prefix_len + kTile - 1) / kTile);
         front_wgs = (int)(wgs * front_parts);
     }
+    static constexpr bool rows_kernel(riftkv_dtype dt, bool bf16) { return dt == RIFTKV_BF16 || (dt != RIFTKV_F32 && bf16); }
     // Tokens of a prefix that every sequence walks itself, walked / in workgroups of its own: 100 sequences of 96 to 608 tokens
     // and 32 heads 92 / 100 us (65 tokens), 101 / 103 (200), 109 / 103 (300); 64 of 1 to 300 in groups of 4 11.7 / 18.6 (65),
     // 13.8 / 18.9 (200), 15.2 / 19.0 (300); 8 of them 10.1 / 10.6 (256), 13.0 / 11.0 (500).
@@ -471,7 +478,7 @@ size_t kv_listed_workspace(const riftkv_cache& c, int n_heads, int64_t, int) {
 }
 
 hipError_t launch_kv_attention_shared(const riftkv_cache& c, const KvAttention& a, const int* prefix_table, int prefix_len, hipStream_t st) {
-    const SharedPlan plan(c, a.n_heads, a.n_seq, prefix_len, a.max_pages);
+    const SharedPlan plan(c, a.n_heads, a.bf16, a.n_seq, prefix_len, a.max_pages);
     RangeParams p = params_of(c, a);
     p.parts = plan.parts;
     p.front_rows = plan.rows;
@@ -497,7 +504,7 @@ hipError_t launch_kv_attention_shared(const riftkv_cache& c, const KvAttention& 
         };
         hipError_t e;
         bool done = false;
-        if constexpr (dt.value != RIFTKV_F32)
+        if constexpr (SharedPlan::rows_kernel(dt.value, sizeof(T) == 2))
             if (plan.by_rows) {
                 e = launch(shared_kernel<T, dt.value, hd.value, true>, kPrefixLds);
                 done = true;
