@@ -417,6 +417,15 @@ int parts_of(int64_t items, int64_t tiles) {
     return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : (int)parts;
 }
 
+// The same where a split alone costs a launch to join the parts, which pays for long items that are few.  In us, whole and in parts:
+// 96 items of 20 tiles 12.2 and 13.2, e4m3 of 64 dimensions 7.9 and 8.7; 32 of 20 9.5 and 8.8, e4m3 10.6 and 8.6; 16 of 12 6.9 and 8.1.  Float32
+// pages, whose products take longer: 96 of 20 29.2 and 23.9, of 64 dimensions 16.1 and 14.3; 32 of 20 24.6 and 13.9; 160 of 30 47.8
+// and 44.3; 192 of up to 31 44.0 and 46.4; 16 of 12 13.4 and 11.2.
+int parts_alone(riftkv_dtype dt, int64_t items, int64_t tiles) {
+    const bool split = dt == RIFTKV_F32 ? items <= kMostSplit && tiles >= 8 : items <= 128 && tiles >= (items <= 64 ? 20 : 24);
+    return split ? parts_of(items, tiles) : 1;
+}
+
 size_t part_bytes(const riftkv_cache& c) { return (size_t)(c.head_dim + 4) * sizeof(float); }
 
 // How the call of a prefix is made.
@@ -439,7 +448,7 @@ struct SharedPlan {
         by_rows = !walk && rows_kernel(c.dt, bf16) && pairs > (c.dt == RIFTKV_BF16 ? 56 : 400) * 1000;
         front_parts = front_wgs = 0;
         row_tiles = (int)((rows + kRows - 1) / kRows);
-        parts = items > 128 || own < 24 ? 1 : parts_of(items, own);   // a split alone costs a launch, which pays for long items that are few
+        parts = parts_alone(c.dt, items, own);
         if (walk) return;
         parts = parts_of(items, own);
         const int64_t wgs = c.n_kv_heads * (by_rows ? row_tiles : (rows + 15) / 16);
@@ -518,7 +527,7 @@ hipError_t launch_kv_attention_shared(const riftkv_cache& c, const KvAttention& 
 hipError_t launch_kv_attention_pages(const riftkv_cache& c, const KvAttention& a, const int* lists, int top, hipStream_t st) {
     RangeParams p = params_of(c, a);
     const int64_t items = (int64_t)a.n_seq * p.n_kv * p.q_tiles, tiles = ((int64_t)top * c.page_size + kTile - 1) / kTile;
-    if (items <= 128 && tiles >= 24) p.parts = parts_of(items, tiles);   // a split costs a launch, which pays for long items that are few
+    p.parts = parts_alone(c.dt, items, tiles);
     const ListedPages where{OwnPages{a.table, a.lens, a.max_pages}, lists, top};
     const size_t lds = (size_t)kWaves * p.rows * (c.head_dim + 4) * sizeof(float);
     return by_types(c, a.bf16, [&](auto t, auto dt, auto hd) {
