@@ -362,12 +362,17 @@ scores_kernel(SelectParams p) {
     }
 }
 
-// A workgroup takes a key head of a sequence, a thread a run of its pages: the key of the last page to take, eleven bits of it
+// A workgroup takes a key head of a sequence, a thread a run of its pages (of every 4,096): the key of the last page to take, eleven bits of it
 // at a time from the first that differs between pages (so that few pages are left in a bucket of the first time, often the
-// one that is looked for), then the list.  A chain of waits: 7.0 us for 8 key heads of 1,024 pages, 8.6 for 384 of up to 2,032.
+// one that is looked for), then the list.  A chain of waits: 6.9 us for 8 key heads of 1,024 pages, 8.2 for 384 of up to 2,032.
+// (A run of all of its pages, however many, took a thread through memory in long steps: 2 key heads of 62,500 pages, with the scores,
+// 190 us, in turns 92; every 512th page: 133, and 2% more below 4,096.)
 constexpr int kPickThreads = 512, kHeldKeys = 8;   // keys that a thread keeps in registers
+constexpr int kTurnKeys = kPickThreads * kHeldKeys;  // more pages are gone through in turns
 constexpr int kBucketBits = 11, kBuckets = 1 << kBucketBits;
 
+// TURNS: there can be more pages than the threads hold.
+template <bool TURNS>
 __global__ void __launch_bounds__(kPickThreads)
 pick_kernel(SelectParams p) {
     constexpr int WAVES = kPickThreads / 64;
@@ -407,23 +412,31 @@ pick_kernel(SelectParams p) {
     }
     const int begin = p.first, n = held - p.first - p.last;          // the pages to choose from, more than need
     const unsigned long long* keys = p.keys + (size_t)item * p.max_pages + begin;
-    const int per = (n + kPickThreads - 1) / kPickThreads;
-    const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
+    const int per = ((TURNS ? min(n, kTurnKeys) : n) + kPickThreads - 1) / kPickThreads;
     unsigned long long mine[kHeldKeys];
+    // this thread's run of the turn that begins at page `first`: i0 .. i1 - 1
+    int i0 = 0, i1 = 0;
+    auto load = [&](int first) __attribute__((always_inline)) {
+        i0 = min(first + tid * per, n);
+        i1 = min(i0 + per, n);
 #pragma unroll
-    for (int i = 0; i < kHeldKeys; ++i) mine[i] = i0 + i < i1 ? keys[i0 + i] : 0;
+        for (int i = 0; i < kHeldKeys; ++i) mine[i] = i0 + i < i1 ? keys[i0 + i] : 0;
+    };
+    load(0);
     // f(key) of every page of this thread
     auto each = [&](auto f) __attribute__((always_inline)) {
-        if (per <= kHeldKeys) {
+        for (int first = 0;;) {
 #pragma unroll
             for (int i = 0; i < kHeldKeys; ++i)
-                if (i0 + i < i1) f(mine[i], i0 + i);
-        } else {
-            for (int i = i0; i < i1; ++i) f(keys[i], i);
+                if (i0 + i < i1) f(mine[i]);
+            if (!TURNS || n <= kTurnKeys) break;
+            first = first + kTurnKeys < n ? first + kTurnKeys : 0;
+            load(first);
+            if (first == 0) break;
         }
     };
     uint32_t highest = 0, complement = 0;
-    each([&](unsigned long long k, int) {
+    each([&](unsigned long long k) {
         highest = max(highest, (uint32_t)(k >> 32));
         complement = max(complement, ~(uint32_t)(k >> 32));
     });
@@ -445,7 +458,7 @@ pick_kernel(SelectParams p) {
     int width = kBuckets;
     for (;;) {
         const unsigned long long base = bucket & ~(unsigned long long)(width - 1);   // the first of the buckets looked at
-        each([&](unsigned long long k, int) {
+        each([&](unsigned long long k) {
             const unsigned long long in = (k >> bit) - base;
             if (in < (unsigned long long)width) atomicAdd(&counts[in], 1);
         });
@@ -494,30 +507,45 @@ pick_kernel(SelectParams p) {
         __syncthreads();
     }
     // places in the list: of the pages above, and of the bucket's first ones
-    int higher = 0, equal = 0;
-    each([&](unsigned long long k, int) {
-        higher += (k >> bit) > bucket;
-        equal += (k >> bit) == bucket;
-    });
-    const int hi_incl = wave_scan(higher), eq_incl = wave_scan(equal);
-    if (lane == 63) {
-        sums[wave][0] = hi_incl;
-        sums[wave][1] = eq_incl;
-    }
-    __syncthreads();
-    int hi = hi_incl - higher, eq = eq_incl - equal;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w)
-        if (w < wave) {
-            hi += sums[w][0];
-            eq += sums[w][1];
+    int higher = 0, equal = 0;                       // in the turns before
+    for (int first = 0; first == 0 || (TURNS && first < n); first += kTurnKeys) {
+        if (TURNS && first > 0) {
+            load(first);
+            __syncthreads();                         // (the sums have been read)
         }
-    each([&](unsigned long long k, int i) {
-        const unsigned long long b = k >> bit;
-        if (b > bucket || (b == bucket && eq < need)) list[p.first + hi + min(eq, need)] = begin + i;
-        hi += b > bucket;
-        eq += b == bucket;
-    });
+        int hi = 0, eq = 0;
+#pragma unroll
+        for (int i = 0; i < kHeldKeys; ++i)
+            if (i0 + i < i1) {
+                hi += (mine[i] >> bit) > bucket;
+                eq += (mine[i] >> bit) == bucket;
+            }
+        const int hi_incl = wave_scan(hi), eq_incl = wave_scan(eq);
+        if (lane == 63) {
+            sums[wave][0] = hi_incl;
+            sums[wave][1] = eq_incl;
+        }
+        __syncthreads();
+        hi = higher + hi_incl - hi;
+        eq = equal + eq_incl - eq;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) {
+                hi += sums[w][0];
+                eq += sums[w][1];
+            }
+            higher += sums[w][0];
+            equal += sums[w][1];
+        }
+#pragma unroll
+        for (int i = 0; i < kHeldKeys; ++i)
+            if (i0 + i < i1) {
+                const unsigned long long b = mine[i] >> bit;
+                if (b > bucket || (b == bucket && eq < need)) list[p.first + hi + min(eq, need)] = begin + i0 + i;
+                hi += b > bucket;
+                eq += b == bucket;
+            }
+    }
 }
 
 }  // namespace
@@ -582,7 +610,8 @@ hipError_t launch_kv_select_pages(const riftkv_cache& c, const KvSelect& s, hipS
         const hipError_t e = c.dt == RIFTKV_F32 ? types(float{}, float{}) : s.bf16 ? types(bf16_t{}, bf16_t{}) : types(float{}, bf16_t{});
         if (e != hipSuccess) return e;
     }
-    return in_pieces(1, kPickThreads, [&](unsigned wgs) { hipLaunchKernelGGL(pick_kernel, dim3(wgs), dim3(kPickThreads), 0, st, p); });
+    const auto pick = s.max_pages > kTurnKeys ? pick_kernel<true> : pick_kernel<false>;
+    return in_pieces(1, kPickThreads, [&](unsigned wgs) { hipLaunchKernelGGL(pick, dim3(wgs), dim3(kPickThreads), 0, st, p); });
 }
 
 }  // namespace rift

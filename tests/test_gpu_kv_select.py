@@ -354,3 +354,19 @@ def test_decode_over_a_sparse_context(R, store):
         assert torch.equal(pages.cpu(), selection(b, P.table, q, held(n, page), n_kv, top, 1, 1))
         check(out, *attend_lists(P, q, n, pages.cpu()), q.dtype, f"step {step}")
     assert int(P.status) == 0
+
+
+def test_select_ties_among_many_pages(R):
+    """Few different scores, in tables of more pages than a workgroup holds at a time: the lowest places of the last score,
+    wherever they end; sequences of one such table that are short, long, just as many pages as are held and one more."""
+    pages = 13000
+    P = plain_cache(R, 1, 64, 16, pages, 7, pages)
+    bounds = torch.zeros(pages, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    bounds[:, 0, :, 0] = torch.randint(0, 3, (pages, 1), generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    q = torch.zeros(7, 1, 64, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 1.0
+    n = [pages, 4096, 4097, 4098, 8192, 300, 12289]
+    for top, first, last in ((2000, 0, 0), (4097, 1, 0), (299, 1, 1), (7000, 5, 7), (9000, 0, 0)):
+        got = select(R, P, bounds, q, [16 * x for x in n], top, first, last).cpu()
+        assert torch.equal(got, selection(bounds, P.table, q, n, 1, top, first, last)), top
+    assert int(P.status) == 0
