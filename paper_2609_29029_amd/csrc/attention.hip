@@ -43,6 +43,7 @@
 // at logical key 0, so the result is the same, bit for bit, as with the prefix
 // packed into every sequence.
 #include "launch.h"
+#include "lds_dma.h"
 #include "rift_common.h"
 
 namespace rift {
@@ -64,23 +65,6 @@ typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
 // 16-bit element at (address passed by lane 16 g + 4 j + i / 4) + i % 4.
 __device__ __forceinline__ v4s_t lds_read_tr16(const void* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(p));
-}
-
-// LDS DMA of 16 bytes per lane from a per-lane global address into
-// LDS[m0 + 16 lane] (m0 wave-uniform).
-__device__ __forceinline__ void dma16v(const void* gaddr, uint32_t lds_addr) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(gaddr) : "memory", "m0");
-}
-
-// Same, saddr form: 64-bit wave-uniform base plus a 32-bit per-lane byte
-// offset.
-__device__ __forceinline__ void dma16s(const void* base, uint32_t voff, uint32_t lds_addr) {
-    const uint64_t b = (uint64_t)(uintptr_t)base;
-    const uint64_t ub = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b) |
-                        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(ub) : "memory", "m0");
 }
 
 // wait until at most n of this wave's vector memory operations are outstanding
@@ -204,7 +188,7 @@ attn_bf16_kernel(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
                 const int row = 4 * jj + dma_row_lo;
                 const int swz = dma_v ? 4 * (row & 3) : (row & 15);
                 const int c = (lane & 15) ^ swz;
-                if (HD == kLdsDims || c < HD / 8) dma16s(base, dma_off[i], sb + (uint32_t)jj * 1024u);
+                if (HD == kLdsDims || c < HD / 8) lds_dma16(base, dma_off[i], sb + (uint32_t)jj * 1024u);
             }
             return;
         }
@@ -218,7 +202,7 @@ attn_bf16_kernel(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
             const int swz = dma_v ? 4 * (row & 3) : (row & 15);
             const int c = (lane & 15) ^ swz;
             if (HD == kLdsDims || c < HD / 8)
-                dma16v(dma_src + (size_t)grow * ld + head_off + c * 8, sb + (uint32_t)jj * 1024u);
+                lds_dma16_lanes(dma_src + (size_t)grow * ld + head_off + c * 8, sb + (uint32_t)jj * 1024u);
         }
     };
 

@@ -23,6 +23,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../lds_dma.h"
+
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -140,11 +142,8 @@ __global__ void __launch_bounds__(512) ceiling_moves(const uint16_t* __restrict_
                     // byte offsets: lane part < 512 KiB, block part < 2 MiB
                     const uint32_t voff = (uint32_t)(lane * 16 + jj * 1024 + wave * 2048 + (blockIdx.x & 31) * 16384);
                     const uint64_t base = dbase + (uint64_t)((((it + u) * D + jj) * 4096) & 2097151);
-                    const uint64_t ub = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base) |
-                                        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32)) << 32);
-                    const uint32_t m0 = lds0 + 65536u + (uint32_t)wave * 4096u + (uint32_t)((u * D + jj) & 3) * 1024u;
-                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
-                                 :: "s"(__builtin_amdgcn_readfirstlane(m0)), "v"(voff), "s"(ub) : "memory", "m0");
+                    const uint32_t to = lds0 + 65536u + (uint32_t)wave * 4096u + (uint32_t)((u * D + jj) & 3) * 1024u;
+                    rift::lds_dma16(reinterpret_cast<const void*>(base), voff, to);
                 }
             }
             asm volatile("s_waitcnt vmcnt(8)" ::: "memory");

@@ -31,6 +31,7 @@
 #include <type_traits>
 
 #include "launch.h"
+#include "lds_dma.h"
 #include "rift_common.h"
 
 namespace rift {
@@ -135,17 +136,6 @@ __device__ __forceinline__ int b_row(const GemmParams& p, int n0, int r) {
     }
 }
 
-// LDS DMA (global_load_lds_dwordx4): 16 bytes per lane to LDS address lds_addr +
-// 16 lane, from a 64-bit wave-uniform base plus a 32-bit per-lane byte offset (the hardware adds them; offsets stay below 2^31 by the host checks).
-__device__ __forceinline__ void dma16s(const void* base, uint32_t voff, uint32_t lds_addr) {
-    const uint64_t b = (uint64_t)(uintptr_t)base;
-    // readfirstlane returns a signed int: go through uint32_t so the low word is
-    // zero-extended (sign extension would corrupt the upper half of the address)
-    const uint64_t ub = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b) |
-                        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(ub) : "memory", "m0");
-}
 __device__ __forceinline__ void wg_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // ---------------------------------------------------------------------------
@@ -426,8 +416,8 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_short_kernel(GemmParams p) {
     auto dma_one = [&](int slot, int kt, int q) {
         const uint32_t sb = lds0 + (uint32_t)slot * (kStage * 2);
         const size_t ko = (size_t)kt * BK3;
-        if (q < MB) dma16s(p.a + ko, aoff[q], sb + (uint32_t)(MB * wave + q) * 1024u);
-        else dma16s(bbase[q - MB] + ko, boff[q - MB], sb + TM * 128u + (uint32_t)(4 * wave + q - MB) * 1024u);
+        if (q < MB) lds_dma16(p.a + ko, aoff[q], sb + (uint32_t)(MB * wave + q) * 1024u);
+        else lds_dma16(bbase[q - MB] + ko, boff[q - MB], sb + TM * 128u + (uint32_t)(4 * wave + q - MB) * 1024u);
     };
     if constexpr (EPI == EPI_QKV) {
         if (tid < TM) {
@@ -608,11 +598,11 @@ __global__ void __launch_bounds__(512, 1) gemm_bf16_pp_kernel(GemmParams p) {
             const int row = 8 * (MB * wn + q) + lrow;
             const int c = (lane & 7) ^ swz8(row);
             const int ar = m0 + row < p.M ? m0 + row : p.M - 1;
-            dma16s(p.a + ko, ((uint32_t)ar * (uint32_t)p.K + (uint32_t)c * 8u) * 2u,
-                   sb + (uint32_t)(MB * wn + q) * 1024u);
+            lds_dma16(p.a + ko, ((uint32_t)ar * (uint32_t)p.K + (uint32_t)c * 8u) * 2u,
+                      sb + (uint32_t)(MB * wn + q) * 1024u);
         } else {
             const int j = q - MB;
-            dma16s(bsrc + ko + (size_t)(8 * j) * p.K, boff[j & 1], sb + TM * 128u + (uint32_t)(8 * wn + j) * 1024u);
+            lds_dma16(bsrc + ko + (size_t)(8 * j) * p.K, boff[j & 1], sb + TM * 128u + (uint32_t)(8 * wn + j) * 1024u);
         }
     };
 

@@ -30,6 +30,7 @@
 #include <type_traits>
 
 #include "launch.h"
+#include "lds_dma.h"
 #include "rift_common.h"
 
 namespace rift {
@@ -62,22 +63,6 @@ __device__ __forceinline__ T* pick_region(int i, T* x, T* y, T* z) {
     uintptr_t r = i == 1 ? b : a;
     r = i == 2 ? c : r;
     return (T*)r;
-}
-
-// LDS DMA (global_load_lds_dwordx4): 16 bytes per lane from base + voff to
-// LDS address lds_addr + 16 lane (base and lds_addr wave-uniform).  NT: nontemporal.
-template <bool NT>
-__device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t lds_addr) {
-    const uint64_t b = (uint64_t)(uintptr_t)base;
-    // through uint32_t so that the low word is zero-extended
-    const uint64_t ub = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b) |
-                        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32);
-    if constexpr (NT)
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
-                     :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(ub) : "memory", "m0");
-    else
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
-                     :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(ub) : "memory", "m0");
 }
 
 // Slot of 16-byte chunk c in an LDS operand row (128 bytes, 8 chunks):
@@ -160,9 +145,9 @@ skinny_gemm_kernel(SkinnyParams p) {
         const uint32_t sb = ring0 + (uint32_t)dslot * kStageBytes + kRows * SK_RB + (uint32_t)wave * (BD * 1024u);
         const size_t ko = (size_t)dk * SK_KS;
 #pragma unroll
-        for (int q = 0; q < BD; ++q) dma16<kNt>(db + ko, boff[q], sb + q * 1024u);
+        for (int q = 0; q < BD; ++q) lds_dma16<kNt>(db + ko, boff[q], sb + q * 1024u);
 #pragma unroll
-        for (int q = 0; q < RB; ++q) dma16<false>(p.a + ko, aoff[q], sa + q * 1024u);
+        for (int q = 0; q < RB; ++q) lds_dma16(p.a + ko, aoff[q], sa + q * 1024u);
         dslot = dslot + 1 == RING ? 0 : dslot + 1;
         if (++dk == nst) {
             dk = 0;

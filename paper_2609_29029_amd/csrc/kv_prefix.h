@@ -22,6 +22,7 @@
 #pragma once
 
 #include "kv_tile.h"
+#include "lds_dma.h"
 
 namespace rift {
 
@@ -67,14 +68,6 @@ __device__ __forceinline__ void round_split(float a, float b, uint32_t (&w)[2]) 
 template <typename X>
 __device__ __forceinline__ void hold(X& x) {
     asm volatile("" : "+v"(x));
-}
-
-// LDS DMA of 16 bytes a lane: from a wave-uniform base and a lane's offset to lds + 16 lane.
-__device__ __forceinline__ void dma16(const unsigned char* base, uint32_t offset, uint32_t lds) {
-    const uint64_t b = (uint64_t)(uintptr_t)base;
-    const uint64_t ub = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b) |
-                        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(ub) : "memory", "m0");
 }
 
 // Workgroup `block` of n_kv * row_tiles * parts; lds: kPrefixLds bytes, two stages, then their scales.
@@ -129,7 +122,7 @@ __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, un
             const int row = 4 * i + (lane >> 4);
             const int c = (lane & 15) ^ (v ? 4 * (row & 3) : row);
             if (HD == 128 || c < CHUNKS)
-                dma16(base, (uint32_t)(row * (HD * B) + c * 16), lds0 + (t & 1) * kStageBytes + (v ? kTileBytes : 0) + (r + 4 * i) * kRowBytes);
+                lds_dma16(base, (uint32_t)(row * (HD * B) + c * 16), lds0 + (t & 1) * kStageBytes + (v ? kTileBytes : 0) + (r + 4 * i) * kRowBytes);
         }
     };
     // An 8-bit tile goes through registers, where it is widened: chunk `chunk` of rows row, row + STEP, .. a thread.  All lanes
