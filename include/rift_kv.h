@@ -233,8 +233,7 @@ RIFT_API size_t riftkv_attention_shared_workspace_size(const riftkv_cache* cache
  * prefix_len   [host] tokens of the prefix, >= 0
  * lens         [n_seq] i32 in [0, max_pages * page_size], the prefix not counted
  * A page of the prefix outside [0, n_pages) sets the status and makes every sequence's output NaN; a sequence
- * without any token gives zeros.  With bf16 queries a weight of the prefix goes into the product with the values short
- * by up to 2^-17 of it.  Weights of the prefix may be as large as 2^8 before their sum divides them: values (or scales of
+ * without any token gives zeros.  Weights of the prefix may be as large as 2^8 before their sum divides them: values (or scales of
  * 8-bit rows) past 2^119 may overflow where they do not in riftkv_attention.  Everything else as for riftkv_attention.
  * Shape rules: prefix_len <= 2^30, n_seq * n_heads <= 2^26.
  */

@@ -7,15 +7,15 @@
 // Weighted values, a reference and the sum of a part go to the workspace.
 //
 // S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds the scores of one query, and its weights are
-// already its share of the second product's right operand, whose left one comes from transposing LDS reads.  Float32 queries and
-// their weights go into the products as three bf16 terms that add up to them; the weights of bf16 queries as two, short by
-// 2^-17 of a weight at most, where the output is rounded to 2^-9.
+// already its share of the second product's right operand, whose left one comes from transposing LDS reads.  Float32
+// queries, and all weights, go into the products as three bf16 terms that add up to them.
 //
-// Bound by the products and the weights' vector instructions together, which overlap only in part: of a wave's tile 48 products of
-// 32 cycles and some 200 vector instructions with 32 exponentials of 16.  64 sequences' 256 rows after 32,768 tokens, 8 key heads,
-// bf16: 34 GFLOP in 56 us alone (134 MB), and 66 with the sequences' own 79 MB beside it; every sequence on its own read the
-// prefix 64 times and took 606.  Kept: halves of a tile in a pipeline, a product and then two weights in turn (61 us a launch of
-// 256 workgroups, 70 without); not kept: more of the next tiles touched ahead into L2, operands two products ahead (no change).
+// Bound by the products and the weights' vector instructions together, which overlap only in part: of a wave's tile 64 products of
+// 32 cycles and some 240 vector instructions with 32 exponentials of 16.  64 sequences' 256 rows after 32,768 tokens, 8 key heads,
+// bf16: 34 GFLOP in 75 us alone (134 MB), and 80.5 with the sequences' own 79 MB beside it (with two terms a weight, which are up
+// to 2^-16 of it off, 66); every sequence on its own read the prefix 64 times and took 606.  Kept, measured with two terms: halves
+// of a tile in a pipeline, a product and then two weights in turn (61 us a launch of 256 workgroups, 70 without); not kept: more of
+// the next tiles touched ahead into L2, operands two products ahead (no change).
 //
 // Rows of a tile are 256 bytes (64 dimensions fill half of them); the 16-byte chunks of row r lie at chunk ^ (r & 15) for
 // keys and at chunk ^ 4 (r & 3) for values, so that neither read meets a bank twice.
@@ -53,17 +53,6 @@ typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
 // Lane i of each 16-lane group g gets, in component j, the 16-bit element at (address of lane 16 g + 4 j + i / 4) + i % 4.
 __device__ __forceinline__ v4s_t lds_read_tr16(const void* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(p)); }
 
-// Two bf16 terms that add up to a and b but for 2^-17 of them: the first is cut off, what is left rounded.
-__device__ __forceinline__ void round_split(float a, float b, uint32_t (&w)[2]) {
-    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-    w[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-    a -= __uint_as_float(x & 0xFFFF0000u);
-    b -= __uint_as_float(y & 0xFFFF0000u);
-    typedef float f2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
-}
-
 // A value that has to be there at this point of the program.
 template <typename X>
 __device__ __forceinline__ void hold(X& x) {
@@ -75,7 +64,7 @@ template <typename T, riftkv_dtype DT, int HD>
 __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, unsigned char* lds) {
     constexpr int B = DT == RIFTKV_BF16 ? 2 : 1;
     constexpr bool SCALED = B == 1;
-    constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;
+    constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = 3;
     constexpr int CHUNKS = HD * B / 16;           // 16-byte chunks of a row in the pages
     constexpr int LOADS = kTokens * CHUNKS / 256; // of a thread, of keys or values
     constexpr int STEP = 256 / CHUNKS;            // rows between them
@@ -230,8 +219,13 @@ __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, un
 
     // Half a tile at a time: s[i] is token 32 kb + 8 (i / 4) + 4 h + i % 4 of tile t.  Steps of one product each: `step` kk of
     // the first, `step` (x, c) of the second.
+    // 8-bit tiles have no registers left for the places of all steps (spilled ones come back behind the next tile's loads, whose
+    // order they share): there each is worked out where it is used.
+    const int k_off = n * kRowBytes + ((h ^ (n & 15)) << 4);
     auto key_at = [&](int t, int kb, int kk) __attribute__((always_inline)) {
-        return *reinterpret_cast<const bf16x8_t*>(lds + (t & 1) * kStageBytes + (kb * 32 + n) * kRowBytes + (((2 * kk + h) ^ (n & 15)) << 4));
+        int at = k_off;
+        if constexpr (SCALED) hold(at);
+        return *reinterpret_cast<const bf16x8_t*>(lds + (t & 1) * kStageBytes + kb * 32 * kRowBytes + (at ^ (kk << 5)));
     };
     auto score = [&](const bf16x8_t& kf, int kk, f32x16_t& s) __attribute__((always_inline)) {
 #pragma unroll
@@ -308,8 +302,7 @@ __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, un
             a *= f.x;
             b *= f.y;
         }
-        if constexpr (NP == 2) round_split(a, b, y);
-        else split_bf16<NP>(a, b, y);
+        split_bf16<NP>(a, b, y);
     };
     auto weights = [&](int t, int kb, f32x16_t& s, u32x4_t(&pf)[2][NP]) __attribute__((always_inline)) {
         const float f = refer(t, kb, s), neg_ref = -ref_of(m);

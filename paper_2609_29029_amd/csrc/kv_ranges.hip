@@ -440,12 +440,14 @@ struct SharedPlan {
         items = n_seq * c.n_kv_heads * ((group + 15) / 16);
         walk = prefix_len <= kWalked;
         // 16 rows at a time keep more CUs busy and wait less; 128 read less and use larger products, which pays from so many (16
-        // rows, token) pairs on.  In us, 16 and 128 rows at a time (bf16 queries, 128 dimensions): bf16 pages, 48,000 pairs 13.1
-        // and 13.3, 64,000 19.5 and 17.2, 128,000 17.5 and 18.4 or 20.0 and 17.0, 384,000 36 and 21; 8 bits, 192,000 21.2 and 23.7,
-        // 384,000 29.3 and 26.5, 512,000 30.3 and 27.6, 4.2 million 160 and 86.  Float32 queries: bf16 pages alike; 8 bits, two times three
-        // terms of widened rows, 29 and 45, 57 and 66, 170 and 180.
+        // rows, token) pairs on.  In us, 16 and 128 rows at a time (bf16 queries, 128 dimensions, 8 key heads, 16 or 64 sequences in
+        // groups of 4): bf16 pages, 48,000 pairs 14.6 and 13.8 or 20.3 and 17.5, 64,000 17.1 and 14.3 or 20.6 and 17.9, 128,000 17.5 and
+        // 19.7 or 23.5 and 21.3, 384,000 26.7 and 25.2 or 29.5 and 28.2, 4.2 million 194 and 92; 8 bits, 512,000 26.7 and 35.3 or 28.9 and
+        // 34.5, 768,000 34.1 and 43.2 or 34.5 and 37.3, 1.0 million 41.5 and 40.0 (int8 48.2 and 41.3), 2.0 million 68.5 and 56.4, 4.2
+        // million 138 and 102 (158 and 98).  Float32 queries: bf16 pages alike; 8 bits, two times three terms of widened rows, 29
+        // and 45, 57 and 66, 170 and 180.
         const int64_t pairs = (int64_t)c.n_kv_heads * ((rows + 15) / 16) * prefix_len;
-        by_rows = !walk && rows_kernel(c.dt, bf16) && pairs > (c.dt == RIFTKV_BF16 ? 56 : 400) * 1000;
+        by_rows = !walk && rows_kernel(c.dt, bf16) && pairs > (c.dt == RIFTKV_BF16 ? 56 : 900) * 1000;
         front_parts = front_wgs = 0;
         row_tiles = (int)((rows + kRows - 1) / kRows);
         parts = parts_alone(c.dt, items, own);
@@ -455,8 +457,8 @@ struct SharedPlan {
         if (by_rows) {
             const int64_t tiles = (prefix_len + kTokens - 1) / kTokens;
             // A workgroup a CU, so that the sequences' own tokens have the other half of it; more where a tile has few bytes or
-            // is widened (64 sequences after 32,768 tokens, groups of 4, with 256 and 384: bf16 73.5 and 74.4 us, 8,192 tokens in
-            // groups of 1 22.4 and 24.9; e4m3 90.6 and 84.1; 64 dimensions 57.3 and 53.9).
+            // is widened (64 sequences after 32,768 tokens, groups of 4, with 256 and 384: bf16 91.0 and 91.7 us, 8,192 tokens in
+            // groups of 1 38.1 and 40.3; e4m3 108 and 106, int8 111 and 105, e4m3 of 64 dimensions 79 and 71).
             int64_t n = (c.dt == RIFTKV_BF16 && c.head_dim == 128 ? 256 : kMostPrefixWgs) / wgs;
             if (n > tiles / 2) n = tiles / 2;
             front_parts = n < 1 ? 1 : n > kMaxParts ? kMaxParts : (int)n;

@@ -1,0 +1,69 @@
+"""How exact the weights of a shared prefix are where it is gone through for 128 query rows at a time: as everywhere else."""
+import math
+
+import pytest
+import torch
+
+from tests.kv_ranges_testlib import TYPES, filled, half_step
+from tests.test_gpu_kv_prefix_rows import held, pairs
+from tests.test_gpu_kv_ranges import shared
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def R():
+    import paper_2609_29029_amd as R
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    R.load()
+    return R
+
+
+# Sequences with 64 rows of one key head each: enough (16 rows, token) pairs for 128 rows at a time.
+SEQS, GROUP, HD = 26, 64, 64
+LENGTH = {"bf16": 4161, "fp8": 9000, "int8": 9000}
+
+
+def terms(x):
+    """Three bf16 numbers that add up to x, to 2^-24 of it."""
+    out = []
+    for _ in range(3):
+        t = float(torch.tensor(x, dtype=torch.float64).bfloat16())
+        out.append(t)
+        x -= t
+    return out
+
+
+@pytest.mark.parametrize("dt, store", [("bf16", "bf16"), ("bf16", "fp8"), ("bf16", "int8"), ("f32", "bf16")])
+def test_every_bit_of_a_weight(R, dt, store):
+    """A weight of 0.5 (1 + 2^-8 + 2^-16), halfway between two sums of two bf16 numbers and 2^-16 from either, against
+    weights that two numbers hold: what is left of the sum is the last 2^-17."""
+    prefix = LENGTH[store]
+    assert pairs(1, GROUP, prefix, SEQS) > (56000 if store == "bf16" else 900000)
+    P = filled(R, store, 1, HD, 16, [prefix] + [0] * SEQS)
+    # scores by token: 0; the odd weight's; those of 0.5; all others none at all
+    q = torch.zeros(SEQS, GROUP, HD, dtype=torch.float64)
+    for i, x in enumerate(terms(math.log(0.5 * (1 + 2.0 ** -8 + 2.0 ** -16))) + terms(math.log(0.5)) + [-200.0]):
+        q[:, :, i] = x
+    q = q.to(TYPES[dt]).cuda()
+    k = torch.zeros(prefix, 1, HD, dtype=torch.bfloat16)
+    v = torch.zeros(prefix, 1, HD, dtype=torch.bfloat16)
+    k[:, 0, 6] = 1
+    place = (70, 77, 130, 131)                                  # one tile's two halves, and the next one
+    k[place, 0] = 0
+    k[place[1], 0, 0:3] = 1
+    k[place[2:], 0, 3:6] = 1
+    v[place[1]] = 1
+    v[place[2]] = -1
+    v[place[3]] = -2.0 ** -8
+    P.put(R, 0, k.cuda(), v.cuda())
+    out = shared(R, P, q, prefix, [0] * SEQS, scale=1.0)
+    kd, vd = (x[:, 0].cpu() for x in held(P, 0, prefix))
+    w = torch.softmax(kd @ q[0, 0].double().cpu(), 0)
+    want = w @ vd
+    # Scores of three products and two roundings, of up to 0.7; an exponential of 2^-22 and twice the scores' error; four
+    # weights that are not zero are added up, in parts of the prefix and then the parts; two more roundings.
+    err = (2 * (3 + 2) * 2.0 ** -24 * 0.7 + 2.0 ** -22 + 12 * 2.0 ** -24) * (w @ vd.abs()) + half_step(TYPES[dt]) * want.abs()
+    off = (out.double().cpu() - want).abs()
+    assert bool((off <= err).all()), float((off / err).max())
+    assert float(err[0]) < 0.5 * 2.0 ** -17 * float(w[place[0]])      # a weight short by 2^-17 of it would be seen
