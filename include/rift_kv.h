@@ -233,8 +233,9 @@ RIFT_API size_t riftkv_attention_shared_workspace_size(const riftkv_cache* cache
  * prefix_len   [host] tokens of the prefix, >= 0
  * lens         [n_seq] i32 in [0, max_pages * page_size], the prefix not counted
  * A page of the prefix outside [0, n_pages) sets the status and makes every sequence's output NaN; a sequence
- * without any token gives zeros.  Weights of the prefix may be as large as 2^8 before their sum divides them: values (or scales of
- * 8-bit rows) past 2^119 may overflow where they do not in riftkv_attention.  Everything else as for riftkv_attention.
+ * without any token gives zeros.  The largest weight of a query, before the sum divides them, is 1 in riftkv_attention and may here be as
+ * small as 2^-8 for a prefix: 8-bit rows' scales lose bits below 2^-102, and sums of values below 2^-118 have fewer bits.  Everything
+ * else as for riftkv_attention.
  * Shape rules: prefix_len <= 2^30, n_seq * n_heads <= 2^26.
  */
 RIFT_API rift_status riftkv_attention_shared(const riftkv_cache* cache, const void* q, int64_t ld_q, int32_t n_heads,

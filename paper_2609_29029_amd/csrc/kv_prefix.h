@@ -45,7 +45,7 @@ constexpr int kStageBytes = 2 * kTileBytes;   // keys, then values
 constexpr int kScaleFloats = 4 * 2 * kTokens; // of keys and values, four tiles
 constexpr size_t kPrefixLds = 2 * kStageBytes + kScaleFloats * sizeof(float);
 static_assert(kPrefixLds >= kRows * (128 + 4) * sizeof(float), "the rows of a workgroup");
-constexpr float kLazy = 8.f;                  // log2 units by which a score may pass the reference
+constexpr float kLazy = 8.f;                  // log2 units that a reference is set above the largest score
 
 typedef short v4s_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
@@ -284,9 +284,10 @@ __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, un
         for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * scale;
-        // It moves only when a score passes it by more than kLazy: weights stay below 2^kLazy, and the sums are rescaled for
-        // few tiles.
-        const float mn = mx > m + kLazy ? mx : m;
+        // It moves only when a score passes it, and then to kLazy above that: weights are 1 at most, the largest 2^-kLazy at
+        // least, and the sums are rescaled for few tiles.  (Set at the largest score, to be passed by kLazy, weights of up to 2^kLazy
+        // made sums of large values overflow that do not with a running maximum.)
+        const float mn = mx > m ? mx + kLazy : m;
         const float f = __builtin_amdgcn_exp2f(m - ref_of(mn));
         m = mn;
         l *= f;

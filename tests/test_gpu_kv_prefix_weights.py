@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests.kv_ranges_testlib import TYPES, filled, half_step
-from tests.test_gpu_kv_prefix_rows import held, pairs
+from tests.test_gpu_kv_prefix_rows import check_prefix, held, pairs
 from tests.test_gpu_kv_ranges import shared
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +67,40 @@ def test_every_bit_of_a_weight(R, dt, store):
     off = (out.double().cpu() - want).abs()
     assert bool((off <= err).all()), float((off / err).max())
     assert float(err[0]) < 0.5 * 2.0 ** -17 * float(w[place[0]])      # a weight short by 2^-17 of it would be seen
+
+
+@pytest.mark.parametrize("dt, store", [("bf16", "bf16"), ("bf16", "fp8"), ("bf16", "int8"), ("f32", "bf16")])
+@pytest.mark.parametrize("exponent", [-100, 114])
+def test_large_and_small_values(R, dt, store, exponent):
+    """Values of 2^114, whose sum over all tokens is below 2^128, as a running maximum's sum is: scores that are 2^7.8 apart in
+    every tile, the smaller ones first.  And values that are as small."""
+    prefix = LENGTH[store]
+    assert pairs(1, GROUP, prefix, SEQS) > (56000 if store == "bf16" else 900000) and prefix * 1.125 * 2.0 ** 114 < 2.0 ** 128
+    P = filled(R, store, 1, HD, 16, [prefix] + [0] * SEQS)
+    k = torch.zeros(prefix, 1, HD)
+    k[:, 0, 0] = (torch.arange(prefix) % 64 >= 32).float()
+    v = 1 + torch.randint(0, 2, (prefix, 1, HD), generator=torch.Generator().manual_seed(3)) / 8
+    v = torch.ldexp(v, torch.tensor(exponent))
+    P.put(R, 0, k.bfloat16().cuda(), v.bfloat16().cuda())
+    q = torch.zeros(SEQS, GROUP, HD, dtype=TYPES[dt], device="cuda")
+    q[:, :, 0] = 7.8 * math.log(2)
+    out = shared(R, P, q, prefix, [0] * SEQS, scale=1.0)
+    assert bool(torch.isfinite(out).all())
+    out = out.double() * 2.0 ** -exponent                        # (the check's smallest bound is 1e-30)
+    P.v = (P.v.double() * 2.0 ** -exponent).to(P.store) if P.vs is None else P.v
+    if P.vs is not None:
+        P.vs = (P.vs.int() - exponent).to(torch.uint8)
+    check_prefix(P, q, prefix, [0] * SEQS, out, scale=1.0)
+
+
+def test_values_below_the_weights_bits(R):
+    """8-bit rows whose scale is 2^-100: a weight of 2^-8 or more times it still has all its bits above 2^-133."""
+    prefix = LENGTH["int8"]
+    P = filled(R, "int8", 1, HD, 16, [prefix] + [0] * SEQS)
+    k = torch.randn(prefix, 1, HD, generator=torch.Generator().manual_seed(5)).bfloat16()
+    v = torch.ldexp(torch.randint(64, 128, (prefix, 1, HD), generator=torch.Generator().manual_seed(6)).float(), torch.tensor(-100))
+    P.put(R, 0, k.cuda(), v.bfloat16().cuda())
+    q = torch.randn(SEQS, GROUP, HD, generator=torch.Generator().manual_seed(7)).bfloat16().cuda()
+    out = shared(R, P, q, prefix, [0] * SEQS)
+    P.vs = (P.vs.int() + 100).to(torch.uint8)
+    check_prefix(P, q, prefix, [0] * SEQS, out.double() * 2.0 ** 100)
