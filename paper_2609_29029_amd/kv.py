@@ -93,6 +93,17 @@ def _load() -> ctypes.CDLL:
 # A call's checks are part of its cost: devices are compared by index, and what the calls of a decode
 # step check of each tensor stands in them in line (a write 7.3 -> 6.7 us a call, 3.1 of it the launch); these functions then say what is
 # wrong, or that nothing is.
+def _int32(x, name):
+    """A number that the C ABI takes in 32 bits: ctypes would cut a larger one off."""
+    if not -0x80000000 <= x <= 0x7FFFFFFF:
+        raise ValueError(f"{name}: {x} does not fit 32 bits")
+    return x
+
+
+def _too_many():
+    raise ValueError("more rows, heads, sequences or pages than 31 bits count")
+
+
 def _dense(t, dtype, shape, device, name):
     """Address of a contiguous device tensor; shape None: any."""
     if t.dtype != dtype:
@@ -198,9 +209,10 @@ def riftkv_rope_freqs(rotary_dim: int, base: float = 10000.0, scaling: str = "no
     import numpy as np
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"scaling: one of {ROPE_SCALINGS}")
-    cfg = _RopeStruct(int(rotary_dim), ROPE_SCALINGS.index(scaling), float(base), float(factor), float(original_len),
+    rotary_dim = _int32(int(rotary_dim), "rotary_dim")
+    cfg = _RopeStruct(rotary_dim, ROPE_SCALINGS.index(scaling), float(base), float(factor), float(original_len),
                       float(low), float(high))
-    out = np.zeros(max(1, int(rotary_dim) // 2), dtype=np.float64)
+    out = np.zeros(max(1, rotary_dim // 2), dtype=np.float64)
     mag = ctypes.c_double(0.0)
     _check(_load().riftkv_rope_freqs(ctypes.byref(cfg), out.ctypes.data, ctypes.byref(mag)), "riftkv_rope_freqs")
     return out, float(mag.value)
@@ -221,14 +233,16 @@ def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, str
         raise ValueError("q or k is needed")
     if x.dim() != 3:
         raise ValueError("rows: expected [rows][heads][head_dim]")
-    dev, dtype, (rows, _, hd) = x.get_device(), x.dtype, x.shape
+    dev, dtype, (rows, heads, hd) = x.get_device(), x.dtype, x.shape
+    if (rows | heads | hd) >> 31:
+        _too_many()
     dt = _ROWS.get(dtype)
     if dt is None or dev < 0:
         _device_of(x, "rows")
         _row_type(x, "rows")
     pq = lq = nq = poq = loq = pk = lk = nk = pok = lok = 0
     if q is not None:
-        nq = x.shape[1]
+        nq = heads
         pq, lq = _rope_rows(q, dtype, rows, nq, hd, dev, "q")
         poq, loq = (pq, lq) if q_out is None else _rope_rows(q_out, dtype, rows, nq, hd, dev, "q_out")
     elif q_out is not None:
@@ -237,6 +251,8 @@ def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, str
         if k.dim() != 3:
             raise ValueError("rows: expected [rows][heads][head_dim]")
         nk = k.shape[1]
+        if nk >> 31:
+            _too_many()
         pk, lk = _rope_rows(k, dtype, rows, nk, hd, dev, "k")
         pok, lok = (pk, lk) if k_out is None else _rope_rows(k_out, dtype, rows, nk, hd, dev, "k_out")
     elif k_out is not None:
@@ -251,6 +267,8 @@ def _rope(name, fn, q, k, positions, freqs, q_out, k_out, layout, magnitude, str
         if axes.shape != freqs.shape:
             raise ValueError("axes: expected as many as freqs")
         shape = (positions.shape[0], rows)
+        if shape[0] >> 31:
+            _too_many()
         places = shape
         by_axis = (_host(axes, _I4, ctypes.c_int32, "axes: expected a contiguous int32 array"),)
     if positions.dtype is not _I32 or positions.shape != shape or not positions.is_contiguous() or positions.get_device() != dev:
@@ -294,6 +312,9 @@ def riftkv_rope_axes(q, k, positions, freqs, axes, q_out=None, k_out=None, layou
 def _move(name, fn, cache, k, v, page_table, positions, status, seq_ids, stream):
     dev, hd, dtype, i32, rows = cache.device, cache.head_dim, k.dtype, _I32, k.shape[0]
     shape, one = (rows, cache.n_kv_heads, hd), (rows,)
+    n_seq, max_pages = page_table.shape
+    if (rows | n_seq | max_pages) >> 31:
+        _too_many()
     dt = _ROWS.get(dtype)
     if dt is None:
         _row_type(k, "k")
@@ -312,7 +333,6 @@ def _move(name, fn, cache, k, v, page_table, positions, status, seq_ids, stream)
         pv, ldv = _rows(v, dtype, shape, dev, "v")
     elif rows < 2:
         ldv = shape[1] * hd
-    n_seq, max_pages = page_table.shape
     if page_table.dtype is not i32 or not page_table.is_contiguous() or page_table.get_device() != dev:
         _dense(page_table, i32, None, dev, "page_table")
     if positions.dtype is not i32 or positions.shape != one or not positions.is_contiguous() or positions.get_device() != dev:
@@ -346,7 +366,8 @@ def riftkv_read(cache: KvCache, page_table, positions, k_out, v_out, status, seq
 
 # ----------------------------------------------------------------------------- attention
 def riftkv_attention_workspace_size(cache: KvCache, n_seq: int, n_heads: int, max_pages: int) -> int:
-    return int(_load().riftkv_attention_workspace_size(cache.ref, int(n_heads), int(n_seq), int(max_pages)))
+    return int(_load().riftkv_attention_workspace_size(cache.ref, _int32(int(n_heads), "n_heads"), _int32(int(n_seq), "n_seq"),
+                                                       _int32(int(max_pages), "max_pages")))
 
 
 def riftkv_attention(cache: KvCache, q, page_table, lens, out, workspace, status, scale: Optional[float] = None,
@@ -356,6 +377,8 @@ def riftkv_attention(cache: KvCache, q, page_table, lens, out, workspace, status
     dev, hd, dtype, i32 = cache.device, cache.head_dim, q.dtype, _I32
     n_seq, max_pages = page_table.shape
     n_heads = q.shape[1]
+    if (n_seq | max_pages | n_heads) >> 31:
+        _too_many()
     shape = (n_seq, n_heads, hd)
     dt = _ROWS.get(dtype)
     if dt is None:
@@ -400,6 +423,8 @@ def _queries(cache, q, page_table, lens, status):
     if dt is None:
         _row_type(q, "q")
     n, n_heads, width = q.shape
+    if (n_seq | max_pages | n_heads) >> 31:
+        _too_many()
     pq = q.data_ptr()
     ldq, sh, se = q.stride()
     if n != n_seq or width != hd or q.get_device() != dev or se != 1 or sh != hd:
@@ -434,6 +459,8 @@ def _lists(cache, pages, n_seq, dev):
     shape = pages.shape
     if len(shape) != 3:
         raise ValueError("pages: expected [n_seq][n_kv_heads][top]")
+    if shape[2] >> 31:
+        _too_many()
     if shape[0] != n_seq or shape[1] != cache.n_kv_heads or pages.dtype is not _I32 or not pages.is_contiguous() or pages.get_device() != dev:
         _dense(pages, _I32, (n_seq, cache.n_kv_heads, shape[2]), dev, "pages")
     return pages.data_ptr(), shape[2]
@@ -446,13 +473,15 @@ def _bounds(cache, bounds):
 
 
 def riftkv_attention_shared_workspace_size(cache: KvCache, n_seq: int, n_heads: int, prefix_len: int, max_pages: int) -> int:
-    return int(_lib.riftkv_attention_shared_workspace_size(cache.ref, int(n_heads), int(n_seq), int(prefix_len), int(max_pages)))
+    return int(_lib.riftkv_attention_shared_workspace_size(cache.ref, _int32(int(n_heads), "n_heads"), _int32(int(n_seq), "n_seq"),
+                                                           _int32(int(prefix_len), "prefix_len"), _int32(int(max_pages), "max_pages")))
 
 
 def riftkv_attention_shared(cache: KvCache, q, prefix_table, prefix_len: int, page_table, lens, out, workspace, status,
                             scale: Optional[float] = None, stream=None) -> None:
     """out[i] := attention of q[i] [n_heads][head_dim] over the prefix_len tokens of the pages prefix_table [pages] i32
     and then the first lens[i] tokens of sequence i's own pages; scale None: 1 / sqrt(head_dim)."""
+    _int32(prefix_len, "prefix_len")
     dev, dt, n_seq, max_pages, n_heads, pq, ldq = _queries(cache, q, page_table, lens, status)
     if prefix_table.dtype is not _I32 or not prefix_table.is_contiguous() or prefix_table.get_device() != dev:
         _dense(prefix_table, _I32, None, dev, "prefix_table")
@@ -473,6 +502,8 @@ def riftkv_page_bounds(cache: KvCache, bounds, page_table, lens, status, begins=
     of the pages that hold tokens begins[i] (None: 0) .. lens[i] - 1 of every sequence."""
     dev, i32 = cache.device, _I32
     n_seq, max_pages = page_table.shape
+    if (n_seq | max_pages) >> 31:
+        _too_many()
     to = _bounds(cache, bounds)
     table = _dense(page_table, i32, None, dev, "page_table")
     n = _dense(lens, i32, (n_seq,), dev, "lens")
@@ -486,13 +517,15 @@ def riftkv_page_bounds(cache: KvCache, bounds, page_table, lens, status, begins=
 
 
 def riftkv_select_pages_workspace_size(cache: KvCache, n_seq: int, max_pages: int) -> int:
-    return int(_lib.riftkv_select_pages_workspace_size(cache.ref, int(n_seq), int(max_pages)))
+    return int(_lib.riftkv_select_pages_workspace_size(cache.ref, _int32(int(n_seq), "n_seq"), _int32(int(max_pages), "max_pages")))
 
 
 def riftkv_select_pages(cache: KvCache, bounds, q, page_table, lens, pages, workspace, status, keep_first: int = 1,
                         keep_last: int = 1, stream=None) -> None:
     """pages [n_seq][n_kv_heads][top] i32 := the places in its row of page_table of the `top` pages that each sequence's
     token needs most of each key head, ascending, -1 behind them; the first keep_first and last keep_last always."""
+    _int32(keep_first, "keep_first")
+    _int32(keep_last, "keep_last")
     dev, dt, n_seq, max_pages, n_heads, pq, ldq = _queries(cache, q, page_table, lens, status)
     of = _bounds(cache, bounds)
     to, top = _lists(cache, pages, n_seq, dev)
@@ -506,7 +539,7 @@ def riftkv_select_pages(cache: KvCache, bounds, q, page_table, lens, pages, work
 
 
 def riftkv_attention_pages_workspace_size(cache: KvCache, n_seq: int, n_heads: int, top: int) -> int:
-    return int(_lib.riftkv_attention_pages_workspace_size(cache.ref, int(n_heads), int(n_seq), int(top)))
+    return int(_lib.riftkv_attention_pages_workspace_size(cache.ref, _int32(int(n_heads), "n_heads"), _int32(int(n_seq), "n_seq"), _int32(int(top), "top")))
 
 
 def riftkv_attention_pages(cache: KvCache, q, page_table, lens, pages, out, workspace, status, scale: Optional[float] = None,
@@ -527,7 +560,7 @@ def riftkv_attention_pages(cache: KvCache, q, page_table, lens, pages, out, work
 
 # ----------------------------------------------------------------------------- decode
 def riftkv_decode_workspace_size(cfg: ModelCfg, cache: KvCache, n_seq: int, max_pages: int) -> int:
-    return int(_load().riftkv_decode_workspace_size(ctypes.byref(cfg), cache.ref, int(n_seq), int(max_pages)))
+    return int(_load().riftkv_decode_workspace_size(ctypes.byref(cfg), cache.ref, _int32(int(n_seq), "n_seq"), _int32(int(max_pages), "max_pages")))
 
 
 def riftkv_decode_step(cfg: ModelCfg, layers: Sequence[dict], x_new, cache: KvCache, page_table, positions, hidden_out,
@@ -542,6 +575,8 @@ def riftkv_decode_step(cfg: ModelCfg, layers: Sequence[dict], x_new, cache: KvCa
         for n, t in w.items():
             _dense(t, torch.bfloat16, None, dev, n)
     n_seq, max_pages = page_table.shape
+    if (n_seq | max_pages) >> 31:
+        _too_many()
     x = _dense(x_new, torch.bfloat16, (n_seq, cfg.d), dev, "x_new")
     out = _dense(hidden_out, torch.float32, (n_seq, cfg.d), dev, "hidden_out")
     table = _dense(page_table, torch.int32, None, dev, "page_table")
