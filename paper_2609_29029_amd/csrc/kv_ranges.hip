@@ -419,10 +419,12 @@ int parts_of(int64_t items, int64_t tiles) {
 
 // The same where a split alone costs a launch to join the parts, which pays for long items that are few.  In us, whole and in parts:
 // 96 items of 20 tiles 12.2 and 13.2, e4m3 of 64 dimensions 7.9 and 8.7; 32 of 20 9.5 and 8.8, e4m3 10.6 and 8.6; 16 of 12 6.9 and 8.1.  Float32
-// pages, whose products take longer: 96 of 20 29.2 and 23.9, of 64 dimensions 16.1 and 14.3; 32 of 20 24.6 and 13.9; 160 of 30 47.8
-// and 44.3; 192 of up to 31 44.0 and 46.4; 16 of 12 13.4 and 11.2.
+// pages, whose products take longer, of 128 (and 64) dimensions: 64 of 10 14.3 and 14.5 (9.5 and 11.0), of 12 14.9 and 12.4 (9.4 and
+// 9.7), of 20 24.3 and 18.3 (12.3 and 11.2); 96 of 12 17.4 and 18.2 (9.0 and 11.1), of 20 26.8 and 19.7 (13.9 and 12.2); 160 of 16 23.9 and 24.9,
+// of 20 29.4 and 27.9 (16.1 and 16.7), of 30 41.8 and 35.3 (23.7 and 21.7); in two parts 176 of 20 29.4 and 33.5, 192 of up to 31 40.9 and
+// 44.4, 256 of 64 91.9 and 97.0.
 int parts_alone(riftkv_dtype dt, int64_t items, int64_t tiles) {
-    const bool split = dt == RIFTKV_F32 ? items <= kMostSplit && tiles >= 8 : items <= 128 && tiles >= (items <= 64 ? 20 : 24);
+    const bool split = dt == RIFTKV_F32 ? items <= kMostSplit / 3 && tiles >= (items <= 64 ? 12 : 20) : items <= 128 && tiles >= (items <= 64 ? 20 : 24);
     return split ? parts_of(items, tiles) : 1;
 }
 

@@ -3,7 +3,7 @@ bounds of large pages."""
 import pytest
 import torch
 
-from tests.kv_ranges_testlib import TYPES, bounds_of, filled, half_step, randn
+from tests.kv_ranges_testlib import TYPES, attend_lists, bounds_of, check, filled, half_step, randn
 from tests.test_gpu_kv_select import i32, new_bounds, same
 
 pytestmark = pytest.mark.gpu
@@ -61,6 +61,22 @@ def test_lists_keep_to_their_workspace(R, dt, store, n_kv, group, seqs, top):
     ws = Guarded(R.riftkv_attention_pages_workspace_size(P.cache, seqs, n_kv * group, top))
     R.riftkv_attention_pages(P.cache, q, P.table, i32(lens), lists, out, ws.space, P.status)
     assert ws.kept() and bool(torch.isfinite(out.float()).all()) and int(P.status) == 0
+
+
+@pytest.mark.parametrize("n_kv, seqs", [(16, 4), (13, 5), (17, 10), (19, 9)])
+@pytest.mark.parametrize("top", [23, 24, 39, 40])
+def test_float32_lists_in_parts_and_whole(R, n_kv, seqs, top):
+    """64, 65, 170 and 171 lists of 12 and 20 tiles, and of one less."""
+    lens = [16 * top + 40 - i for i in range(seqs)]
+    P = filled(R, "f32", n_kv, 64, 16, lens, seed=top)
+    q = randn(2, seqs, n_kv, 64, dtype=torch.float32, scale=2)
+    g = torch.Generator().manual_seed(seqs)
+    lists = torch.stack([torch.stack([torch.randperm(-(-n // 16), generator=g)[:top] for _ in range(n_kv)]) for n in lens]).int().cuda()
+    out = torch.full_like(q, 7.0)
+    ws = Guarded(R.riftkv_attention_pages_workspace_size(P.cache, seqs, n_kv, top))
+    R.riftkv_attention_pages(P.cache, q, P.table, i32(lens), lists, out, ws.space, P.status)
+    check(out, *attend_lists(P, q, lens, lists), q.dtype)
+    assert ws.kept() and int(P.status) == 0
 
 
 @pytest.mark.parametrize("dt, store", [("bf16", "bf16"), ("f32", "f32")])
