@@ -12,7 +12,7 @@
  *   riftkv_read       rows of the pages back, as dense rows
  *   riftkv_attention  one new token of every sequence over its pages
  *   riftkv_attention_shared  the same after a prefix that all sequences share,
- *                     read once for all
+ *                     read for many of them at a time
  *   riftkv_page_bounds, riftkv_select_pages, riftkv_attention_pages
  *                     the same over the pages that promise the largest scores
  *   riftkv_decode_step  a decode step of rift.h's model over them
@@ -228,7 +228,8 @@ RIFT_API size_t riftkv_attention_shared_workspace_size(const riftkv_cache* cache
 /*
  * riftkv_attention_shared -- riftkv_attention of sequences that all begin with the same prefix_len tokens: each
  * attends to those and then to the first lens[i] tokens of its own pages, its own row i of page_table.  The prefix'
- * keys and values are read once for all sequences, not once for each.
+ * keys and values are read once for every 128 query rows of a key head (a sequence has n_heads / n_kv_heads), or every 16 where there
+ * is little to do and where the pages are f32, or 8-bit with f32 queries; by every sequence if the prefix has 256 tokens at most.
  * prefix_table [ceil(prefix_len / page_size)] i32 pages of the prefix; its last page need not be full
  * prefix_len   [host] tokens of the prefix, >= 0
  * lens         [n_seq] i32 in [0, max_pages * page_size], the prefix not counted
