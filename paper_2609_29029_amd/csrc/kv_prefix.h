@@ -279,11 +279,17 @@ __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, un
                 for (int e = 0; e < 4; ++e) s[i + e] *= f[e];
             }
         }
+        // A rounding of its own: fused with the reference's subtraction, scores past 2^31 would be whole exponents off it.
+        {
+#pragma clang fp contract(off)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] *= scale;
+        }
         float mx = s[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-        mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * scale;
+        mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
         // It moves only when a score passes it, and then to kLazy above that: weights are 1 at most, the largest 2^-kLazy at
         // least, and the sums are rescaled for few tiles.  (Set at the largest score, to be passed by kLazy, weights of up to 2^kLazy
         // made sums of large values overflow that do not with a running maximum.)
@@ -293,7 +299,7 @@ __device__ __forceinline__ void prefix_body(const PrefixParams& p, int block, un
         l *= f;
         return f;
     };
-    auto weight = [&](float s, float neg_ref) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(fmaf(s, scale, neg_ref)); };
+    auto weight = [&](float s, float neg_ref) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(s + neg_ref); };
     // The j-th two weights, as a word of each of the second product's operands.
     auto split_pair = [&](int t, int kb, int j, float a, float b, uint32_t(&y)[NP]) __attribute__((always_inline)) {
         l += a;

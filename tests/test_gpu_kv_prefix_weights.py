@@ -104,3 +104,34 @@ def test_values_below_the_weights_bits(R):
     out = shared(R, P, q, prefix, [0] * SEQS)
     P.vs = (P.vs.int() + 100).to(torch.uint8)
     check_prefix(P, q, prefix, [0] * SEQS, out.double() * 2.0 ** 100)
+
+
+@pytest.mark.parametrize("dt, store", [("bf16", "bf16"), ("bf16", "fp8"), ("bf16", "int8"), ("f32", "bf16")])
+@pytest.mark.parametrize("exponent", [10, 20, 34, 60])
+@pytest.mark.parametrize("scale", [1.0, -0.3])
+@pytest.mark.parametrize("seqs, prefix", [(SEQS, None), (2, 700), (2, 200)])
+def test_scores_of_any_size(R, dt, store, exponent, scale, seqs, prefix):
+    """Scores of 2^10 to 2^60, whose last bit is worth far more than an exponent can be: the tokens of the largest one share all
+    the weight.  By 128 rows, by 16, and a prefix that every sequence walks."""
+    prefix = prefix or LENGTH[store]
+    P = filled(R, store, 1, HD, 16, [prefix] + [0] * seqs)
+    g = torch.Generator().manual_seed(exponent)
+    k = torch.zeros(prefix, 1, HD)
+    k[:, 0, 0] = torch.randint(-100, 101, (prefix,), generator=g).float() / 64
+    k[:, 0, 1] = 1
+    P.put(R, 0, k.bfloat16().cuda(), torch.randn(prefix, 1, HD, generator=g).bfloat16().cuda())
+    q = torch.zeros(seqs, GROUP, HD, dtype=TYPES[dt], device="cuda")
+    q[:, ::2, 0], q[:, 1::2, 0] = 2.0 ** exponent, -1.25 * 2.0 ** exponent
+    q[:, ::3, 1] = 1.0
+    out = shared(R, P, q, prefix, [0] * seqs, scale=scale)
+    kd, vd = (x[:, 0].cpu() for x in held(P, 0, prefix))
+    for row in range(6):
+        s = (kd @ q[0, row].double().cpu()) * scale
+        assert exponent < 20 or float(s.max() - s[s < s.max()].max()) > 1000
+        if exponent >= 20:
+            best = s == s.max()
+            want = vd[best].mean(0)
+            err = (int(best.sum()) + 8) * 2.0 ** -24 * vd[best].abs().mean(0) + half_step(TYPES[dt]) * want.abs() * (1 + 1e-3)
+            assert bool(((out[:, row].double().cpu() - want).abs() <= err).all()), row
+    if exponent < 20:
+        check_prefix(P, q, prefix, [0] * seqs, out, scale=scale)
