@@ -11,8 +11,8 @@
 // queries, and all weights, go into the products as three bf16 terms that add up to them.
 //
 // Bound by the products and the weights' vector instructions together, which overlap only in part: of a wave's tile 64 products of
-// 32 cycles and some 240 vector instructions with 32 exponentials of 16.  64 sequences' 256 rows after 32,768 tokens, 8 key heads,
-// bf16: 34 GFLOP in 75 us alone (134 MB), and 80.5 with the sequences' own 79 MB beside it (with two terms a weight, which are up
+// 32 cycles and some 270 vector instructions with 32 exponentials of 16.  64 sequences' 256 rows after 32,768 tokens, 8 key heads,
+// bf16: 34 GFLOP in 76 us alone (134 MB), and 81.5 with the sequences' own 79 MB beside it (with two terms a weight, which are up
 // to 2^-16 of it off, 66); every sequence on its own read the prefix 64 times and took 606.  Kept, measured with two terms: halves
 // of a tile in a pipeline, a product and then two weights in turn (61 us a launch of 256 workgroups, 70 without); not kept: more of
 // the next tiles touched ahead into L2, operands two products ahead (no change).
